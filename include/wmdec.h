@@ -258,6 +258,110 @@ int wmdec_adaln_fused_projection(const void* c, int c_dtype, const void* w_fused
                                  int apply_silu, void* stream);
 
 /* ------------------------------------------------------------------------
+ * What stands around the AdaLN projections in a transformer block (the "DiT
+ * block" whose modulation Sec. IV-B-2 fuses; the paper gives no more of it):
+ * the gated residual with the norms on both of its sides, rotary positions, and
+ * attention to states of another length.  Tokens are rows: [n, t, channels].
+ *
+ * Gated residual and norms, one pass over the rows:
+ *   x' = x + res_scale * gate[n] * P(h)        written to x_out, rounded to x_dtype
+ *   y  = N(x') * (1 + scale[n]) + shift[n]     of x' as stored, rounded to act_dtype
+ * P (post) and N (pre) are norms over the d channels of a row with an optional
+ * affine part: NONE v, LAYER (v - mean) / sqrt(var + eps) with the biased
+ * variance, RMS v / sqrt(mean(v^2) + eps); then * weight + bias (fp32 [d], NULL:
+ * ones, zeros; NONE takes neither).  A NULL wmdec_norm is NONE.
+ * h == NULL: x' = x (the norm in front of a block); x_out, gate and post must be
+ * NULL.  y == NULL: only x' (the end of a block); pre, scale and shift must be NULL.
+ * gate, scale, shift: fp32, d values per sample, mod_stride elements from sample
+ * to sample (0: one vector for all), any of them NULL: ones, zeros, zeros.  With
+ * the output of wmdec_adaln_fused_projection they are out + 2 * d, out + d and
+ * out, mod_stride = rows.
+ * x, x_out: dense [n,t,d] of x_dtype; h, y: of act_dtype.  x_dtype is act_dtype or
+ * F32 (a residual stream in fp32 beside 16-bit blocks).  x_out may be x, and y may
+ * be h (or x, where h is NULL and the types are the same); nothing else may
+ * overlap.  All arithmetic is fp32.  d at most 16384.  Pointers need the alignment of their elements;
+ * rows that are 16-byte aligned (d % 8 == 0) are read in vectors. */
+typedef enum { WMDEC_NORM_NONE = 0, WMDEC_NORM_LAYER = 1, WMDEC_NORM_RMS = 2 } wmdec_norm_kind;
+typedef struct {
+  int kind;
+  float eps;
+  const float* weight;
+  const float* bias;
+} wmdec_norm;
+int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype, const wmdec_norm* post,
+                        const float* gate, float res_scale, void* x_out, const wmdec_norm* pre,
+                        const float* scale, const float* shift, long long mod_stride, void* y,
+                        int n, int t, int d, void* stream);
+
+/* Rotary positions of queries and keys.
+ * wmdec_rope_frequencies writes the angles per unit of position, fp64
+ * [sum(axis_dim) / 2] (device memory), once per model.  Axis a owns axis_dim[a]
+ * (even) consecutive channels of a head; its pair j turns by
+ *   f = base^(-2j / axis_dim[a])                                   PLAIN
+ *   f / factor                                                     LINEAR
+ *   (base * factor^(D / (D - 2)))^(-2j / D), D = axis_dim[a] > 2   BASE
+ *   f * (w + (1 - w) / factor),                                    RAMP
+ *     w = clamp((trained_length * f / 2pi - low_turns) / (high_turns - low_turns), 0, 1)
+ * (the last three stretch positions past the trained length).
+ *
+ * wmdec_rope: with theta = positions[token][a] * f in fp64,
+ *   (u, v) -> magnitude * (u cos theta - v sin theta, u sin theta + v cos theta)
+ * for every pair, channels sum(axis_dim) .. d - 1 copied.  Pairs of an axis are
+ * channels (2j, 2j + 1) if interleaved, else (j, j + axis_dim / 2), counted from
+ * the axis' first channel.  inverse: -theta, which for the same magnitude is also
+ * the gradient of the operator.  q, k: [n, t, heads, d] through strides in
+ * elements, channels contiguous (parts of a fused projection need no copy); k may
+ * be NULL.  Outputs may be the inputs themselves (same pointer and strides); no
+ * other overlap.  positions: int32 [t][axes], positions_stride elements from
+ * sample to sample (0: the same for all).  1 to 3 axes.  Rotations are exact to
+ * fp32 for every int32 position; one rounding to dtype. */
+typedef enum { WMDEC_ROPE_PLAIN = 0, WMDEC_ROPE_LINEAR = 1, WMDEC_ROPE_BASE = 2, WMDEC_ROPE_RAMP = 3 } wmdec_rope_scaling_kind;
+typedef struct {
+  int kind;
+  double base;   /* > 1 */
+  double factor; /* >= 1; PLAIN ignores it */
+  double trained_length, low_turns, high_turns; /* RAMP: > 0, low < high */
+} wmdec_rope_scaling;
+typedef struct {
+  long long sample, token, head;
+} wmdec_strides;
+typedef struct {
+  int axes;
+  int axis_dim[3];
+  int interleaved;
+  int inverse;
+  float magnitude;
+} wmdec_rope_layout;
+int wmdec_rope_frequencies(double* freq, int axes, const int* axis_dim, const wmdec_rope_scaling* scaling, void* stream);
+int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const wmdec_strides* q_out_strides, int heads_q,
+               const void* k, const wmdec_strides* k_strides, void* k_out, const wmdec_strides* k_out_strides, int heads_k,
+               int dtype, const int* positions, long long positions_stride, const double* freq,
+               const wmdec_rope_layout* layout, int n, int t, int d, void* stream);
+
+/* Attention of tq queries to tk keys per sample (the conditioning of a block, the
+ * frames before this one, or, with tq = tk, the tokens themselves):
+ *   o = softmax over the valid keys (scale * q k^T) v
+ * heads_q is a multiple of heads_kv; query head i reads key head
+ * i / (heads_q / heads_kv).  Key j of sample i is valid if j < key_lens[i]
+ * (int32 [n], NULL: tk; clamped to 0 .. tk) and key_mask[i * tk + j] != 0 (bytes,
+ * NULL: all).  What invalid keys and values hold does not matter.  A query with no
+ * valid key, or whose valid scores are all -inf, gets zeros; tk may be 0.
+ * q, o: [n,tq,heads_q,d], k, v: [n,tk,heads_kv,d] of dtype through strides in
+ * elements, channels contiguous.  d: a multiple of 8 (16-bit types) or 4 (F32), at
+ * most 256; pointers and strides multiples of 16 bytes; 128 tokens of k or v span
+ * less than 2 GiB.  scale > 0.  o must not overlap the inputs.
+ * Scores, softmax and sums are fp32; 16-bit types round the probabilities to dtype
+ * for the second product.  F32 is fp32 throughout.  A sample's bits do not depend
+ * on what it is batched with.
+ * workspace: wmdec_cross_attention_workspace_bytes(...) bytes (may be 0) of
+ * 16-byte aligned device memory, no initialisation; one or two kernels. */
+size_t wmdec_cross_attention_workspace_bytes(int dtype, int tk, int n, int tq, int heads_q, int heads_kv, int d);
+int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const void* k, const wmdec_strides* k_strides,
+                          const void* v, const wmdec_strides* v_strides, void* o, const wmdec_strides* o_strides, int dtype,
+                          float scale, const int* key_lens, const unsigned char* key_mask, int n, int tq, int tk,
+                          int heads_q, int heads_kv, int d, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Whole decoder:  latent z[N,latent_c,h,w] -> frame [N,out_c,8h,8w]
  * (the I_t <- VAE_Decode(z_t) step of Alg. 1 / Alg. 2).
  * Graph: conv_in 3x3; mid = ResBlock, attention, ResBlock; per level

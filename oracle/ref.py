@@ -221,3 +221,82 @@ def rel_err(got, want):
     got = np.asarray(got, dtype=np.float64)
     rms = math.sqrt(float(np.mean(want * want)))
     return float(np.max(np.abs(got - want))) / (rms if rms > 0 else 1.0)
+
+
+# ------------------------------------------------------------------ around the AdaLN projections of a transformer block
+def row_norm(v, kind="none", eps=0.0, weight=None, bias=None):
+    """Norm of the rows (last dimension): "none", "layer" (biased variance, two passes) or "rms", then weight and bias."""
+    v = _f64(v)
+    if kind == "none":
+        return v
+    mean = v.mean(-1, keepdims=True) if kind == "layer" else 0.0
+    out = (v - mean) / np.sqrt(((v - mean) ** 2).mean(-1, keepdims=True) + eps)
+    if weight is not None:
+        out = out * _f64(weight)
+    return out if bias is None else out + _f64(bias)
+
+
+def gated_residual(x, h, post=(), gate=None, res_scale=1.0):
+    """x + res_scale * gate * P(h); x, h [n,t,d], gate [n,d]."""
+    b = row_norm(h, *post)
+    return _f64(x) + res_scale * (b if gate is None else b * _f64(gate)[:, None])
+
+
+def norm_modulate(x, pre=(), scale=None, shift=None):
+    """N(x) * (1 + scale) + shift; scale, shift [n,d]."""
+    y = row_norm(x, *pre)
+    if scale is not None:
+        y = y * (1.0 + _f64(scale)[:, None])
+    return y if shift is None else y + _f64(shift)[:, None]
+
+
+def rope_frequencies(axis_dims, base=10000.0, scaling="none", factor=1.0, trained_length=1.0, low_turns=1.0, high_turns=4.0):
+    out = []
+    for dim in axis_dims:
+        for j in range(dim // 2):
+            b = base * factor ** (dim / (dim - 2)) if scaling == "base" else base
+            f = b ** (-2.0 * j / dim)
+            if scaling == "linear":
+                f /= factor
+            if scaling == "ramp":
+                w = min(max((trained_length * f / (2 * math.pi) - low_turns) / (high_turns - low_turns), 0.0), 1.0)
+                f = f * (w + (1 - w) / factor)
+            out.append(f)
+    return np.array(out)
+
+
+def rope(x, positions, freq, axis_dims, interleaved=False, inverse=False, magnitude=1.0):
+    """x [n,t,heads,d], positions [n,t,axes]; pair after pair."""
+    x = _f64(x)
+    out, first, at = x.copy(), 0, 0
+    for axis, dim in enumerate(axis_dims):
+        for j in range(dim // 2):
+            c0, c1 = (first + 2 * j, first + 2 * j + 1) if interleaved else (first + j, first + j + dim // 2)
+            theta = np.asarray(positions)[:, :, axis].astype(np.float64)[:, :, None] * freq[at + j] * (-1.0 if inverse else 1.0)
+            c, s = magnitude * np.cos(theta), magnitude * np.sin(theta)
+            out[..., c0] = x[..., c0] * c - x[..., c1] * s
+            out[..., c1] = x[..., c0] * s + x[..., c1] * c
+        first, at = first + dim, at + dim // 2
+    return out
+
+
+def cross_attention(q, k, v, scale, key_lens=None, key_mask=None):
+    """q [n,tq,hq,d], k, v [n,tk,hk,d] -> (o, a) with o = softmax over the valid keys v, a = the same weights times |v|; a query with
+    no valid key has zeros."""
+    q, k, v = _f64(q), _f64(k), _f64(v)
+    n, tq, hq, d = q.shape
+    tk, hk = k.shape[1:3]
+    o, a = np.zeros((n, tq, hq, d)), np.zeros((n, tq, hq, d))
+    for i in range(n):
+        keep = np.arange(tk) < (tk if key_lens is None else key_lens[i])
+        if key_mask is not None:
+            keep = keep & (np.asarray(key_mask)[i] != 0)
+        if not keep.any():
+            continue
+        for h in range(hq):
+            kk, vv = k[i, keep, h // (hq // hk)], v[i, keep, h // (hq // hk)]
+            s = q[i, :, h] @ kk.T * scale
+            p = np.exp(s - s.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            o[i, :, h], a[i, :, h] = p @ vv, p @ np.abs(vv)
+    return o, a

@@ -811,6 +811,171 @@ int wmdec_adaln_fused_projection(const void* c, int c_dtype, const void* w_fused
   return launch_adaln_projection(c, c_dtype, w_fused, w_dtype, bias, out, batch, d_cond, rows, apply_silu ? 1 : 0, (hipStream_t)stream);
 }
 
+// ---- gated residual and norms
+static inline bool element_aligned(const void* p, size_t size) { return ((uintptr_t)p) % size == 0; }
+static inline bool in_range(long v, long lo, long hi) { return v >= lo && v <= hi; }
+
+static int check_norm(const char* who, const wmdec_norm* in, wmdec_norm* out) {
+  if (!in) return WMDEC_OK;
+  WMDEC_REQUIRE(in_range(in->kind, WMDEC_NORM_NONE, WMDEC_NORM_RMS), WMDEC_ERR_INVALID_ARG, "%s: unknown kind of norm %d", who, in->kind);
+  WMDEC_REQUIRE(in->kind != WMDEC_NORM_NONE || (!in->weight && !in->bias), WMDEC_ERR_INVALID_ARG, "%s: a norm of kind NONE takes no weight and no bias", who);
+  WMDEC_REQUIRE(in->kind == WMDEC_NORM_NONE || (isfinite(in->eps) && in->eps >= 0.f), WMDEC_ERR_INVALID_ARG, "%s: eps must be finite and not negative", who);
+  WMDEC_REQUIRE(element_aligned(in->weight, 4) && element_aligned(in->bias, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  *out = *in;
+  return WMDEC_OK;
+}
+
+int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype, const wmdec_norm* post, const float* gate, float res_scale,
+                        void* x_out, const wmdec_norm* pre, const float* scale, const float* shift, long long mod_stride, void* y,
+                        int n, int t, int d, void* stream) {
+  const char* who = "residual_norm";
+  WMDEC_REQUIRE(x && (h || y), WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(valid_dtype(x_dtype) && valid_dtype(act_dtype), WMDEC_ERR_INVALID_ARG, "%s: bad dtype", who);
+  WMDEC_REQUIRE(x_dtype == act_dtype || x_dtype == WMDEC_F32, WMDEC_ERR_UNSUPPORTED, "%s: x_dtype must be act_dtype or F32", who);
+  WMDEC_REQUIRE(n > 0 && t > 0 && d > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
+  WMDEC_REQUIRE(d <= kResidualNormMaxD, WMDEC_ERR_UNSUPPORTED, "%s: d %d above the limit of %d", who, d, kResidualNormMaxD);
+  WMDEC_REQUIRE((long)n * t <= (1L << 31) - 1, WMDEC_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows", who);
+  WMDEC_REQUIRE(!h || x_out, WMDEC_ERR_INVALID_ARG, "%s: h given without x_out", who);
+  ResidualNormArgs a;
+  int rc = check_norm(who, post, &a.post);
+  if (rc == WMDEC_OK) rc = check_norm(who, pre, &a.pre);
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(h || (!x_out && !gate && a.post.kind == WMDEC_NORM_NONE), WMDEC_ERR_INVALID_ARG, "%s: x_out, gate and post belong to h, which is null", who);
+  WMDEC_REQUIRE(y || (!scale && !shift && a.pre.kind == WMDEC_NORM_NONE), WMDEC_ERR_INVALID_ARG, "%s: pre, scale and shift belong to y, which is null", who);
+  WMDEC_REQUIRE(isfinite(res_scale), WMDEC_ERR_INVALID_ARG, "%s: res_scale must be finite", who);
+  WMDEC_REQUIRE(mod_stride == 0 || mod_stride >= d || n == 1, WMDEC_ERR_SHAPE, "%s: mod_stride %lld below d %d", who, mod_stride, d);
+  const size_t xs = dtype_size(x_dtype), as = dtype_size(act_dtype);
+  WMDEC_REQUIRE(element_aligned(x, xs) && element_aligned(x_out, xs) && element_aligned(h, as) && element_aligned(y, as) && element_aligned(gate, 4) &&
+                    element_aligned(scale, 4) && element_aligned(shift, 4),
+                WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  WMDEC_REQUIRE(!(x_out && x_out == h) && !(y && x_out == y) && !(x == h) && !(y == x && (h || x_dtype != act_dtype)), WMDEC_ERR_INVALID_ARG,
+                "%s: x_out may be x and y may be h (or x without h), nothing else may overlap", who);
+  a.x = x; a.h = h; a.x_out = x_out; a.y = y;
+  a.gate = gate; a.scale = scale; a.shift = shift;
+  a.res_scale = res_scale; a.mod_stride = n == 1 ? 0 : (long)mod_stride;
+  a.n = n; a.t = t; a.d = d;
+  return launch_residual_norm(a, x_dtype, act_dtype, (hipStream_t)stream);
+}
+
+// ---- rotary positions
+static int check_axes(const char* who, int axes, const int* axis_dim, int* rot) {
+  WMDEC_REQUIRE(in_range(axes, 1, 3), WMDEC_ERR_INVALID_ARG, "%s: one to three axes, got %d", who, axes);
+  long sum = 0;
+  for (int i = 0; i < axes; ++i) {
+    WMDEC_REQUIRE(axis_dim[i] > 0 && axis_dim[i] % 2 == 0, WMDEC_ERR_SHAPE, "%s: an axis has an even, positive number of channels, got %d", who, axis_dim[i]);
+    sum += axis_dim[i];
+  }
+  WMDEC_REQUIRE(sum <= kRopeMaxRot, WMDEC_ERR_UNSUPPORTED, "%s: more than %d rotated channels", who, kRopeMaxRot);
+  *rot = (int)sum;
+  return WMDEC_OK;
+}
+
+int wmdec_rope_frequencies(double* freq, int axes, const int* axis_dim, const wmdec_rope_scaling* scaling, void* stream) {
+  const char* who = "rope_frequencies";
+  WMDEC_REQUIRE(freq && axis_dim && scaling && element_aligned(freq, 8), WMDEC_ERR_INVALID_ARG, "%s: null or misaligned pointer", who);
+  int rot = 0;
+  const int rc = check_axes(who, axes, axis_dim, &rot);
+  if (rc != WMDEC_OK) return rc;
+  const wmdec_rope_scaling& s = *scaling;
+  WMDEC_REQUIRE(in_range(s.kind, WMDEC_ROPE_PLAIN, WMDEC_ROPE_RAMP), WMDEC_ERR_INVALID_ARG, "%s: unknown kind of scaling %d", who, s.kind);
+  WMDEC_REQUIRE(isfinite(s.base) && s.base > 1.0, WMDEC_ERR_INVALID_ARG, "%s: base must be above 1", who);
+  WMDEC_REQUIRE(s.kind == WMDEC_ROPE_PLAIN || (isfinite(s.factor) && s.factor >= 1.0), WMDEC_ERR_INVALID_ARG, "%s: factor must be at least 1", who);
+  WMDEC_REQUIRE(s.kind != WMDEC_ROPE_RAMP || (isfinite(s.trained_length) && s.trained_length > 0.0 && isfinite(s.low_turns) && isfinite(s.high_turns) && s.low_turns < s.high_turns),
+                WMDEC_ERR_INVALID_ARG, "%s: a ramp needs a positive trained_length and low_turns < high_turns", who);
+  for (int i = 0; i < axes; ++i)
+    WMDEC_REQUIRE(s.kind != WMDEC_ROPE_BASE || axis_dim[i] > 2, WMDEC_ERR_SHAPE, "%s: a scaled base needs more than two channels an axis", who);
+  return launch_rope_frequencies(freq, axes, axis_dim, s, (hipStream_t)stream);
+}
+
+// not negative, and every element has an offset well below 2^63 bytes
+static bool strides_in_range(const wmdec_strides& s, int n, int t, int heads) {
+  return s.sample >= 0 && s.token >= 0 && s.head >= 0 && (double)n * s.sample + (double)t * s.token + (double)heads * s.head < 0x1p58;
+}
+
+static int check_rope_tensor(const char* who, const void* in, const wmdec_strides* si, void* out, const wmdec_strides* so, int heads, size_t es, int n, int tokens,
+                             RopeTensor* t) {
+  WMDEC_REQUIRE(in && si && out && so, WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(heads > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive number of heads", who);
+  WMDEC_REQUIRE(element_aligned(in, es) && element_aligned(out, es), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  WMDEC_REQUIRE(strides_in_range(*si, n, tokens, heads) && strides_in_range(*so, n, tokens, heads), WMDEC_ERR_INVALID_ARG, "%s: a stride is negative or too large", who);
+  WMDEC_REQUIRE(in != out || (si->sample == so->sample && si->token == so->token && si->head == so->head), WMDEC_ERR_INVALID_ARG,
+                "%s: in place the output has the input's strides", who);
+  t->in = in; t->out = out; t->si = *si; t->so = *so; t->heads = heads;
+  return WMDEC_OK;
+}
+
+int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const wmdec_strides* q_out_strides, int heads_q,
+               const void* k, const wmdec_strides* k_strides, void* k_out, const wmdec_strides* k_out_strides, int heads_k,
+               int dtype, const int* positions, long long positions_stride, const double* freq, const wmdec_rope_layout* layout,
+               int n, int t, int d, void* stream) {
+  const char* who = "rope";
+  WMDEC_REQUIRE(positions && freq && layout, WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(valid_dtype(dtype), WMDEC_ERR_INVALID_ARG, "%s: bad dtype", who);
+  WMDEC_REQUIRE(n > 0 && t > 0 && d > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
+  RopeArgs a;
+  int rc = check_axes(who, layout->axes, layout->axis_dim, &a.rot);
+  if (rc == WMDEC_OK) rc = check_rope_tensor(who, q, q_strides, q_out, q_out_strides, heads_q, dtype_size(dtype), n, t, &a.q);
+  if (rc == WMDEC_OK && k) rc = check_rope_tensor(who, k, k_strides, k_out, k_out_strides, heads_k, dtype_size(dtype), n, t, &a.k);
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(a.rot <= d, WMDEC_ERR_SHAPE, "%s: %d rotated channels in a head of %d", who, a.rot, d);
+  WMDEC_REQUIRE((long)n * t <= (1L << 31) - 1 && d <= kRopeMaxD && (long)a.q.heads + a.k.heads <= kRopeMaxHeads, WMDEC_ERR_UNSUPPORTED,
+                "%s: more than 2^31 - 1 tokens, %d heads or %d channels", who, kRopeMaxHeads, kRopeMaxD);
+  WMDEC_REQUIRE(q_out != k_out && q_out != k && k_out != q, WMDEC_ERR_INVALID_ARG, "%s: an output may be its own input, nothing else may overlap", who);
+  WMDEC_REQUIRE(isfinite(layout->magnitude), WMDEC_ERR_INVALID_ARG, "%s: magnitude must be finite", who);
+  WMDEC_REQUIRE(element_aligned(positions, 4) && element_aligned(freq, 8), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  WMDEC_REQUIRE(positions_stride == 0 || n == 1 || positions_stride >= (long long)t * layout->axes, WMDEC_ERR_SHAPE, "%s: positions_stride %lld below t * axes", who, positions_stride);
+  a.positions = positions; a.positions_stride = n == 1 ? 0 : (long)positions_stride; a.freq = freq; a.layout = *layout;
+  a.n = n; a.t = t; a.d = d;
+  return launch_rope(a, dtype, (hipStream_t)stream);
+}
+
+// ---- attention to states of another length
+size_t wmdec_cross_attention_workspace_bytes(int dtype, int tk, int n, int tq, int heads_q, int heads_kv, int d) {
+  if (!valid_dtype(dtype) || tk < 0 || n <= 0 || tq <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q % heads_kv || d <= 0 || d > kCrossMaxD) return 0;
+  return cross_attention_scratch_bytes(dtype, tk, n, tq, heads_kv, heads_q / heads_kv, d);
+}
+
+static int check_cross_tensor(const char* who, const void* p, const wmdec_strides* s, int n, int tokens, int heads, size_t es) {
+  WMDEC_REQUIRE(s && (p || tokens == 0), WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(strides_in_range(*s, n, tokens, heads), WMDEC_ERR_INVALID_ARG, "%s: a stride is negative or too large", who);
+  WMDEC_REQUIRE(aligned16(p) && s->sample * es % 16 == 0 && s->token * es % 16 == 0 && s->head * es % 16 == 0, WMDEC_ERR_INVALID_ARG,
+                "%s: pointers and strides must be multiples of 16 bytes", who);
+  return WMDEC_OK;
+}
+
+int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const void* k, const wmdec_strides* k_strides, const void* v,
+                          const wmdec_strides* v_strides, void* o, const wmdec_strides* o_strides, int dtype, float scale, const int* key_lens,
+                          const unsigned char* key_mask, int n, int tq, int tk, int heads_q, int heads_kv, int d, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  const char* who = "cross_attention";
+  WMDEC_REQUIRE(valid_dtype(dtype), WMDEC_ERR_INVALID_ARG, "%s: bad dtype", who);
+  WMDEC_REQUIRE(n > 0 && tq > 0 && tk >= 0 && heads_q > 0 && heads_kv > 0 && d > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
+  WMDEC_REQUIRE(heads_q % heads_kv == 0, WMDEC_ERR_SHAPE, "%s: %d query heads are no multiple of %d key heads", who, heads_q, heads_kv);
+  const size_t es = dtype_size(dtype);
+  WMDEC_REQUIRE(d * es % 16 == 0 && d <= kCrossMaxD, WMDEC_ERR_UNSUPPORTED, "%s: d %d must be a multiple of %d and at most %d", who, d, (int)(16 / es), kCrossMaxD);
+  int rc = check_cross_tensor(who, q, q_strides, n, tq, heads_q, es);
+  if (rc == WMDEC_OK) rc = check_cross_tensor(who, k, k_strides, n, tk, heads_kv, es);
+  if (rc == WMDEC_OK) rc = check_cross_tensor(who, v, v_strides, n, tk, heads_kv, es);
+  if (rc == WMDEC_OK) rc = check_cross_tensor(who, o, o_strides, n, tq, heads_q, es);
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(128 * k_strides->token * es < (1L << 31) && 128 * v_strides->token * es < (1L << 31), WMDEC_ERR_UNSUPPORTED, "%s: 128 tokens of k or v span 2 GiB or more", who);
+  WMDEC_REQUIRE(isfinite(scale) && scale > 0.f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  WMDEC_REQUIRE(o != q && o != k && o != v, WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs", who);
+  WMDEC_REQUIRE(element_aligned(key_lens, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  const long rows = (long)tq * (heads_q / heads_kv);
+  WMDEC_REQUIRE(rows <= (1L << 31) - 512 && tk <= (1L << 31) - 512 && (long)n * heads_kv * (rows / 32 + 1) <= (1L << 31) / kCrossMaxSplits, WMDEC_ERR_UNSUPPORTED, "%s: too many rows", who);
+  const size_t need = cross_attention_scratch_bytes(dtype, tk, n, tq, heads_kv, heads_q / heads_kv, d);
+  WMDEC_REQUIRE(need == 0 || (workspace && aligned16(workspace) && workspace_bytes >= need), WMDEC_ERR_WORKSPACE,
+                "%s: workspace needs %zu 16-byte aligned bytes, got %zu", who, need, workspace ? workspace_bytes : (size_t)0);
+  CrossArgs a;
+  a.q = q; a.k = k; a.v = v; a.o = o;
+  a.qs = *q_strides; a.ks = *k_strides; a.vs = *v_strides; a.os = *o_strides;
+  a.lens = key_lens; a.mask = key_mask; a.scale = scale;
+  a.n = n; a.tq = tq; a.tk = tk; a.heads = heads_kv; a.group = heads_q / heads_kv; a.d = d;
+  a.scratch = workspace;
+  return launch_cross_attention(a, dtype, (hipStream_t)stream);
+}
+
 // ---- decoder
 void decoder_default_config(wmdec_decoder_config* cfg) {
   if (!cfg) return;

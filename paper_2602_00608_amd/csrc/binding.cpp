@@ -8,6 +8,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <initializer_list>
+#include <utility>
 
 #include "../../include/wmdec.h"
 
@@ -21,6 +23,9 @@ decltype(&wmdec_gn_silu_conv3x3_stats) g_conv_stats;
 decltype(&wmdec_upsample2x_conv3x3) g_upconv;
 decltype(&wmdec_attention) g_attention;
 decltype(&wmdec_adaln_fused_projection) g_adaln;
+decltype(&wmdec_residual_norm) g_residual_norm;
+decltype(&wmdec_rope) g_rope;
+decltype(&wmdec_cross_attention) g_cross_attention;
 
 constexpr Py_ssize_t kBind = 8;   // arguments of bind(): as many as no other function has
 
@@ -86,6 +91,62 @@ struct Reader {
     void* v = PyLong_AsVoidPtr(args[i]);
     if (!v && PyErr_Occurred()) ok = false;
     return v;
+  }
+};
+// The arguments of the operators whose tensors may be strided: every tensor is on the device that the stream belongs to, and sizes that have to be
+// the same are.  As above, the first fault leaves a Python error.
+struct StridedReader : Reader {
+  int device;
+  StridedReader(const char* who, PyObject* const* a, Py_ssize_t given, Py_ssize_t wanted, int at) : Reader(who, a, given, wanted), device(ok ? integer(at) : 0) {
+    if (ok && !g_cross_attention) { ok = false; PyErr_SetString(PyExc_RuntimeError, "the entry points have not been bound"); }
+  }
+  bool none(int i) const { return args[i] == Py_None; }
+  void fail(PyObject* type, const char* what, int i) { if (ok) { ok = false; PyErr_Format(type, "argument %d: %s", i, what); } }
+  // a tensor of `dims` dimensions on the device, its last dimension contiguous; null for None or a fault
+  const at::Tensor* get(int i, int dims) {
+    if (!ok || none(i)) return nullptr;
+    if (!THPVariable_Check(args[i])) { fail(PyExc_TypeError, "tensor expected", i); return nullptr; }
+    const at::Tensor& t = THPVariable_Unpack(args[i]);
+    if (!t.is_cuda() || t.device().index() != device) { fail(PyExc_AssertionError, "a tensor on the current device is expected", i); return nullptr; }
+    if (t.dim() != dims) { fail(PyExc_ValueError, "wrong number of dimensions", i); return nullptr; }
+    if (dims && t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) { fail(PyExc_ValueError, "the last dimension has to be contiguous", i); return nullptr; }
+    for (int64_t s : t.sizes())
+      if (s > 0x7fffffff) { fail(PyExc_ValueError, "a dimension of 2^31 or more", i); return nullptr; }
+    return &t;
+  }
+  const at::Tensor* need(int i, int dims) {
+    const at::Tensor* t = get(i, dims);
+    if (ok && !t) fail(PyExc_TypeError, "tensor expected", i);
+    return t;
+  }
+  void* address_of(const at::Tensor* t) { return ok && t ? t->data_ptr() : nullptr; }
+  int type_of(const at::Tensor* t, int i) {
+    if (!ok || !t) return WMDEC_F32;
+    switch (t->scalar_type()) {
+      case at::kFloat: return WMDEC_F32;
+      case at::kBFloat16: return WMDEC_BF16;
+      case at::kHalf: return WMDEC_F16;
+      default: fail(PyExc_KeyError, "tensor type is none of float32, bfloat16, float16", i); return WMDEC_F32;
+    }
+  }
+  void same(const at::Tensor* t, const at::Tensor* like, int i) {   // sizes and type
+    if (ok && t && (t->sizes() != like->sizes() || t->scalar_type() != like->scalar_type())) fail(PyExc_ValueError, "sizes or type do not match", i);
+  }
+  void dense(const at::Tensor* t, int i) { if (ok && t && !t->is_contiguous()) fail(PyExc_AssertionError, "contiguous tensor expected", i); }
+  void* typed(int i, std::initializer_list<int64_t> sizes, std::initializer_list<at::ScalarType> types) {   // dense, of these sizes and one of these types; null for None
+    const at::Tensor* t = get(i, (int)sizes.size());
+    dense(t, i);
+    if (!ok || !t) return nullptr;
+    bool fits = t->sizes() == at::IntArrayRef(sizes), known = false;
+    for (at::ScalarType type : types) known = known || t->scalar_type() == type;
+    if (!fits || !known) fail(PyExc_ValueError, "sizes or type do not match", i);
+    return address_of(t);
+  }
+  // strides of a [sample, token, head, channel] tensor; those of dimensions of one element are not used
+  wmdec_strides strides(const at::Tensor* t) {
+    if (!ok || !t) return {0, 0, 0};
+    auto of = [&](int i) -> long long { return t->size(i) > 1 ? t->stride(i) : 0; };
+    return {of(0), of(1), of(2)};
   }
 };
 // Other threads run Python until its end, also where that is an exception: the handler in entry() sets a Python error.
@@ -217,6 +278,107 @@ PyObject* adaln(PyObject*, PyObject* const* a, Py_ssize_t na) {
   WMDEC_RETURN(g_adaln(c, cdt, w, wdt, bias, out, batch, d, rows, silu, stream));
 }
 
+// kind, eps, weight, bias of a norm over d channels, from argument `at` on
+wmdec_norm norm(StridedReader& r, int at, int64_t d) {
+  wmdec_norm v;
+  v.kind = r.integer(at); v.eps = r.real(at + 1);
+  v.weight = (const float*)r.typed(at + 2, {d}, {at::kFloat}); v.bias = (const float*)r.typed(at + 3, {d}, {at::kFloat});
+  return v;
+}
+
+// x, h, <post>, gate, res_scale, x_out, <pre>, scale, shift, y, device, stream
+PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  StridedReader r("residual_norm", a, na, 18, 16);
+  const at::Tensor *x = r.need(0, 3), *h = r.ok ? r.get(1, 3) : nullptr, *x_out = r.ok ? r.get(8, 3) : nullptr, *y = r.ok ? r.get(15, 3) : nullptr;
+  for (auto [t, i] : {std::pair{x, 0}, {h, 1}, {x_out, 8}, {y, 15}}) r.dense(t, i);
+  if (!r.ok) return nullptr;
+  const at::Tensor* act = h ? h : y ? y : x;
+  const int xdt = r.type_of(x, 0), adt = r.type_of(act, 1);
+  r.same(x_out, x, 8);
+  if (h && y) r.same(y, h, 15);
+  if (r.ok && act->sizes() != x->sizes()) r.fail(PyExc_ValueError, "sizes or type do not match", h ? 1 : 15);
+  if (!r.ok) return nullptr;
+  const int64_t n = x->size(0), d = x->size(2);
+  const wmdec_norm post = norm(r, 2, d), pre = norm(r, 9, d);
+  long long stride = -1;
+  const float* mod[3];
+  const int at_mod[3] = {6, 13, 14};
+  for (int i = 0; i < 3; ++i) {
+    const at::Tensor* m = r.get(at_mod[i], 2);
+    mod[i] = (const float*)r.address_of(m);
+    if (!r.ok || !m) continue;
+    const long long s = n > 1 ? m->stride(0) : 0;
+    if (m->size(0) != n || m->size(1) != d || m->scalar_type() != at::kFloat) r.fail(PyExc_ValueError, "sizes or type do not match", at_mod[i]);
+    else if (stride >= 0 && s != stride) r.fail(PyExc_ValueError, "gate, scale and shift have the same stride", at_mod[i]);
+    stride = s;
+  }
+  const float res_scale = r.real(7);
+  void *px = r.address_of(x), *ph = r.address_of(h), *pxo = r.address_of(x_out), *py = r.address_of(y);
+  void* stream = r.address(17);
+  WMDEC_RETURN(g_residual_norm(px, xdt, ph, adt, &post, mod[0], res_scale, pxo, &pre, mod[1], mod[2], stride < 0 ? 0 : stride, py, (int)n, (int)x->size(1), (int)d, stream));
+}
+
+// q, k, positions, freq, axes, dim0, dim1, dim2, q_out, k_out, interleaved, inverse, magnitude, device, stream
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  StridedReader r("rope", a, na, 15, 13);
+  const at::Tensor *q = r.need(0, 4), *q_out = r.ok ? r.need(8, 4) : nullptr, *k = r.ok ? r.get(1, 4) : nullptr, *k_out = r.ok && k ? r.need(9, 4) : nullptr;
+  if (!r.ok) return nullptr;
+  if (!k && !r.none(9)) r.fail(PyExc_ValueError, "k_out without k", 9);
+  const int dt = r.type_of(q, 0);
+  r.same(q_out, q, 8);
+  if (k) r.same(k_out, k, 9);
+  const int64_t n = q->size(0), t = q->size(1), d = q->size(3);
+  if (r.ok && k && (k->size(0) != n || k->size(1) != t || k->size(3) != d || k->scalar_type() != q->scalar_type())) r.fail(PyExc_ValueError, "sizes or type do not match", 1);
+  wmdec_rope_layout lay;
+  lay.axes = r.integer(4);
+  for (int i = 0; i < 3; ++i) lay.axis_dim[i] = r.integer(5 + i);
+  lay.interleaved = r.flag(10); lay.inverse = r.flag(11); lay.magnitude = r.real(12);
+  if (!r.ok) return nullptr;
+  if (r.none(2) || r.none(3)) { r.fail(PyExc_TypeError, "tensor expected", r.none(2) ? 2 : 3); return nullptr; }
+  const bool shared = THPVariable_Check(a[2]) && THPVariable_Unpack(a[2]).dim() == 2;
+  const int* pos = (const int*)(shared ? r.typed(2, {t, lay.axes}, {at::kInt}) : r.typed(2, {n, t, lay.axes}, {at::kInt}));
+  int64_t pairs = 0;
+  for (int i = 0; i < lay.axes && i < 3; ++i) pairs += lay.axis_dim[i] / 2;
+  const double* freq = (const double*)r.typed(3, {pairs}, {at::kDouble});
+  const wmdec_strides qs = r.strides(q), qos = r.strides(q_out), ks = r.strides(k), kos = r.strides(k_out);
+  void *pq = r.address_of(q), *pqo = r.address_of(q_out), *pk = r.address_of(k), *pko = r.address_of(k_out);
+  void* stream = r.address(14);
+  WMDEC_RETURN(g_rope(pq, &qs, pqo, &qos, (int)q->size(2), pk, &ks, pko, &kos, k ? (int)k->size(2) : 0, dt, pos, shared ? 0 : t * lay.axes, freq, &lay, (int)n, (int)t, (int)d, stream));
+}
+
+// q, k, v, o, scale, key_lens, key_mask, workspace, device, stream
+PyObject* cross_attention(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  StridedReader r("cross_attention", a, na, 10, 8);
+  const at::Tensor *q = r.need(0, 4), *k = r.ok ? r.need(1, 4) : nullptr, *v = r.ok ? r.need(2, 4) : nullptr, *o = r.ok ? r.need(3, 4) : nullptr;
+  if (!r.ok) return nullptr;
+  const int dt = r.type_of(q, 0);
+  r.same(v, k, 2);
+  r.same(o, q, 3);
+  const int64_t n = q->size(0), tk = k->size(1);
+  if (r.ok && (k->size(0) != n || k->size(3) != q->size(3) || k->scalar_type() != q->scalar_type())) r.fail(PyExc_ValueError, "sizes or type do not match", 1);
+  const float scale = r.real(4);
+  const int* lens = (const int*)r.typed(5, {n}, {at::kInt});
+  const unsigned char* mask = (const unsigned char*)r.typed(6, {n, tk}, {at::kBool, at::kByte});
+  const at::Tensor* ws = r.get(7, 1);
+  r.dense(ws, 7);
+  const wmdec_strides qs = r.strides(q), ks = r.strides(k), vs = r.strides(v), os = r.strides(o);
+  void *pq = r.address_of(q), *pk = r.address_of(k), *pv = r.address_of(v), *po = r.address_of(o), *pw = r.address_of(ws);
+  const size_t bytes = ws ? (size_t)ws->nbytes() : 0;
+  void* stream = r.address(9);
+  WMDEC_RETURN(g_cross_attention(pq, &qs, pk, &ks, pv, &vs, po, &os, dt, scale, lens, mask, (int)n, (int)q->size(1), (int)tk, (int)q->size(2), (int)k->size(2), (int)q->size(3), pw,
+                                 bytes, stream));
+}
+
+// the addresses of these three, in the order of wmdec.py
+PyObject* bind_block(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  Reader r("bind_block", a, na, 3);
+  void* f[3];
+  for (int i = 0; i < 3; ++i) f[i] = r.address(i);
+  if (!r.ok) return nullptr;
+  g_residual_norm = (decltype(g_residual_norm))f[0]; g_rope = (decltype(g_rope))f[1]; g_cross_attention = (decltype(g_cross_attention))f[2];
+  Py_RETURN_NONE;
+}
+
 // the addresses of the entry points, in the order of wmdec.py
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t na) {
   Reader r("bind", a, na, kBind);
@@ -239,7 +401,8 @@ template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyObject* ent
 }
 #define WMDEC_METHOD(name_) {#name_, (PyCFunction)(void (*)())entry<name_>, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {WMDEC_METHOD(gn_stats), WMDEC_METHOD(conv), WMDEC_METHOD(conv_shortcut), WMDEC_METHOD(conv_stats), WMDEC_METHOD(upconv),
-                           WMDEC_METHOD(attention), WMDEC_METHOD(adaln), WMDEC_METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                           WMDEC_METHOD(attention), WMDEC_METHOD(adaln), WMDEC_METHOD(residual_norm), WMDEC_METHOD(rope), WMDEC_METHOD(cross_attention),
+                           WMDEC_METHOD(bind), WMDEC_METHOD(bind_block), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -196,6 +196,45 @@ int adaln_max_d_cond(int w_dtype);  // longest conditioning vector (a lane keeps
 int launch_adaln_projection(const void* c, int c_dtype, const void* w, int w_dtype, const float* bias, float* out, int batch,
                             int d_cond, int rows, int apply_silu, hipStream_t s);
 
+// kernels_residual_norm.hip: x' = x + res_scale * gate * P(h), y = N(x') * (1 + scale) + shift over rows of d channels
+struct ResidualNormArgs {
+  const void* x = nullptr; const void* h = nullptr;
+  void* x_out = nullptr; void* y = nullptr;
+  const float* gate = nullptr; const float* scale = nullptr; const float* shift = nullptr;
+  wmdec_norm post{WMDEC_NORM_NONE, 0.f, nullptr, nullptr}, pre{WMDEC_NORM_NONE, 0.f, nullptr, nullptr};
+  float res_scale = 1.f;
+  long mod_stride = 0;
+  int n = 0, t = 0, d = 0;
+};
+constexpr int kResidualNormMaxD = 16384;
+int launch_residual_norm(const ResidualNormArgs& a, int x_dtype, int act_dtype, hipStream_t s);
+
+// kernels_rope.hip
+struct RopeTensor { const void* in = nullptr; void* out = nullptr; wmdec_strides si{0, 0, 0}, so{0, 0, 0}; int heads = 0; };
+struct RopeArgs {
+  RopeTensor q, k;
+  const int* positions = nullptr; long positions_stride = 0;
+  const double* freq = nullptr;
+  wmdec_rope_layout layout{1, {0, 0, 0}, 0, 0, 1.f};
+  int n = 0, t = 0, d = 0, rot = 0;   // rot: channels of a head that are rotated
+};
+constexpr int kRopeMaxRot = 4096, kRopeMaxD = 16384, kRopeMaxHeads = 16384;
+int launch_rope_frequencies(double* freq, int axes, const int* axis_dim, const wmdec_rope_scaling& sc, hipStream_t s);
+int launch_rope(const RopeArgs& a, int dtype, hipStream_t s);
+
+// kernels_cross.hip: attention of the rows of a query head group (tq tokens x group heads) to tk keys
+struct CrossArgs {
+  const void* q = nullptr; const void* k = nullptr; const void* v = nullptr; void* o = nullptr;
+  wmdec_strides qs{0, 0, 0}, ks{0, 0, 0}, vs{0, 0, 0}, os{0, 0, 0};
+  const int* lens = nullptr; const unsigned char* mask = nullptr;
+  float scale = 1.f;
+  int n = 0, tq = 0, tk = 0, heads = 0, group = 1, d = 0;   // heads: of keys and values
+  void* scratch = nullptr;
+};
+constexpr int kCrossMaxD = 256, kCrossMaxSplits = 64;   // splits: ranges of keys of one row
+size_t cross_attention_scratch_bytes(int dtype, int tk, int n, int tq, int heads, int group, int d);
+int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s);
+
 // kernels_attn.hip: attention over the t tokens of a sample, head dimension 512 (q, k, v in the fragment order described there)
 size_t attention_fragment_bytes(int n, int t);
 size_t flash_attention_scratch_bytes(int n, int t);   // partial outputs of the key ranges (none where one range holds all keys)

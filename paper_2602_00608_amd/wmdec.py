@@ -4,6 +4,7 @@ ctypes, and for the operators that a layer is made of a native module
 (csrc/binding.cpp), whose calls cost a tenth.
 Every computation happens in the library's HIP kernels; there is no fallback:
 if the shared library or the native module is missing, loading raises."""
+import collections
 import ctypes
 import os
 
@@ -37,6 +38,26 @@ class DecoderConfig(ctypes.Structure):
 
 _vp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
 
+
+class _CNorm(ctypes.Structure):
+    _fields_ = [("kind", _i), ("eps", _f), ("weight", _vp), ("bias", _vp)]
+
+
+class _CRopeScaling(ctypes.Structure):
+    _fields_ = [("kind", _i), ("base", ctypes.c_double), ("factor", ctypes.c_double), ("trained_length", ctypes.c_double),
+                ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double)]
+
+
+class _CRopeLayout(ctypes.Structure):
+    _fields_ = [("axes", _i), ("axis_dim", _i * 3), ("interleaved", _i), ("inverse", _i), ("magnitude", _f)]
+
+
+class _CStrides(ctypes.Structure):
+    _fields_ = [("sample", ctypes.c_longlong), ("token", ctypes.c_longlong), ("head", ctypes.c_longlong)]
+
+
+_nm, _st = ctypes.POINTER(_CNorm), ctypes.POINTER(_CStrides)
+
 # name -> (restype, argtypes): every symbol include/wmdec.h and include/wmdec_measure.h declare
 SIGNATURES = {
     "wmdec_last_error": (ctypes.c_char_p, []),
@@ -63,6 +84,11 @@ SIGNATURES = {
     "wmdec_attention": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _sz, _vp]),
     "wmdec_adaln_max_batch": (_i, [_i]),
     "wmdec_adaln_fused_projection": (_i, [_vp, _i, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp]),
+    "wmdec_residual_norm": (_i, [_vp, _i, _vp, _i, _nm, _vp, _f, _vp, _nm, _vp, _vp, ctypes.c_longlong, _vp, _i, _i, _i, _vp]),
+    "wmdec_rope_frequencies": (_i, [_vp, _i, ctypes.POINTER(_i), ctypes.POINTER(_CRopeScaling), _vp]),
+    "wmdec_rope": (_i, [_vp, _st, _vp, _st, _i, _vp, _st, _vp, _st, _i, _i, _vp, ctypes.c_longlong, _vp, ctypes.POINTER(_CRopeLayout), _i, _i, _i, _vp]),
+    "wmdec_cross_attention_workspace_bytes": (_sz, [_i] * 7),
+    "wmdec_cross_attention": (_i, [_vp, _st, _vp, _st, _vp, _st, _vp, _st, _i, _f, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
     "decoder_default_config": (None, [ctypes.POINTER(DecoderConfig)]),
     "decoder_create": (_i, [ctypes.POINTER(DecoderConfig), ctypes.POINTER(_vp)]),
     "decoder_destroy": (_i, [_vp]),
@@ -96,6 +122,7 @@ _native = None   # the native module, bound to the loaded library
 # entry points that the native module calls, in the order of its bind()
 _BOUND = ("wmdec_gn_stats", "wmdec_gn_silu_conv3x3", "wmdec_gn_conv1x1", "wmdec_gn_silu_conv3x3_shortcut",
           "wmdec_gn_silu_conv3x3_stats", "wmdec_upsample2x_conv3x3", "wmdec_attention", "wmdec_adaln_fused_projection")
+_BOUND_BLOCK = ("wmdec_residual_norm", "wmdec_rope", "wmdec_cross_attention")   # ... and of its bind_block()
 
 
 def lib():
@@ -116,6 +143,7 @@ def lib():
             raise RuntimeError("the native binding is missing (%s): build it with "
                                "`python -m paper_2602_00608_amd.build`; there is no fallback path" % e) from e
         _binding.bind(*(ctypes.cast(getattr(l, name), _vp).value for name in _BOUND))
+        _binding.bind_block(*(ctypes.cast(getattr(l, name), _vp).value for name in _BOUND_BLOCK))
         _native = _binding   # (before _lib: another thread takes a set _lib for both)
         _lib = l
     return _lib
@@ -265,6 +293,65 @@ def adaln_max_batch(d_cond):
 def adaln_fused_projection(c, w_fused, bias, out, apply_silu=True):
     """out[b, :] = bias + w_fused @ act(c[b]); c [batch, d_cond], w_fused [rows, d_cond], out fp32 [batch, rows]."""
     _check(_ops().adaln(c, w_fused, bias, out, apply_silu, _stream()))
+
+
+# ------------------------------------------------------------------ around the AdaLN projections of a transformer block
+def _device():
+    return torch.cuda.current_device() if _current_device is None else _current_device()
+
+
+class Norm(collections.namedtuple("Norm", "kind eps weight bias", defaults=(0.0, None, None))):
+    """A norm over the channels of a row: kind "none", "layer" or "rms", eps, fp32 weight and bias [d] or None."""
+
+
+_NORM_KINDS = {"none": 0, "layer": 1, "rms": 2}
+_NO_NORM = (0, 0.0, None, None)
+
+
+def _norm(spec):
+    return _NO_NORM if spec is None else (_NORM_KINDS[spec[0]],) + tuple(spec[1:])
+
+
+def residual_norm(x, h, post, gate, res_scale, x_out, pre, scale, shift, y):
+    """x_out = x + res_scale * gate * post(h);  y = pre(x_out) * (1 + scale) + shift.
+    x, x_out [n,t,d]; h, y [n,t,d] of x's type, or 16-bit beside an fp32 x; gate, scale, shift fp32 [n,d] with one row stride (the
+    thirds of adaln_fused_projection's output: shift, scale, gate) or None; post, pre: a Norm or None.  h None: y = pre(x) * ...;
+    y None: x_out alone.  x_out may be x, y may be h."""
+    _check(_ops().residual_norm(x, h, *_norm(post), gate, res_scale, x_out, *_norm(pre), scale, shift, y, _device(), _stream()))
+
+
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+def rope_frequencies(axis_dims, freq, base=10000.0, scaling="none", factor=1.0, trained_length=1.0, low_turns=1.0, high_turns=4.0):
+    """freq: float64 tensor [sum(axis_dims) / 2], the angle per unit of position of every pair (see wmdec.h for the scalings)."""
+    dims = [int(v) for v in axis_dims]
+    if freq.dtype != torch.float64 or tuple(freq.shape) != (sum(dims) // 2,):
+        raise ValueError("freq: float64 [%d] expected" % (sum(dims) // 2))
+    if not freq.is_cuda or freq.device.index != _device():
+        raise AssertionError("a tensor on the current device is expected")
+    sc = _CRopeScaling(_ROPE_SCALINGS[scaling], base, factor, trained_length, low_turns, high_turns)
+    _check(lib().wmdec_rope_frequencies(_ptr(freq), len(dims), (_i * max(len(dims), 1))(*dims), ctypes.byref(sc), _stream()))
+
+
+def rope(q, k, positions, freq, axis_dims, q_out, k_out, interleaved=False, inverse=False, magnitude=1.0):
+    """Rotary positions of q [n,t,heads_q,d] and k [n,t,heads_k,d] (or None); positions int32 [n,t,axes], or [t,axes] for all samples;
+    freq from rope_frequencies(axis_dims, ...).  Strides are free but for the channels'; outputs may be the inputs."""
+    dims = tuple(axis_dims)
+    if not 1 <= len(dims) <= 3:
+        raise ValueError("one to three axes expected")
+    _check(_ops().rope(q, k, positions, freq, len(dims), *(dims + (0, 0))[:3], q_out, k_out, interleaved, inverse, magnitude, _device(), _stream()))
+
+
+def cross_attention_workspace_bytes(q, k):
+    n, tq, hq, d = q.shape
+    return lib().wmdec_cross_attention_workspace_bytes(dtype_enum(q), k.shape[1], n, tq, hq, k.shape[2], d)
+
+
+def cross_attention(q, k, v, o, scale, key_lens=None, key_mask=None, workspace=None):
+    """o = softmax(scale * q k^T) v over the keys below key_lens[n] (int32 [n]) whose key_mask [n,tk] (bool or uint8) is set.
+    q, o [n,tq,heads_q,d]; k, v [n,tk,heads_kv,d]; strides are free but for the channels'."""
+    _check(_ops().cross_attention(q, k, v, o, scale, key_lens, key_mask, workspace, _device(), _stream()))
 
 
 # ------------------------------------------------------------------ decoder
