@@ -1,71 +1,274 @@
 // Gated residual with the norms on both of its sides: x' = x + s * g * P(h), y = N(x') * (1 + c) + b, rows of d channels.
-#include "common.hpp"
+//
+// Bound by HBM: x and h are read once, x' and y written once, some twenty operations an element.  The vectors of a sample (gate, shift, scale, the
+// norms' weights and biases: up to seven times four bytes a channel, more than a row of 16-bit tensors has) would be read again for every row, so a
+// thread owns eight channels of many rows and keeps what they come to in registers, two multiply-adds an element:
+//   x' = x + ((h - mean) * rstd) * ga + gb,   ga = s * g * w, gb = s * g * u;     y = ((x' - mean) * rstd) * ya + yb,   ya = w (1 + c), yb = u (1 + c) + b.
+// A row is 8 to 64 lanes of a wavefront (up to 512 channels), or whole wavefronts of a workgroup; the next rows are requested before the present ones
+// are reduced.  Moments: mean and squares about it over the values of a wavefront, joined over the wavefronts (Chan, Golub, LeVeque) behind one barrier a norm.
+#include "conv_device.hpp"
 
 namespace wmdec {
 namespace {
 
-constexpr int NT = 256;
-
-__device__ __forceinline__ float block_sum(float v, float* s_red) {
-  for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return s_red[0] + s_red[1] + s_red[2] + s_red[3];
-}
+constexpr int kMaxThreads = 512;   // of a workgroup: 4096 channels at a vector a thread
+constexpr int E = 8;               // channels of a vector
 
 struct Params {
   ResidualNormArgs a;
+  int tpr, segs;   // threads of a row, ranges of rows of a sample
 };
 
-// A workgroup takes a row, its values in LDS.
-template <typename TX, typename TA>
-__global__ __launch_bounds__(NT) void residual_norm_kernel(Params p) {
-  __shared__ float s_v[kResidualNormMaxD];
-  __shared__ float s_red[4];
-  const ResidualNormArgs& a = p.a;
-  const int d = a.d, n = blockIdx.x / a.t;
-  const size_t row = (size_t)blockIdx.x * d, mod = (size_t)n * a.mod_stride;
-  auto statistics = [&](const wmdec_norm& norm, float& mean, float& rstd) {
-    mean = 0.f; rstd = 1.f;
-    if (norm.kind == WMDEC_NORM_NONE) return;
-    float sum = 0.f;
-    if (norm.kind == WMDEC_NORM_LAYER) {
-      for (int c = threadIdx.x; c < d; c += NT) sum += s_v[c];
-      mean = block_sum(sum, s_red) / d;
+template <typename T, bool VEC> __device__ __forceinline__ void load8(const T* p, int count, T (&v)[E]) {
+  if constexpr (VEC) {
+    u32x4 q[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = u32x4{0, 0, 0, 0};
+    if (count > 0) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = reinterpret_cast<const u32x4*>(p)[i];
     }
-    sum = 0.f;
-    for (int c = threadIdx.x; c < d; c += NT) sum += (s_v[c] - mean) * (s_v[c] - mean);
-    rstd = 1.f / sqrtf(block_sum(sum, s_red) / d + norm.eps);
-  };
-  auto normalise = [&](const wmdec_norm& norm, float mean, float rstd, int c) {
-    if (norm.kind == WMDEC_NORM_NONE) return s_v[c];
-    return (s_v[c] - mean) * rstd * (norm.weight ? norm.weight[c] : 1.f) + (norm.bias ? norm.bias[c] : 0.f);
-  };
-  float mean, rstd;
-  if (a.h) {
-    for (int c = threadIdx.x; c < d; c += NT) s_v[c] = to_float(((const TA*)a.h)[row + c]);
-    statistics(a.post, mean, rstd);
-    for (int c = threadIdx.x; c < d; c += NT) {
-      const float v = to_float(((const TX*)a.x)[row + c]) + a.res_scale * (a.gate ? a.gate[mod + c] : 1.f) * normalise(a.post, mean, rstd, c);
-      const TX stored = from_float<TX>(v);
-      ((TX*)a.x_out)[row + c] = stored;
-      s_v[c] = to_float(stored);
+    __builtin_memcpy(&v, &q, sizeof(v));
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = e < count ? p[e] : T{};
+  }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int count, const float (&v)[E]) {
+  T t[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) t[e] = from_float<T>(v[e]);
+  if constexpr (VEC) {
+    u32x4 q[sizeof(T) / 2];
+    __builtin_memcpy(&q, &t, sizeof(t));
+    if (count > 0) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<u32x4*>(p)[i] = q[i];
     }
   } else {
-    for (int c = threadIdx.x; c < d; c += NT) s_v[c] = to_float(((const TX*)a.x)[row + c]);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e < count) p[e] = t[e];
   }
-  if (!a.y) return;
-  statistics(a.pre, mean, rstd);
-  for (int c = threadIdx.x; c < d; c += NT)
-    ((TA*)a.y)[row + c] = from_float<TA>(normalise(a.pre, mean, rstd, c) * (1.f + (a.scale ? a.scale[mod + c] : 0.f)) + (a.shift ? a.shift[mod + c] : 0.f));
+}
+// eight of a vector that may be missing
+template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long at, int count, float missing, float (&v)[E]) {
+  if (p) load8<float, VEC>(p + at, count, v);
+  else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = missing;
+  }
+}
+
+// VPT vectors a thread, R rows at once
+template <typename TX, typename TA, int VPT, int R, bool VEC>
+__global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
+  __shared__ float4 s_red[2][2][R][kMaxThreads / 64];
+  const ResidualNormArgs& a = p.a;
+  const int d = a.d, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int groups = p.tpr < 64 ? (int)blockDim.x / p.tpr : 1, group = p.tpr < 64 ? tid / p.tpr : 0, lane = p.tpr < 64 ? tid % p.tpr : tid;
+  const int n = blockIdx.x / p.segs, seg = blockIdx.x % p.segs;
+  const int row0 = (int)((long)a.t * seg / p.segs), row1 = (int)((long)a.t * (seg + 1) / p.segs);
+  const bool has_h = a.h != nullptr, has_y = a.y != nullptr;
+  int col[VPT], count[VPT];
+  float held = 0.f;                       // values of this wavefront in a row
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    col[i] = (i * p.tpr + lane) * E;
+    count[i] = min(max(d - col[i], 0), E);
+    held += (float)min(max(d - (i * p.tpr + wave * 64) * E, 0), 64 * E);
+  }
+  const TX* x = (const TX*)a.x + (long)n * a.t * d;
+  const TA* h = (const TA*)a.h + (has_h ? (long)n * a.t * d : 0);
+  TX* x_out = (TX*)a.x_out + (has_h ? (long)n * a.t * d : 0);
+  TA* y = (TA*)a.y + (has_y ? (long)n * a.t * d : 0);
+
+  TX rx[R][VPT][E];
+  TA rh[R][VPT][E];
+  auto ask = [&](int first) {             // rows past the range: the last one again, not stored
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const long at = (long)min(first + r * groups + group, row1 - 1) * d;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        load8<TX, VEC>(x + at + col[i], count[i], rx[r][i]);
+        if (has_h) load8<TA, VEC>(h + at + col[i], count[i], rh[r][i]);
+      }
+    }
+  };
+  constexpr bool AHEAD = VPT < 4;         // (four vectors a thread leave no registers for the next rows)
+  if (AHEAD && row0 < row1) ask(row0);
+  __builtin_amdgcn_sched_barrier(0);
+
+  float ga[VPT][E], gb[VPT][E], ya[VPT][E], yb[VPT][E];
+  const long mod = (long)n * a.mod_stride;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    float w[E], u[E], m[E];
+    if (has_h) {
+      vector8<VEC>(a.gate, mod + col[i], count[i], 1.f, m);
+      vector8<VEC>(a.post.weight, col[i], count[i], 1.f, w);
+      vector8<VEC>(a.post.bias, col[i], count[i], 0.f, u);
+#pragma unroll
+      for (int e = 0; e < E; ++e) { ga[i][e] = a.res_scale * m[e] * w[e]; gb[i][e] = a.res_scale * m[e] * u[e]; }
+    }
+    if (has_y) {
+      vector8<VEC>(a.scale, mod + col[i], count[i], 0.f, m);
+      vector8<VEC>(a.pre.weight, col[i], count[i], 1.f, w);
+      vector8<VEC>(a.pre.bias, col[i], count[i], 0.f, u);
+#pragma unroll
+      for (int e = 0; e < E; ++e) { ya[i][e] = w[e] * (1.f + m[e]); yb[i][e] = u[e] * (1.f + m[e]); }
+      vector8<VEC>(a.shift, mod + col[i], count[i], 0.f, m);
+#pragma unroll
+      for (int e = 0; e < E; ++e) yb[i][e] += m[e];
+    }
+  }
+
+  const float inv_d = 1.f / (float)d;
+  auto row_sum = [&](float v) {           // over the lanes of a row, or of a wavefront of it
+    v = lane_group_sum<8>(v);
+    if (p.tpr > 8) v += mirror16(v);
+    if (p.tpr > 16) v = swap_sum<16>(v);
+    if (p.tpr > 32) v = swap_sum<32>(v);
+    return v;
+  };
+  // mean and 1 / sqrt(variance + eps) of the R rows; RMS: the mean is zero
+  auto statistics = [&](const wmdec_norm& norm, const float (&v)[R][VPT][E], int which, int parity, float (&mean)[R], float (&rstd)[R]) {
+    const bool layer = norm.kind == WMDEC_NORM_LAYER;
+    const float inv = p.tpr > 64 ? __builtin_amdgcn_rcpf(fmaxf(held, 1.f)) : inv_d;
+    float m2[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mean[r] = 0.f;
+      if (layer) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum += v[r][i][e];
+        mean[r] = row_sum(sum) * inv;
+      }
+      float sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float dev = e < count[i] ? v[r][i][e] - mean[r] : 0.f;
+          sq = fmaf(dev, dev, sq);
+        }
+      m2[r] = row_sum(sq);
+    }
+    if (p.tpr > 64) {
+      if ((tid & 63) == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) s_red[parity][which][r][wave] = make_float4(mean[r], m2[r], held, 0.f);
+      }
+      __syncthreads();
+      const int waves = blockDim.x >> 6;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float sum = 0.f, sq = 0.f;
+        for (int w = 0; w < waves; ++w) { const float4 q = s_red[parity][which][r][w]; sum = fmaf(q.x, q.z, sum); }
+        mean[r] = sum * inv_d;
+        for (int w = 0; w < waves; ++w) { const float4 q = s_red[parity][which][r][w]; sq += fmaf(q.z * (q.x - mean[r]), q.x - mean[r], q.y); }
+        m2[r] = sq;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd[r] = __builtin_amdgcn_rsqf(fmaf(m2[r], inv_d, norm.eps));
+  };
+
+  int parity = 0;
+  for (int first = row0; first < row1; first += R * groups, parity ^= 1) {
+    if (!AHEAD) ask(first);
+    float v[R][VPT][E], b[R][VPT][E];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          v[r][i][e] = to_float(rx[r][i][e]);
+          if (has_h) b[r][i][e] = to_float(rh[r][i][e]);
+        }
+    if (AHEAD && first + R * groups < row1) ask(first + R * groups);
+    __builtin_amdgcn_sched_barrier(0);
+    float mean[R], rstd[R];
+    if (has_h) {
+      if (a.post.kind != WMDEC_NORM_NONE) {
+        statistics(a.post, b, 0, parity, mean, rstd);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) b[r][i][e] = (b[r][i][e] - mean[r]) * rstd[r];
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int row = first + r * groups + group;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[r][i][e] = round_through<TX>(v[r][i][e] + fmaf(b[r][i][e], ga[i][e], gb[i][e]));   // (what is stored is what is normalised)
+          if (row < row1) store8<TX, VEC>(x_out + (long)row * d + col[i], count[i], v[r][i]);
+        }
+      }
+    }
+    if (!has_y) continue;
+    if (a.pre.kind != WMDEC_NORM_NONE) {
+      statistics(a.pre, v, 1, parity, mean, rstd);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[r][i][e] = (v[r][i][e] - mean[r]) * rstd[r];
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int row = first + r * groups + group;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[r][i][e] = fmaf(v[r][i][e], ya[i][e], yb[i][e]);
+        if (row < row1) store8<TA, VEC>(y + (long)row * d + col[i], count[i], v[r][i]);
+      }
+    }
+  }
+}
+
+template <typename TX, typename TA, int VPT, int R, bool VEC>
+int launch_form(const ResidualNormArgs& a, int tpr, int threads, hipStream_t s) {
+  Params p{a, tpr, 1};
+  const int groups = tpr < 64 ? threads / tpr : 1;
+  const int most = (a.t + groups * R - 1) / (groups * R), target = 4096 / (threads / 64) / a.n;   // workgroups: 16 wavefronts a compute unit
+  p.segs = max(1, min(most, target));
+  hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, R, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);
+  WMDEC_HIP(hipGetLastError());
+  return WMDEC_OK;
+}
+
+template <typename TX, typename TA, bool VEC>
+int launch_width(const ResidualNormArgs& a, hipStream_t s) {
+  const int vectors = (a.d + E - 1) / E;
+  int tpr = 8;
+  while (tpr < 64 && tpr < vectors) tpr *= 2;
+  if (vectors <= 64) return launch_form<TX, TA, 1, 2, VEC>(a, tpr, 256, s);
+  if (vectors <= kMaxThreads) return launch_form<TX, TA, 1, 2, VEC>(a, (vectors + 63) / 64 * 64, (vectors + 63) / 64 * 64, s);
+  tpr = ((vectors + 1) / 2 + 63) / 64 * 64;
+  if (tpr <= kMaxThreads) return launch_form<TX, TA, 2, 1, VEC>(a, tpr, tpr, s);
+  tpr = ((vectors + 3) / 4 + 63) / 64 * 64;
+  static_assert(4 * kMaxThreads * E == kResidualNormMaxD, "four vectors a thread hold the widest row");
+  return launch_form<TX, TA, 4, 1, VEC>(a, tpr, tpr, s);
 }
 
 template <typename TX, typename TA>
 int launch(const ResidualNormArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((residual_norm_kernel<TX, TA>), dim3((unsigned)(a.n * a.t)), dim3(NT), 0, s, Params{a});
-  WMDEC_HIP(hipGetLastError());
-  return WMDEC_OK;
+  auto aligned = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
+  const bool vec = a.d % E == 0 && a.mod_stride % 4 == 0 && aligned(a.x) && aligned(a.h) && aligned(a.x_out) && aligned(a.y) && aligned(a.gate) && aligned(a.scale) &&
+                   aligned(a.shift) && aligned(a.post.weight) && aligned(a.post.bias) && aligned(a.pre.weight) && aligned(a.pre.bias);
+  return vec ? launch_width<TX, TA, true>(a, s) : launch_width<TX, TA, false>(a, s);
 }
 
 }  // namespace
