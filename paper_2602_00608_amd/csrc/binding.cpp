@@ -278,31 +278,41 @@ PyObject* adaln(PyObject*, PyObject* const* a, Py_ssize_t na) {
   WMDEC_RETURN(g_adaln(c, cdt, w, wdt, bias, out, batch, d, rows, silu, stream));
 }
 
-// kind, eps, weight, bias of a norm over d channels, from argument `at` on
+// (kind, eps, weight, bias) of a norm over d channels; None is the norm that does nothing
 wmdec_norm norm(StridedReader& r, int at, int64_t d) {
-  wmdec_norm v;
-  v.kind = r.integer(at); v.eps = r.real(at + 1);
-  v.weight = (const float*)r.typed(at + 2, {d}, {at::kFloat}); v.bias = (const float*)r.typed(at + 3, {d}, {at::kFloat});
+  wmdec_norm v{WMDEC_NORM_NONE, 0.f, nullptr, nullptr};
+  if (!r.ok || r.none(at)) return v;
+  PyObject* spec = r.args[at];
+  if (!PyTuple_Check(spec) || PyTuple_GET_SIZE(spec) != 4 || !PyUnicode_Check(PyTuple_GET_ITEM(spec, 0))) { r.fail(PyExc_TypeError, "a Norm or None is expected", at); return v; }
+  PyObject* kind = PyTuple_GET_ITEM(spec, 0);
+  if (PyUnicode_CompareWithASCIIString(kind, "layer") == 0) v.kind = WMDEC_NORM_LAYER;
+  else if (PyUnicode_CompareWithASCIIString(kind, "rms") == 0) v.kind = WMDEC_NORM_RMS;
+  else if (PyUnicode_CompareWithASCIIString(kind, "none") != 0) { r.fail(PyExc_KeyError, "the kind of a norm is none of none, layer, rms", at); return v; }
+  PyObject* const* outer = r.args;
+  r.args = &PyTuple_GET_ITEM(spec, 0);
+  v.eps = r.real(1);
+  v.weight = (const float*)r.typed(2, {d}, {at::kFloat}); v.bias = (const float*)r.typed(3, {d}, {at::kFloat});
+  r.args = outer;
   return v;
 }
 
-// x, h, <post>, gate, res_scale, x_out, <pre>, scale, shift, y, device, stream
+// x, h, post, gate, res_scale, x_out, pre, scale, shift, y, device, stream
 PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t na) {
-  StridedReader r("residual_norm", a, na, 18, 16);
-  const at::Tensor *x = r.need(0, 3), *h = r.ok ? r.get(1, 3) : nullptr, *x_out = r.ok ? r.get(8, 3) : nullptr, *y = r.ok ? r.get(15, 3) : nullptr;
-  for (auto [t, i] : {std::pair{x, 0}, {h, 1}, {x_out, 8}, {y, 15}}) r.dense(t, i);
+  StridedReader r("residual_norm", a, na, 12, 10);
+  const at::Tensor *x = r.need(0, 3), *h = r.ok ? r.get(1, 3) : nullptr, *x_out = r.ok ? r.get(5, 3) : nullptr, *y = r.ok ? r.get(9, 3) : nullptr;
+  for (auto [t, i] : {std::pair{x, 0}, {h, 1}, {x_out, 5}, {y, 9}}) r.dense(t, i);
   if (!r.ok) return nullptr;
   const at::Tensor* act = h ? h : y ? y : x;
   const int xdt = r.type_of(x, 0), adt = r.type_of(act, 1);
-  r.same(x_out, x, 8);
-  if (h && y) r.same(y, h, 15);
-  if (r.ok && act->sizes() != x->sizes()) r.fail(PyExc_ValueError, "sizes or type do not match", h ? 1 : 15);
+  r.same(x_out, x, 5);
+  if (h && y) r.same(y, h, 9);
+  if (r.ok && act->sizes() != x->sizes()) r.fail(PyExc_ValueError, "sizes or type do not match", h ? 1 : 9);
   if (!r.ok) return nullptr;
   const int64_t n = x->size(0), d = x->size(2);
-  const wmdec_norm post = norm(r, 2, d), pre = norm(r, 9, d);
+  const wmdec_norm post = norm(r, 2, d), pre = norm(r, 6, d);
   long long stride = -1;
   const float* mod[3];
-  const int at_mod[3] = {6, 13, 14};
+  const int at_mod[3] = {3, 7, 8};
   for (int i = 0; i < 3; ++i) {
     const at::Tensor* m = r.get(at_mod[i], 2);
     mod[i] = (const float*)r.address_of(m);
@@ -312,9 +322,9 @@ PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t na) {
     else if (stride >= 0 && s != stride) r.fail(PyExc_ValueError, "gate, scale and shift have the same stride", at_mod[i]);
     stride = s;
   }
-  const float res_scale = r.real(7);
+  const float res_scale = r.real(4);
   void *px = r.address_of(x), *ph = r.address_of(h), *pxo = r.address_of(x_out), *py = r.address_of(y);
-  void* stream = r.address(17);
+  void* stream = r.address(11);
   WMDEC_RETURN(g_residual_norm(px, xdt, ph, adt, &post, mod[0], res_scale, pxo, &pre, mod[1], mod[2], stride < 0 ? 0 : stride, py, (int)n, (int)x->size(1), (int)d, stream));
 }
 

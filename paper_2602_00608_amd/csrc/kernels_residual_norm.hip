@@ -19,7 +19,9 @@ struct Params {
   int tpr, segs;   // threads of a row, ranges of rows of a sample
 };
 
-template <typename T, bool VEC> __device__ __forceinline__ void load8(const T* p, int count, T (&v)[E]) {
+// A thread's eight channels of a vector are consecutive where rows are aligned; where they are not, they are `gap` apart, so that the lanes of every load and
+// store are next to each other.  `count` of them are there.
+template <typename T, bool VEC> __device__ __forceinline__ void load8(const T* p, int count, int gap, T (&v)[E]) {
   if constexpr (VEC) {
     u32x4 q[sizeof(T) / 2];
 #pragma unroll
@@ -31,10 +33,10 @@ template <typename T, bool VEC> __device__ __forceinline__ void load8(const T* p
     __builtin_memcpy(&v, &q, sizeof(v));
   } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = e < count ? p[e] : T{};
+    for (int e = 0; e < E; ++e) v[e] = e < count ? p[e * gap] : T{};
   }
 }
-template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int count, const float (&v)[E]) {
+template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int count, int gap, const float (&v)[E]) {
   T t[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) t[e] = from_float<T>(v[e]);
@@ -48,12 +50,12 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      if (e < count) p[e] = t[e];
+      if (e < count) p[e * gap] = t[e];
   }
 }
 // eight of a vector that may be missing
-template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long at, int count, float missing, float (&v)[E]) {
-  if (p) load8<float, VEC>(p + at, count, v);
+template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long at, int count, int gap, float missing, float (&v)[E]) {
+  if (p) load8<float, VEC>(p + at, count, gap, v);
   else {
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = missing;
@@ -62,7 +64,7 @@ template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long
 
 // VPT vectors a thread, R rows at once
 template <typename TX, typename TA, int VPT, int R, bool VEC>
-__global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
+__global__ __launch_bounds__(kMaxThreads, VPT == 1 && VEC ? 4 : 2) void residual_norm_kernel(Params p) {
   __shared__ float4 s_red[2][2][R][kMaxThreads / 64];
   const ResidualNormArgs& a = p.a;
   const int d = a.d, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -70,12 +72,13 @@ __global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
   const int n = blockIdx.x / p.segs, seg = blockIdx.x % p.segs;
   const int row0 = (int)((long)a.t * seg / p.segs), row1 = (int)((long)a.t * (seg + 1) / p.segs);
   const bool has_h = a.h != nullptr, has_y = a.y != nullptr;
+  const int gap = min(p.tpr, 64);
   int col[VPT], count[VPT];
   float held = 0.f;                       // values of this wavefront in a row
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    col[i] = (i * p.tpr + lane) * E;
-    count[i] = min(max(d - col[i], 0), E);
+    col[i] = VEC ? (i * p.tpr + lane) * E : i * p.tpr * E + (p.tpr < 64 ? lane : wave * 64 * E + (tid & 63));
+    count[i] = min(VEC ? max(d - col[i], 0) : max(d - col[i] + gap - 1, 0) / gap, E);
     held += (float)min(max(d - (i * p.tpr + wave * 64) * E, 0), 64 * E);
   }
   const TX* x = (const TX*)a.x + (long)n * a.t * d;
@@ -91,8 +94,8 @@ __global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
       const long at = (long)min(first + r * groups + group, row1 - 1) * d;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
-        load8<TX, VEC>(x + at + col[i], count[i], rx[r][i]);
-        if (has_h) load8<TA, VEC>(h + at + col[i], count[i], rh[r][i]);
+        load8<TX, VEC>(x + at + col[i], count[i], gap, rx[r][i]);
+        if (has_h) load8<TA, VEC>(h + at + col[i], count[i], gap, rh[r][i]);
       }
     }
   };
@@ -106,19 +109,19 @@ __global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
   for (int i = 0; i < VPT; ++i) {
     float w[E], u[E], m[E];
     if (has_h) {
-      vector8<VEC>(a.gate, mod + col[i], count[i], 1.f, m);
-      vector8<VEC>(a.post.weight, col[i], count[i], 1.f, w);
-      vector8<VEC>(a.post.bias, col[i], count[i], 0.f, u);
+      vector8<VEC>(a.gate, mod + col[i], count[i], gap, 1.f, m);
+      vector8<VEC>(a.post.weight, col[i], count[i], gap, 1.f, w);
+      vector8<VEC>(a.post.bias, col[i], count[i], gap, 0.f, u);
 #pragma unroll
       for (int e = 0; e < E; ++e) { ga[i][e] = a.res_scale * m[e] * w[e]; gb[i][e] = a.res_scale * m[e] * u[e]; }
     }
     if (has_y) {
-      vector8<VEC>(a.scale, mod + col[i], count[i], 0.f, m);
-      vector8<VEC>(a.pre.weight, col[i], count[i], 1.f, w);
-      vector8<VEC>(a.pre.bias, col[i], count[i], 0.f, u);
+      vector8<VEC>(a.scale, mod + col[i], count[i], gap, 0.f, m);
+      vector8<VEC>(a.pre.weight, col[i], count[i], gap, 1.f, w);
+      vector8<VEC>(a.pre.bias, col[i], count[i], gap, 0.f, u);
 #pragma unroll
       for (int e = 0; e < E; ++e) { ya[i][e] = w[e] * (1.f + m[e]); yb[i][e] = u[e] * (1.f + m[e]); }
-      vector8<VEC>(a.shift, mod + col[i], count[i], 0.f, m);
+      vector8<VEC>(a.shift, mod + col[i], count[i], gap, 0.f, m);
 #pragma unroll
       for (int e = 0; e < E; ++e) yb[i][e] += m[e];
     }
@@ -150,12 +153,15 @@ __global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
       }
       float sq = 0.f;
 #pragma unroll
-      for (int i = 0; i < VPT; ++i)
+      for (int i = 0; i < VPT; ++i) {
+        float part = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float dev = e < count[i] ? v[r][i][e] - mean[r] : 0.f;
-          sq = fmaf(dev, dev, sq);
+          const float dev = v[r][i][e] - mean[r];
+          part = VEC || e < count[i] ? fmaf(dev, dev, part) : part;
         }
+        sq += VEC && count[i] == 0 ? 0.f : part;
+      }
       m2[r] = row_sum(sq);
     }
     if (p.tpr > 64) {
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
         for (int i = 0; i < VPT; ++i) {
 #pragma unroll
           for (int e = 0; e < E; ++e) v[r][i][e] = round_through<TX>(v[r][i][e] + fmaf(b[r][i][e], ga[i][e], gb[i][e]));   // (what is stored is what is normalised)
-          if (row < row1) store8<TX, VEC>(x_out + (long)row * d + col[i], count[i], v[r][i]);
+          if (row < row1) store8<TX, VEC>(x_out + (long)row * d + col[i], count[i], gap, v[r][i]);
         }
       }
     }
@@ -232,7 +238,7 @@ __global__ __launch_bounds__(kMaxThreads) void residual_norm_kernel(Params p) {
       for (int i = 0; i < VPT; ++i) {
 #pragma unroll
         for (int e = 0; e < E; ++e) v[r][i][e] = fmaf(v[r][i][e], ya[i][e], yb[i][e]);
-        if (row < row1) store8<TA, VEC>(y + (long)row * d + col[i], count[i], v[r][i]);
+        if (row < row1) store8<TA, VEC>(y + (long)row * d + col[i], count[i], gap, v[r][i]);
       }
     }
   }
@@ -242,7 +248,8 @@ template <typename TX, typename TA, int VPT, int R, bool VEC>
 int launch_form(const ResidualNormArgs& a, int tpr, int threads, hipStream_t s) {
   Params p{a, tpr, 1};
   const int groups = tpr < 64 ? threads / tpr : 1;
-  const int most = (a.t + groups * R - 1) / (groups * R), target = 4096 / (threads / 64) / a.n;   // workgroups: 16 wavefronts a compute unit
+  const int most = (a.t + groups * R - 1) / (groups * R), waves = VPT == 1 && VEC ? 16 : 8;   // wavefronts of a compute unit
+  const int target = 256 * (waves / (threads / 64)) / a.n;   // all workgroups at once: those of a second round would run alone
   p.segs = max(1, min(most, target));
   hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, R, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);
   WMDEC_HIP(hipGetLastError());

@@ -300,16 +300,8 @@ def _device():
     return torch.cuda.current_device() if _current_device is None else _current_device()
 
 
-class Norm(collections.namedtuple("Norm", "kind eps weight bias", defaults=(0.0, None, None))):
-    """A norm over the channels of a row: kind "none", "layer" or "rms", eps, fp32 weight and bias [d] or None."""
-
-
-_NORM_KINDS = {"none": 0, "layer": 1, "rms": 2}
-_NO_NORM = (0, 0.0, None, None)
-
-
-def _norm(spec):
-    return _NO_NORM if spec is None else (_NORM_KINDS[spec[0]],) + tuple(spec[1:])
+Norm = collections.namedtuple("Norm", "kind eps weight bias", defaults=(0.0, None, None))
+Norm.__doc__ = """A norm over the channels of a row: kind "none", "layer" or "rms", eps, fp32 weight and bias [d] or None."""
 
 
 def residual_norm(x, h, post, gate, res_scale, x_out, pre, scale, shift, y):
@@ -317,7 +309,7 @@ def residual_norm(x, h, post, gate, res_scale, x_out, pre, scale, shift, y):
     x, x_out [n,t,d]; h, y [n,t,d] of x's type, or 16-bit beside an fp32 x; gate, scale, shift fp32 [n,d] with one row stride (the
     thirds of adaln_fused_projection's output: shift, scale, gate) or None; post, pre: a Norm or None.  h None: y = pre(x) * ...;
     y None: x_out alone.  x_out may be x, y may be h."""
-    _check(_ops().residual_norm(x, h, *_norm(post), gate, res_scale, x_out, *_norm(pre), scale, shift, y, _device(), _stream()))
+    _check(_ops().residual_norm(x, h, post, gate, res_scale, x_out, pre, scale, shift, y, _device(), _stream()))
 
 
 _ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
