@@ -20,7 +20,7 @@ BINDING = os.path.join(HERE, "_binding.so")
 
 SOURCES = ["api.cpp", "kernels_gn.hip", "kernels_conv_direct.hip", "kernels_conv_mfma.hip", "kernels_conv_rows.hip", "kernels_conv_rows_bf16.hip", "kernels_conv_ksplit.hip", "kernels_conv_up.hip",
            "kernels_conv_taps.hip", "kernels_misc.hip", "kernels_attn.hip", "kernels_adaln.hip", "kernels_residual_norm.hip",
-           "kernels_rope.hip", "kernels_cross.hip"]
+           "kernels_rope.hip", "kernels_cross.hip", "kernels_cross_bf16.hip", "kernels_cross_f32.hip"]
 
 # what asm_check looks for beside the stores of every source: kernels with matrix instructions in inline assembly, kernels that must not spill
 CHECKED = {"kernels_attn.hip": {"scores": "flash_attn_kernel"}, "kernels_conv_rows.hip": {"spills": "conv_mfma_kernel"},

@@ -25,14 +25,6 @@ constexpr int D = 512;            // head dimension
 constexpr int KB = 32;            // tokens per tile
 constexpr int TILE = KB * D;      // elements of a tile
 
-// lane l: its own a and the a of lane l + 32 (l < 32), or the b of lane l - 32 and its own b: four channels of eight become
-// eight of four when a and b hold an accumulator tile's channels 8 * g + 4 * lk + 0..3 for g and g + 1
-__device__ __forceinline__ u32x4 join_halves(u32x2 a, u32x2 b) {
-  const u32x2 lo = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
-  const u32x2 hi = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
-  return u32x4{lo.x, hi.x, lo.y, hi.y};
-}
-
 // ---------------------------------------------------------------- q, k, v projection
 // A workgroup takes 64 tokens and the 512 channels of one of q, k, v: the normalised input (64 KiB) is staged once, after
 // which eight wavefronts (64 tokens x 64 channels each) walk the contraction without a barrier.  Bound by the 512 KiB of
@@ -205,20 +197,6 @@ constexpr int NT = 256;           // threads: four wavefronts of 32 queries
 constexpr int R = 8;              // fragments read from LDS ahead of their MFMAs, a divisor of 32
 constexpr float kSlack = 8.0f;    // log2 of how far a block's maximum may exceed the running reference before it moves
 constexpr size_t kSmemBytes = (size_t)4 * TILE * 2;
-
-__device__ __forceinline__ float max3(float a, float b, float c) {   // (fmaxf would quiet its operands first: twice the instructions)
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-// max over lanes l and l ^ 32 (the results of the swap are made opaque: this compiler otherwise takes both for the first one)
-__device__ __forceinline__ float half_max(float v) {
-  const unsigned u = __builtin_bit_cast(unsigned, v);
-  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  unsigned a = r.x, b = r.y;
-  asm volatile("" : "+v"(a), "+v"(b));
-  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
-}
 
 // Registers.  The output accumulators of a wavefront (32 queries x 512) are 256 registers, exactly the accumulation half of the
 // register file; its query fragments are 128 of the other half.  The compiler gives every MFMA of a kernel its result in the

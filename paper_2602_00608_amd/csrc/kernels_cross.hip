@@ -1,54 +1,43 @@
-// Attention to states of another length: o = softmax(scale * q k^T over the valid keys) v.
-#include "common.hpp"
+// Attention to states of another length: o = softmax(scale * q k^T over the valid keys) v.  The kernels are in cross_device.hpp; here is what is decided on
+// sizes alone, and the f16 kernels.
+#include "cross_device.hpp"
 
 namespace wmdec {
+
+template int cross_launch<f16_t>(const CrossLaunch&, int, bool, hipStream_t);
+
 namespace {
 
-// A wavefront takes one row (a token of one query head); a lane holds every 64th channel, scores are summed over the lanes key by
-// key, with the running maximum and sum of the softmax.
-template <typename T>
-__global__ __launch_bounds__(64) void cross_attention_kernel(CrossArgs a) {
-  const int lane = threadIdx.x, heads_q = a.heads * a.group;
-  const long row = blockIdx.x;
-  const int hq = (int)(row % heads_q), tok = (int)(row / heads_q % a.tq), n = (int)(row / ((long)heads_q * a.tq)), h = hq / a.group;
-  const int len = a.lens ? min(max(a.lens[n], 0), a.tk) : a.tk;
-  const T* q = (const T*)a.q + n * a.qs.sample + tok * a.qs.token + hq * a.qs.head;
-  const T* k = (const T*)a.k + n * a.ks.sample + h * a.ks.head;
-  const T* v = (const T*)a.v + n * a.vs.sample + h * a.vs.head;
-  float qv[4], acc[4], m = -INFINITY, l = 0.f;
-  for (int i = 0; i < 4; ++i) { qv[i] = lane + 64 * i < a.d ? to_float(q[lane + 64 * i]) : 0.f; acc[i] = 0.f; }
-  const float c = a.scale * 1.4426950408889634f;
-  for (int j = 0; j < len; ++j) {
-    if (a.mask && !a.mask[(long)n * a.tk + j]) continue;
-    float s = 0.f;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.d) s = fmaf(qv[i], to_float(k[j * a.ks.token + lane + 64 * i]), s);
-    for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w);
-    s *= c;
-    if (s == -INFINITY) continue;   // (weight zero, also where the maximum is -inf itself)
-    const float top = fmaxf(m, s);
-    const float keep = __builtin_amdgcn_exp2f(m - top), p = __builtin_amdgcn_exp2f(s - top);
-    m = top;
-    l = fmaf(l, keep, p);
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.d) acc[i] = fmaf(acc[i], keep, p * to_float(v[j * a.vs.token + lane + 64 * i]));
-  }
-  T* o = (T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head;
-  for (int i = 0; i < 4; ++i)
-    if (lane + 64 * i < a.d) o[lane + 64 * i] = from_float<T>(l == 0.f ? 0.f : acc[i] / l);
+// channels of a head that the kernels are made for
+int width_of(int d) { return d <= 128 ? (d + 31) / 32 * 32 : d <= 192 ? 192 : 256; }
+
+// Ranges of keys of a row: workgroups for every compute unit twice, of 256 keys at least.  Independent of the batch, so that the bits of a sample are.
+int splits_of(int tk, int heads, long rows) {
+  const long units = heads * (rows <= 32 ? 1 : (rows + 127) / 128);
+  const long want = (512 + units - 1) / units, most = tk / 256;
+  return (int)max(1L, min(min(want, most), (long)kCrossMaxSplits));
 }
 
 }  // namespace
 
-size_t cross_attention_scratch_bytes(int, int, int, int, int, int, int) { return 0; }
+size_t cross_attention_scratch_bytes(int dtype, int tk, int n, int tq, int heads, int group, int d) {
+  const long rows = (long)tq * group;
+  const int splits = splits_of(tk, heads, rows);
+  return splits == 1 ? 0 : (size_t)splits * n * heads * rows * (width_of(d) + 2) * sizeof(float);
+}
 
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.n * a.tq * a.heads * a.group));
-  if (dtype == WMDEC_F32) hipLaunchKernelGGL(cross_attention_kernel<float>, grid, dim3(64), 0, s, a);
-  else if (dtype == WMDEC_BF16) hipLaunchKernelGGL(cross_attention_kernel<bf16_t>, grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(cross_attention_kernel<f16_t>, grid, dim3(64), 0, s, a);
-  WMDEC_HIP(hipGetLastError());
-  return WMDEC_OK;
+  CrossLaunch p;
+  p.a = a;
+  p.rows = a.tq * a.group;
+  p.row_blocks = 0;
+  p.splits = splits_of(a.tk, a.heads, p.rows);
+  const int width = width_of(a.d);
+  p.part = (float*)a.scratch;
+  p.ml = (float2*)(p.part + (size_t)p.splits * a.n * a.heads * p.rows * width);
+  const bool few = p.rows <= 32;
+  if (dtype == WMDEC_F32) return cross_launch<float>(p, width, few, s);
+  return dtype == WMDEC_BF16 ? cross_launch<bf16_t>(p, width, few, s) : cross_launch<f16_t>(p, width, few, s);
 }
 
 }  // namespace wmdec

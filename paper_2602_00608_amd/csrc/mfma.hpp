@@ -60,4 +60,26 @@ template <> __device__ __forceinline__ uint32_t pack2<bf16_t>(float a, float b) 
 template <typename T> __device__ __forceinline__ float unpack_lo(uint32_t w) { return to_float(T{(uint16_t)(w & 0xffffu)}); }
 template <typename T> __device__ __forceinline__ float unpack_hi(uint32_t w) { return to_float(T{(uint16_t)(w >> 16)}); }
 
+// lane l: its own a and the a of lane l + 32 (l < 32), or the b of lane l - 32 and its own b: four channels of eight become
+// eight of four when a and b hold an accumulator tile's channels 8 * g + 4 * lk + 0..3 for g and g + 1
+__device__ __forceinline__ u32x4 join_halves(u32x2 a, u32x2 b) {
+  const u32x2 lo = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
+  const u32x2 hi = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
+  return u32x4{lo.x, hi.x, lo.y, hi.y};
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {   // (fmaxf would quiet its operands first: twice the instructions)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+// max over lanes l and l ^ 32 (the results of the swap are made opaque: this compiler otherwise takes both for the first one)
+__device__ __forceinline__ float half_max(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  unsigned a = r.x, b = r.y;
+  asm volatile("" : "+v"(a), "+v"(b));
+  return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
 }  // namespace wmdec
