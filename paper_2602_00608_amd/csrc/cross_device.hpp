@@ -31,43 +31,44 @@ template <int CH> __device__ __forceinline__ int chunk_turn(int row) {   // CH: 
 
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // (NaN if one is: one instruction for three)
 
+constexpr int kMaskKeys = 32768;      // keys whose mask is staged as bits at a time
+
 // D: channels, rounded up to a multiple of 32; a wavefront has QT * 32 rows; QW x KW wavefronts
 template <typename T, int D, int QT, int QW, int KW, int KT>
 struct CrossForm {
   static constexpr int EC = kChunkElems<T>, CH = D / EC, NW = QW * KW, NT = 64 * NW, SUB = KT / KW, NS = SUB / 32, LOADS = KT * CH / NT, BQ = 32 * QT * QW;
   static constexpr int TILE = KT * D;
-  static constexpr int kSmem = 4 * TILE * (int)sizeof(T);
+  static constexpr int kTiles = 4 * TILE * (int)sizeof(T), kSmem = kTiles + kMaskKeys / 8;
   static constexpr int RED = D + 4;   // floats from row to row of the outputs that are joined
   static_assert(D % 32 == 0 && KT % (32 * KW) == 0 && KT * CH % NT == 0 && (KW == 1 || (QW == 1 && QT == 1)));
-  static_assert(kSmem <= 128 * 1024 && (KW == 1 || KW * 32 * (RED + 2) * 4 <= kSmem));
+  static_assert(kTiles <= 128 * 1024 && 3 * LOADS < 64 && (KW == 1 || KW * 32 * (RED + 2) * 4 <= kTiles));
 };
 
+// Tiles are asked for and waited for in assembly: the compiler would wait for all of them in front of every transposed read.  No registers are written.
+// 16 bytes a lane from `offset` of the buffer to lds + 16 * lane; past the buffer's end the LDS gets zeros.
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, unsigned offset, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(offset), "s"(buffer) : "memory", "m0");
+}
+// all but the last N loads of this wavefront have landed
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 // every load and LDS access of this wavefront is done, and so for the others
-__device__ __forceinline__ void sync_tiles() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-}
+__device__ __forceinline__ void sync_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 // the same for LDS accesses alone: tiles on their way are not waited for
-__device__ __forceinline__ void sync_lds() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0xC07F);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-}
+__device__ __forceinline__ void sync_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+constexpr unsigned kPastEnd = 0x80000000u;   // an offset that no buffer reaches
 
 constexpr float kCrossSlack = 8.0f;   // log2 of how far a tile's maximum may exceed the reference before that moves
 
 template <typename T, int D, int QT, int QW, int KW, int KT, int WAVES>
 __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(CrossLaunch p) {
   using F = CrossForm<T, D, QT, QW, KW, KT>;
-  constexpr int EC = F::EC, CH = F::CH, NW = F::NW, NS = F::NS, LOADS = F::LOADS, TILE = F::TILE, QS = CH / 2, ND = D / 32, MW = (KT + 63) / 64;
+  constexpr int EC = F::EC, CH = F::CH, NW = F::NW, NS = F::NS, LOADS = F::LOADS, TILE = F::TILE, QS = CH / 2, ND = D / 32;
   constexpr int GP = CH % 8 == 0 ? 8 : 4;   // chunks that are exchanged among each other
-  constexpr bool WIDE = sizeof(T) == 4;
+  constexpr bool WIDE = sizeof(T) == 4, OWN = KW > 1;   // OWN: a wavefront loads the keys it works on, and waits for nobody
   extern __shared__ __align__(16) unsigned char smem[];
   T* s_k = reinterpret_cast<T*>(smem);      // [2] tiles
   T* s_v = s_k + 2 * TILE;
+  unsigned* s_bits = reinterpret_cast<unsigned*>(smem + F::kTiles);   // the mask, 32 keys a word
   const CrossArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lk = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = wave / KW, kw = wave % KW;
@@ -81,58 +82,34 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   const int len = a.lens ? min(max(a.lens[n], 0), a.tk) : a.tk;
   const int tiles = (len + KT - 1) / KT, first = (int)((long)split * tiles / p.splits), nt = (int)((long)(split + 1) * tiles / p.splits) - first;
 
-  // ---- tiles
-  typedef const __attribute__((address_space(1))) void* gptr_t;
-  typedef __attribute__((address_space(3))) void* lptr_t;
+  // ---- tiles.  A load is 64 consecutive chunks of a tile; chunks past the last channel and keys past the last one are read past the buffer's end
+  const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const char* kp = (const char*)a.k + (n * a.ks.sample + h * a.ks.head) * (long)sizeof(T);
   const char* vp = (const char*)a.v + (n * a.vs.sample + h * a.vs.head) * (long)sizeof(T);
   const int kstep = (int)(a.ks.token * (long)sizeof(T)), vstep = (int)(a.vs.token * (long)sizeof(T));   // (128 of them are below 2^31: checked on the host)
   const unsigned char* mask = a.mask ? a.mask + (long)n * a.tk : nullptr;
-  int chunk[LOADS], koff[LOADS], voff[LOADS];
-  auto slot = [&](int i) { return (i * NW + wave) * 64 + lane; };
-  bool there[LOADS];
+  auto slot0 = [&](int i) { return OWN ? wave * F::SUB * CH + i * 64 : (i * NW + wave) * 64; };
+  unsigned koff[LOADS], voff[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
-    const int r = slot(i) / CH;
-    const int c = (slot(i) % CH) ^ chunk_turn<CH>(r);
-    there[i] = c * EC < a.d;
-    chunk[i] = c * 16;
-    koff[i] = r * kstep + c * 16;
-    voff[i] = r * vstep + c * 16;
-    if (!there[i]) {   // channels past the last: zero in both buffers, once
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        *reinterpret_cast<u32x4*>(s_k + b * TILE + slot(i) * EC) = u32x4{0, 0, 0, 0};
-        *reinterpret_cast<u32x4*>(s_v + b * TILE + slot(i) * EC) = u32x4{0, 0, 0, 0};
-      }
-    }
+    const int r = (slot0(i) + lane) / CH, c = ((slot0(i) + lane) % CH) ^ chunk_turn<CH>(r);
+    koff[i] = c * EC < a.d ? (unsigned)(r * kstep + c * 16) : kPastEnd;
+    voff[i] = c * EC < a.d ? (unsigned)(r * vstep + c * 16) : kPastEnd;
   }
-  int valid[MW];   // of the tile that is on its way: whether this lane's key of every 64 counts
-  auto ask = [&](int j) {
+  auto ask = [&](const char* base, int step, const unsigned (&off)[LOADS], int at, int j) {
     const int k0 = (first + j) * KT, left = len - k0;
-    const char *kt = kp + (long)k0 * kstep, *vt = vp + (long)k0 * vstep;
-    T *dk = s_k + (j & 1) * TILE, *dv = s_v + (j & 1) * TILE;
+    const uint64_t from = (uint64_t)(base + (long)k0 * step);
+    const u32x4 buffer{(unsigned)from, (unsigned)(from >> 32) & 0xffffu, kPastEnd - 1, 0x00020000u};
+    const unsigned to = lds + (at + (j & 1) * TILE) * (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      int ko = koff[i], vo = voff[i];
-      if (left < KT) {   // keys past the last one: the last one again
-        const int r = min(slot(i) / CH, left - 1);
-        ko = r * kstep + chunk[i];
-        vo = r * vstep + chunk[i];
-      }
-      if (there[i]) {
-        __builtin_amdgcn_global_load_lds((gptr_t)(kt + (unsigned)ko), (lptr_t)(dk + (i * NW + wave) * 64 * EC), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((gptr_t)(vt + (unsigned)vo), (lptr_t)(dv + (i * NW + wave) * 64 * EC), 16, 0, 0);
-      }
-    }
-#pragma unroll
-    for (int w = 0; w < MW; ++w) {
-      const int key = w * 64 + lane;
-      valid[w] = key < left && (KT >= 64 || lane < KT);
-      if (mask && valid[w]) valid[w] = mask[k0 + key];
+      unsigned o = off[i];
+      if (left < KT) o = (slot0(i) + lane) / CH < left ? o : kPastEnd;
+      load_to_lds(buffer, o, to + slot0(i) * 16);
     }
   };
-  if (nt > 0) ask(0);
+  auto ask_k = [&](int j) { ask(kp, kstep, koff, 0, j); };
+  auto ask_v = [&](int j) { ask(vp, vstep, voff, 2 * TILE, j); };
 
   // ---- queries: chunk 2 s + lk of the lane's row
   const int row0 = rb * F::BQ + qw * QT * 32 + l32;
@@ -178,31 +155,9 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   }
   const float c = a.scale * 1.4426950408889634f;
 
-  for (int j = 0; j < nt; ++j) {
-    sync_tiles();           // the tile has landed, and every wavefront is done with the other buffer
-    unsigned long long word[MW], any = 0;
-    bool all = true;
-#pragma unroll
-    for (int w = 0; w < MW; ++w) {
-      word[w] = __ballot(valid[w] != 0);
-      any |= word[w];
-      all = all && word[w] == (KT >= 64 ? ~0ull : (1ull << (KT & 63)) - 1);
-    }
-    if (j + 1 < nt) ask(j + 1);
-    if (any == 0) continue;
-    T *tk = s_k + (j & 1) * TILE, *tv = s_v + (j & 1) * TILE;
-    if (!all) {             // what a masked value holds times a probability of zero need not be zero
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int r = slot(i) / CH;
-        if (!((word[MW == 1 ? 0 : r / 64] >> (r & 63)) & 1)) *reinterpret_cast<u32x4*>(tv + slot(i) * EC) = u32x4{0, 0, 0, 0};
-      }
-      sync_lds();
-    }
-    tk += kw * F::SUB * D;
-    tv += kw * F::SUB * D;
-
-    f32x16 s[QT][NS];
+  f32x16 s[QT][NS];
+  // scores of a tile (its valid keys in `bits`)
+  auto scores = [&](const T* tk, const unsigned (&bits)[NS]) {
 #pragma unroll
     for (int ns = 0; ns < NS; ++ns) {
 #pragma unroll
@@ -222,18 +177,18 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
           }
         }
       }
-      if (!all) {
-        const int at = kw * F::SUB + ns * 32;
-        const unsigned bits = (unsigned)(word[MW == 1 ? 0 : at / 64] >> (at & 63)) >> (4 * lk);
+      if (bits[ns] != ~0u) {
+        const unsigned b = bits[ns] >> (4 * lk);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (!((bits >> (8 * (r / 4) + r % 4)) & 1)) {
+          if (!((b >> (8 * (r / 4) + r % 4)) & 1)) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) s[t][ns][r] = -INFINITY;
           }
       }
     }
-
+  };
+  auto softmax = [&]() {
     // softmax: the reference moves when a maximum exceeds it by 2^kCrossSlack; until then probabilities may reach that, well inside the 16-bit types
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -261,7 +216,8 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
           l[t] += s[t][ns][r];
         }
     }
-
+  };
+  auto values = [&](const T* tv) {
 #pragma unroll
     for (int ns = 0; ns < NS; ++ns) {
       if constexpr (WIDE) {
@@ -295,6 +251,101 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         }
       }
     }
+  };
+
+  // The mask of up to kMaskKeys keys is staged at a time; without one all keys are one block.
+  constexpr int MB = kMaskKeys / KT;
+  for (int b0 = 0; b0 < nt;) {
+    const int b1 = mask ? min(nt, b0 + MB) : nt;
+    if (mask) {
+      if (b0) sync_tiles();   // (the bits before have been read)
+      const int k0 = (first + b0) * KT, words = ((b1 - b0) * KT + 63) / 64;
+#pragma unroll 4
+      for (int w = wave; w < words; w += NW) {
+        const int key = k0 + w * 64 + lane;
+        const unsigned long long bit = __ballot(key < len && mask[min(key, len - 1)] != 0);
+        if (lane == 0) *reinterpret_cast<u32x2*>(s_bits + 2 * w) = u32x2{(unsigned)bit, (unsigned)(bit >> 32)};
+      }
+      sync_lds();
+    }
+    // valid keys of the wavefront's part of tile j
+    bool none, all;
+    auto valid = [&](int j, unsigned (&bits)[NS]) {
+      none = true; all = true;
+#pragma unroll
+      for (int ns = 0; ns < NS; ++ns) {
+        const int at = kw * F::SUB + ns * 32, left = len - (first + j) * KT - at;
+        unsigned u = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+        if (mask) u &= __builtin_amdgcn_readfirstlane(s_bits[((j - b0) * KT + at) / 32]);
+        bits[ns] = u;
+        none = none && u == 0;
+        all = all && u == ~0u;
+      }
+    };
+    // what a masked value holds times a probability of zero need not be zero (keys past the last one are zeros already)
+    auto clear = [&](T* tile, const unsigned (&bits)[NS]) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = (slot0(i) + lane) / CH - kw * F::SUB;
+        unsigned u = bits[0];
+#pragma unroll
+        for (int ns = 1; ns < NS; ++ns) u = r / 32 == ns ? bits[ns] : u;
+        if (!((u >> (r & 31)) & 1)) *reinterpret_cast<u32x4*>(tile + (slot0(i) + lane) * EC) = u32x4{0, 0, 0, 0};
+      }
+    };
+    unsigned bits[NS];
+    // (the queries are waited for here: the compiler, which does not see the tiles' loads, would wait for all of them wherever it first uses a query)
+    auto queries_landed = [&]() {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int s = 0; s < QS; ++s) asm volatile("" : "+v"(q[t][s]));
+    };
+    if constexpr (OWN) {
+      // keys and values each have two tiles on their way while a third is worked on
+      ask_k(b0);
+      ask_v(b0);
+      if (b0 + 1 < b1) { ask_k(b0 + 1); ask_v(b0 + 1); }
+      queries_landed();
+      for (int j = b0; j < b1; ++j) {
+        T *tk = s_k + (j & 1) * TILE + kw * F::SUB * D, *tv = s_v + (j & 1) * TILE;
+        const int more = b1 - 1 - j;
+        valid(j, bits);
+        if (more > 0) wait_loads<3 * LOADS>();
+        else wait_loads<LOADS>();
+        if (!none) scores(tk, bits);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more > 1) ask_k(j + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!none) softmax();
+        if (more > 1) wait_loads<3 * LOADS>();
+        else if (more > 0) wait_loads<2 * LOADS>();
+        else wait_loads<0>();
+        if (!none) {
+          if (mask && !all) { clear(tv, bits); asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+          values(tv + kw * F::SUB * D);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more > 1) ask_v(j + 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      ask_k(b0);
+      ask_v(b0);
+      queries_landed();
+      for (int j = b0; j < b1; ++j) {
+        sync_tiles();       // the tile has landed, and every wavefront is done with the other buffer
+        T *tk = s_k + (j & 1) * TILE, *tv = s_v + (j & 1) * TILE;
+        if (j + 1 < b1) { ask_k(j + 1); ask_v(j + 1); }
+        valid(j, bits);
+        if (none) continue;
+        if (mask && !all) { clear(tv, bits); sync_lds(); }
+        scores(tk, bits);
+        softmax();
+        values(tv);
+      }
+    }
+    b0 = b1;
   }
 
   // ---- output.  A lane holds channels 32 dt + 8 g + 4 lk .. + 3 of its row
