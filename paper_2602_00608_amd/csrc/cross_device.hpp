@@ -4,22 +4,29 @@
 // wavefront forms S^T = K Q^T (keys along the accumulator's registers, one row a lane), the softmax against a running maximum, and O^T += V^T P^T with the
 // probabilities as they are in their registers: an accumulator's keys of lane half lk are 8 (r / 4) + 4 lk + r % 4, so V^T is read from LDS in that order of
 // keys (16-bit types: transposed on the way, four keys of one channel a lane).  fp32 takes the same steps with 32x32x2 products.
-// The wavefronts of a workgroup take QT * 32 rows each (QW of them), or, where there are few rows, the same rows and a part of a tile's keys (KW), joined at the end.
+// The wavefronts of a workgroup take 32 rows each (QW of them), or, where there are few rows, the same rows and a part of a tile's keys (KW), joined at the end.
 //
 // 16-byte chunk c of key r lies at chunk c ^ turn(r) of its row in LDS: the eight lanes of a pass over K (eight keys, one chunk) and the sixteen over V (four
 // keys, two chunks) then have banks of their own.  The loads bring the chunks in that order, as a lane chooses what it reads and not where it lands.
 #pragma once
 #include <mutex>
 
-#include "mfma.hpp"
+#include "conv_device.hpp"
 
 namespace wmdec {
 
+// How the work is divided (kernels_cross.hip decides).  A block is BQ rows of a key head; it is a workgroup that writes the output, or `splits` workgroups that
+// take a range of the keys each and leave partial outputs, and a launch that joins these.
+struct CrossPlan {
+  int width = 0;                  // channels that the kernel is made for
+  bool few = false;               // 32 rows a workgroup, whose wavefronts share them; else 128
+  int rows = 0, row_blocks = 0, splits = 1;   // rows of a key head, blocks of them
+};
 struct CrossLaunch {
   CrossArgs a;
-  int rows, row_blocks, splits;   // rows of a key head, blocks of them, ranges of keys
-  float* part;                    // [split][sample][key head][row][D] sums of probabilities times values
-  float2* ml;                     // [split][sample][key head][row] reference and sum of the probabilities
+  CrossPlan plan;
+  float* part;                    // [sample][key head][row block][split][BQ][width] sums of probabilities times values
+  float2* ml;                     // [sample][key head][row block][split][BQ] reference and sum of the probabilities
 };
 
 template <typename T> constexpr int kChunkElems = 16 / (int)sizeof(T);
@@ -33,21 +40,21 @@ __device__ __forceinline__ float maximum(float a, float b) { return __builtin_el
 
 constexpr int kMaskKeys = 32768;      // keys whose mask is staged as bits at a time
 
-// D: channels, rounded up to a multiple of 32; a wavefront has QT * 32 rows; QW x KW wavefronts
-template <typename T, int D, int QT, int QW, int KW, int KT>
+// D: channels, rounded up to a multiple of 32; QW x KW wavefronts of 32 rows and 1 / KW of a tile's keys
+template <typename T, int D, int QW, int KW, int KT>
 struct CrossForm {
-  static constexpr int EC = kChunkElems<T>, CH = D / EC, NW = QW * KW, NT = 64 * NW, SUB = KT / KW, NS = SUB / 32, LOADS = KT * CH / NT, BQ = 32 * QT * QW;
-  static constexpr int TILE = KT * D;
-  static constexpr int kTiles = 4 * TILE * (int)sizeof(T), kSmem = kTiles + kMaskKeys / 8;
+  static constexpr int EC = kChunkElems<T>, CH = D / EC, NW = QW * KW, NT = 64 * NW, SUB = KT / KW, NS = SUB / 32, LOADS = KT * CH / NT, BQ = 32 * QW;
+  static constexpr int TILE = KT * D, NB = KW == 1 ? 2 : 1;   // buffers of keys, and of values
   static constexpr int RED = D + 4;   // floats from row to row of the outputs that are joined
-  static_assert(D % 32 == 0 && KT % (32 * KW) == 0 && KT * CH % NT == 0 && (KW == 1 || (QW == 1 && QT == 1)));
-  static_assert(kTiles <= 128 * 1024 && 3 * LOADS < 64 && (KW == 1 || KW * 32 * (RED + 2) * 4 <= kTiles));
+  static constexpr int kTiles = 2 * NB * TILE * (int)sizeof(T), kRed = KW == 1 ? 0 : KW * 32 * (RED + 2) * 4, kLow = kTiles > kRed ? kTiles : kRed, kSmem = kLow + kMaskKeys / 8;
+  static_assert(D % 32 == 0 && KT % (32 * KW) == 0 && KT * CH % NT == 0 && (KW == 1 || QW == 1));
+  static_assert(kSmem <= 160 * 1024 && LOADS < 64);
 };
 
 // Tiles are asked for and waited for in assembly: the compiler would wait for all of them in front of every transposed read.  No registers are written.
-// 16 bytes a lane from `offset` of the buffer to lds + 16 * lane; past the buffer's end the LDS gets zeros.
-__device__ __forceinline__ void load_to_lds(u32x4 buffer, unsigned offset, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(offset), "s"(buffer) : "memory", "m0");
+// 16 bytes a lane from `offset` + `more` of the buffer to lds + AT + 16 * lane; past the buffer's end the LDS gets zeros.  (Nothing else here uses M0.)
+template <int AT> __device__ __forceinline__ void load_to_lds(u32x4 buffer, unsigned offset, unsigned more, unsigned lds) {
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(buffer), "s"(more), "n"(AT) : "memory", "scc");
 }
 // all but the last N loads of this wavefront have landed
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
@@ -57,28 +64,40 @@ __device__ __forceinline__ void sync_tiles() { asm volatile("s_waitcnt vmcnt(0) 
 __device__ __forceinline__ void sync_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 constexpr unsigned kPastEnd = 0x80000000u;   // an offset that no buffer reaches
 
+// what a sum taken against the reference m counts for against the reference `top`, which is at least m (nothing seen yet: nothing)
+__device__ __forceinline__ float weight_of(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
+// four channels of a row from channel `at` on, if it has them
+template <typename T> __device__ __forceinline__ void store_quad(T* row, int at, int d, f32x4 v) {
+  if (at >= d) return;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(row + at) = v;
+  else *reinterpret_cast<u32x2*>(row + at) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+}
+
 constexpr float kCrossSlack = 8.0f;   // log2 of how far a tile's maximum may exceed the reference before that moves
 
-template <typename T, int D, int QT, int QW, int KW, int KT, int WAVES>
-__global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(CrossLaunch p) {
-  using F = CrossForm<T, D, QT, QW, KW, KT>;
-  constexpr int EC = F::EC, CH = F::CH, NW = F::NW, NS = F::NS, LOADS = F::LOADS, TILE = F::TILE, QS = CH / 2, ND = D / 32;
+template <typename T, int D, int QW, int KW, int KT, int WAVES>
+__global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(CrossLaunch launch) {
+  using F = CrossForm<T, D, QW, KW, KT>;
+  constexpr int EC = F::EC, CH = F::CH, NW = F::NW, NS = F::NS, LOADS = F::LOADS, TILE = F::TILE, NB = F::NB, QS = CH / 2, ND = D / 32;
   constexpr int GP = CH % 8 == 0 ? 8 : 4;   // chunks that are exchanged among each other
   constexpr bool WIDE = sizeof(T) == 4, OWN = KW > 1;   // OWN: a wavefront loads the keys it works on, and waits for nobody
   extern __shared__ __align__(16) unsigned char smem[];
-  T* s_k = reinterpret_cast<T*>(smem);      // [2] tiles
-  T* s_v = s_k + 2 * TILE;
-  unsigned* s_bits = reinterpret_cast<unsigned*>(smem + F::kTiles);   // the mask, 32 keys a word
-  const CrossArgs& a = p.a;
+  T* s_k = reinterpret_cast<T*>(smem);      // [NB] tiles
+  T* s_v = s_k + NB * TILE;
+  unsigned* s_bits = reinterpret_cast<unsigned*>(smem + F::kLow);   // the mask, 32 keys a word
+  const CrossArgs& a = launch.a;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lk = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = wave / KW, kw = wave % KW;
-  // workgroup id -> (sample, key head, key range, row block); the ids of one XCD (id % 8) are neighbours and share their keys
+  // workgroup id -> (sample, key head, range of keys, row block); within a sample the ids of one XCD (id % 8) are neighbours and share their keys.  (Neighbours over
+  // all samples: an XCD had one sample's work, and where samples have different lengths those with long ones ran alone.)
+  const CrossPlan& p = launch.plan;
+  const int per_sample = a.heads * p.splits * p.row_blocks, n = blockIdx.x / per_sample;
   int L;
   {
-    const int i = blockIdx.x, total = gridDim.x, per = total / 8, rem = total % 8, x = i % 8, j = i / 8;
+    const int i = blockIdx.x - n * per_sample, per = per_sample / 8, rem = per_sample % 8, x = i % 8, j = i / 8;
     L = x * per + (x < rem ? x : rem) + j;
   }
-  const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, nh = L / (p.row_blocks * p.splits), h = nh % a.heads, n = nh / a.heads;
+  const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits);
   const int len = a.lens ? min(max(a.lens[n], 0), a.tk) : a.tk;
   const int tiles = (len + KT - 1) / KT, first = (int)((long)split * tiles / p.splits), nt = (int)((long)(split + 1) * tiles / p.splits) - first;
 
@@ -89,40 +108,47 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   const int kstep = (int)(a.ks.token * (long)sizeof(T)), vstep = (int)(a.vs.token * (long)sizeof(T));   // (128 of them are below 2^31: checked on the host)
   const unsigned char* mask = a.mask ? a.mask + (long)n * a.tk : nullptr;
   auto slot0 = [&](int i) { return OWN ? wave * F::SUB * CH + i * 64 : (i * NW + wave) * 64; };
-  unsigned koff[LOADS], voff[LOADS];
+  // Offsets of the loads: every PER-th one has the same chunks of keys that are a multiple of eight further, a scalar part of the address.
+  constexpr int ROWS = 64 % CH == 0 ? 64 / CH * (OWN ? 1 : NW) : 0;   // keys from a load to the next; 0: loads end inside a key
+  constexpr int PER = ROWS == 0 ? LOADS : ROWS % 8 == 0 ? 1 : 8 / ROWS < LOADS ? 8 / ROWS : LOADS;
+  unsigned koff[PER], voff[PER];
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int r = (slot0(i) + lane) / CH, c = ((slot0(i) + lane) % CH) ^ chunk_turn<CH>(r);
     koff[i] = c * EC < a.d ? (unsigned)(r * kstep + c * 16) : kPastEnd;
     voff[i] = c * EC < a.d ? (unsigned)(r * vstep + c * 16) : kPastEnd;
   }
-  auto ask = [&](const char* base, int step, const unsigned (&off)[LOADS], int at, int j) {
+  auto ask = [&](const char* base, int step, const unsigned (&off)[PER], int at, int j) {
     const int k0 = (first + j) * KT, left = len - k0;
     const uint64_t from = (uint64_t)(base + (long)k0 * step);
     const u32x4 buffer{(unsigned)from, (unsigned)(from >> 32) & 0xffffu, kPastEnd - 1, 0x00020000u};
-    const unsigned to = lds + (at + (j & 1) * TILE) * (int)sizeof(T);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      unsigned o = off[i];
+    const unsigned to = lds + (at + (NB == 2 ? j & 1 : 0) * TILE) * (int)sizeof(T) + slot0(0) * 16;
+    unsigned more = 0;
+    static_for<LOADS>([&](auto i_c) {
+      constexpr int i = decltype(i_c)::value;
+      if constexpr (i > 0 && i % PER == 0) {
+        more += PER * ROWS * step;
+        asm volatile("" : "+s"(more));   // (one after the other: worked out beforehand for all loads they do not fit the scalar registers)
+      }
+      unsigned o = off[i % PER];
       if (left < KT) o = (slot0(i) + lane) / CH < left ? o : kPastEnd;
-      load_to_lds(buffer, o, to + slot0(i) * 16);
-    }
+      load_to_lds<i * (OWN ? 1 : NW) * 1024>(buffer, o, more, to);
+    });
   };
   auto ask_k = [&](int j) { ask(kp, kstep, koff, 0, j); };
-  auto ask_v = [&](int j) { ask(vp, vstep, voff, 2 * TILE, j); };
+  auto ask_v = [&](int j) { ask(vp, vstep, voff, NB * TILE, j); };
 
   // ---- queries: chunk 2 s + lk of the lane's row
-  const int row0 = rb * F::BQ + qw * QT * 32 + l32;
-  u32x4 q[QT][QS];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int row = min(row0 + t * 32, p.rows - 1), tok = row / a.group, hq = h * a.group + (row - tok * a.group);
+  const int row = rb * F::BQ + qw * 32 + l32;
+  u32x4 q[QS];
+  {
+    const int r = min(row, p.rows - 1), tok = r / a.group, hq = h * a.group + (r - tok * a.group);
     const T* src = (const T*)a.q + n * a.qs.sample + tok * a.qs.token + hq * a.qs.head;
 #pragma unroll
     for (int s = 0; s < QS; ++s) {
       const int c = (2 * s + lk) * EC;
-      q[t][s] = u32x4{0, 0, 0, 0};
-      if (c < a.d) q[t][s] = *reinterpret_cast<const u32x4*>(src + c);
+      q[s] = u32x4{0, 0, 0, 0};
+      if (c < a.d) q[s] = *reinterpret_cast<const u32x4*>(src + c);
     }
   }
 
@@ -143,113 +169,130 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     }
   }
 
-  f32x16 o[QT][ND];
-  float m[QT], l[QT];
+  f32x16 o[ND];
+  float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = -INFINITY; l[t] = 0.f;
+  for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[t][dt][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
   const float c = a.scale * 1.4426950408889634f;
 
-  f32x16 s[QT][NS];
+  f32x16 s[NS];
+  // Fragments.  Where a SIMD has few wavefronts (EAGER) they are read RK and RV ahead of their products, in that order; else the compiler places them.
+  constexpr bool EAGER = OWN || WIDE;
+  constexpr int KF = NS * QS, RK = WIDE || D > 192 ? 4 : 8, VF = NS * (WIDE ? 16 : 2) * ND, RV = D > 192 ? 4 : 8;
+  u32x4 kr[RK];
+  typename std::conditional<WIDE, float, u32x4>::type vr[RV];
+  auto key_fragment = [&](const T* tk, auto i_c) -> u32x4 {        // i = ns * QS + step
+    constexpr int i = decltype(i_c)::value, ns = i / QS, st = i % QS;
+    return *reinterpret_cast<const u32x4*>(tk + kb[st % (GP / 2)] + st / (GP / 2) * GP * EC + ns * 32 * D);
+  };
+  auto value_fragment = [&](const T* tv, auto i_c) {               // i = (ns, register or half of 32 keys, channel tile)
+    constexpr int i = decltype(i_c)::value, dt = i % ND;
+    if constexpr (WIDE) {
+      constexpr int r = i / ND % 16, ns = i / ND / 16;
+      return to_float(tv[vb[r % 4] + (ns * 32 + 8 * (r / 4)) * D + dt * 32]);
+    } else {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4* tptr_t;
+      const T* at = tv + vb[dt % (GP / 4)] + dt / (GP / 4) * GP * EC + i / ND * 16 * D;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 8 * D)));
+      return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  };
+  auto score_step = [&](const u32x4& kf, auto i_c) {
+    constexpr int i = decltype(i_c)::value, ns = i / QS, st = i % QS;
+    if constexpr (st == 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[ns][r] = 0.f;
+    }
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[ns] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[st][e]), s[ns], 0, 0, 0);
+    } else {
+      s[ns] = Mma<T>::m32(kf, q[st], s[ns]);
+    }
+  };
   // scores of a tile (its valid keys in `bits`)
   auto scores = [&](const T* tk, const unsigned (&bits)[NS]) {
+    if constexpr (EAGER) {
+      static_for<(RK < KF ? RK : KF)>([&](auto i) { kr[decltype(i)::value] = key_fragment(tk, i); });
+      static_for<KF>([&](auto i_c) {
+        constexpr int i = decltype(i_c)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        score_step(kr[i % RK], i_c);
+        if constexpr (i + RK < KF) kr[i % RK] = key_fragment(tk, std::integral_constant<int, i + RK>{});
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
+      static_for<KF>([&](auto i) { score_step(key_fragment(tk, i), i); });
+    }
 #pragma unroll
-    for (int ns = 0; ns < NS; ++ns) {
-#pragma unroll
-      for (int t = 0; t < QT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][ns][r] = 0.f;
-#pragma unroll
-      for (int st = 0; st < QS; ++st) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(tk + kb[st % (GP / 2)] + st / (GP / 2) * GP * EC + ns * 32 * D);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          if constexpr (WIDE) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][ns] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[t][st][e]), s[t][ns], 0, 0, 0);
-          } else {
-            s[t][ns] = Mma<T>::m32(kf, q[t][st], s[t][ns]);
-          }
-        }
-      }
+    for (int ns = 0; ns < NS; ++ns)
       if (bits[ns] != ~0u) {
         const unsigned b = bits[ns] >> (4 * lk);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (!((b >> (8 * (r / 4) + r % 4)) & 1)) {
-#pragma unroll
-            for (int t = 0; t < QT; ++t) s[t][ns][r] = -INFINITY;
-          }
+          if (!((b >> (8 * (r / 4) + r % 4)) & 1)) s[ns][r] = -INFINITY;
       }
-    }
   };
+  // The reference moves when a maximum exceeds it by 2^kCrossSlack; until then probabilities may reach that, well inside the 16-bit types.
   auto softmax = [&]() {
-    // softmax: the reference moves when a maximum exceeds it by 2^kCrossSlack; until then probabilities may reach that, well inside the 16-bit types
+    float mx = maximum(maximum(s[0][0], s[0][1]), s[0][2]);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float mx = maximum(maximum(s[t][0][0], s[t][0][1]), s[t][0][2]);
+    for (int i = 3; i + 1 < 16 * NS; i += 2) mx = maximum(maximum(mx, s[i / 16][i % 16]), s[(i + 1) / 16][(i + 1) % 16]);
+    mx = maximum(mx, s[NS - 1][15]);
+    mx = half_max(mx) * c;
+    const bool moves = mx > m + kCrossSlack;
+    if (__ballot(moves)) {
+      const float to = moves ? mx : m, factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+      m = to;
+      l *= factor;
 #pragma unroll
-      for (int i = 3; i + 1 < 16 * NS; i += 2) mx = maximum(maximum(mx, s[t][i / 16][i % 16]), s[t][(i + 1) / 16][(i + 1) % 16]);
-      mx = maximum(mx, s[t][NS - 1][15]);
-      mx = half_max(mx) * c;
-      const bool moves = mx > m[t] + kCrossSlack;
-      if (__ballot(moves)) {
-        const float to = moves ? mx : m[t], factor = moves ? __builtin_amdgcn_exp2f(m[t] - mx) : 1.f;
-        m[t] = to;
-        l[t] *= factor;
+      for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
+        for (int r = 0; r < 16; ++r) o[dt][r] *= factor;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[t][dt][r] *= factor;
+    for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[ns][r] = __builtin_amdgcn_exp2f(fmaf(s[ns][r], c, -ref));
+        l += s[ns][r];
       }
-      const float ref = m[t] == -INFINITY ? 0.f : m[t];
-#pragma unroll
-      for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[t][ns][r] = __builtin_amdgcn_exp2f(fmaf(s[t][ns][r], c, -ref));
-          l[t] += s[t][ns][r];
-        }
+  };
+  auto values_head = [&](const T* tv) {
+    if constexpr (EAGER) {
+      static_for<(RV < VF ? RV : VF)>([&](auto i) { vr[decltype(i)::value] = value_fragment(tv, i); });
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   auto values = [&](const T* tv) {
-#pragma unroll
-    for (int ns = 0; ns < NS; ++ns) {
+    u32x4 pf;   // the one rounding inside the operator: probabilities as operands of T
+    auto value_step = [&](const auto& vf, auto i_c) {
+      constexpr int i = decltype(i_c)::value, dt = i % ND;
       if constexpr (WIDE) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt) {
-            const float vf = to_float(tv[vb[r % 4] + (ns * 32 + 8 * (r / 4)) * D + dt * 32]);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[t][ns][r], o[t][dt], 0, 0, 0);
-          }
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[i / ND / 16][i / ND % 16], o[dt], 0, 0, 0);
       } else {
+        constexpr int ns = i / ND / 2, ks = i / ND % 2;
+        if constexpr (dt == 0) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          u32x4 pf[QT];   // the one rounding inside the operator: probabilities as operands of T
-#pragma unroll
-          for (int t = 0; t < QT; ++t)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) pf[t][w] = pack2<T>(s[t][ns][8 * ks + 2 * w], s[t][ns][8 * ks + 2 * w + 1]);
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4* tptr_t;
-            const T* at = tv + vb[dt % (GP / 4)] + dt / (GP / 4) * GP * EC + (ns * 32 + ks * 16) * D;
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 8 * D)));
-            const u32x4 vf{lo.x, lo.y, hi.x, hi.y};
-#pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][dt] = Mma<T>::m32(vf, pf[t], o[t][dt]);
-          }
+          for (int w = 0; w < 4; ++w) pf[w] = pack2<T>(s[ns][8 * ks + 2 * w], s[ns][8 * ks + 2 * w + 1]);
         }
+        o[dt] = Mma<T>::m32(vf, pf, o[dt]);
       }
+    };
+    if constexpr (EAGER) {
+      static_for<VF>([&](auto i_c) {
+        constexpr int i = decltype(i_c)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        value_step(vr[i % RV], i_c);
+        if constexpr (i + RV < VF) vr[i % RV] = value_fragment(tv, std::integral_constant<int, i + RV>{});
+      });
+    } else {
+      static_for<VF>([&](auto i) { value_step(value_fragment(tv, i), i); });
     }
   };
 
@@ -260,7 +303,6 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     if (mask) {
       if (b0) sync_tiles();   // (the bits before have been read)
       const int k0 = (first + b0) * KT, words = ((b1 - b0) * KT + 63) / 64;
-#pragma unroll 4
       for (int w = wave; w < words; w += NW) {
         const int key = k0 + w * 64 + lane;
         const unsigned long long bit = __ballot(key < len && mask[min(key, len - 1)] != 0);
@@ -297,36 +339,32 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     // (the queries are waited for here: the compiler, which does not see the tiles' loads, would wait for all of them wherever it first uses a query)
     auto queries_landed = [&]() {
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
-#pragma unroll
-        for (int s = 0; s < QS; ++s) asm volatile("" : "+v"(q[t][s]));
+      for (int s = 0; s < QS; ++s) asm volatile("" : "+v"(q[s]));
     };
     if constexpr (OWN) {
-      // keys and values each have two tiles on their way while a third is worked on
+      // One buffer of either, asked for again as soon as it has been read: the next keys travel behind the softmax and the values, the next values behind the
+      // scores.  (Two buffers each: half the workgroups a compute unit, and slower throughout, 16 x 4096 keys of 8 heads of 128 channels 74.0 us against 55.3.)
       ask_k(b0);
       ask_v(b0);
-      if (b0 + 1 < b1) { ask_k(b0 + 1); ask_v(b0 + 1); }
       queries_landed();
+      static_assert(!OWN || NS == 1, "a wavefront has 32 keys of a tile");
+      T *tk = s_k + kw * F::SUB * D, *tv = s_v + kw * F::SUB * D;
       for (int j = b0; j < b1; ++j) {
-        T *tk = s_k + (j & 1) * TILE + kw * F::SUB * D, *tv = s_v + (j & 1) * TILE;
-        const int more = b1 - 1 - j;
+        const bool more = j + 1 < b1;
         valid(j, bits);
-        if (more > 0) wait_loads<3 * LOADS>();
-        else wait_loads<LOADS>();
+        wait_loads<LOADS>();
         if (!none) scores(tk, bits);
         __builtin_amdgcn_sched_barrier(0);
-        if (more > 1) ask_k(j + 2);
-        __builtin_amdgcn_sched_barrier(0);
-        if (!none) softmax();
-        if (more > 1) wait_loads<3 * LOADS>();
-        else if (more > 0) wait_loads<2 * LOADS>();
+        if (more) { ask_k(j + 1); wait_loads<LOADS>(); }
         else wait_loads<0>();
         if (!none) {
-          if (mask && !all) { clear(tv, bits); asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
-          values(tv + kw * F::SUB * D);
+          if (mask && !all) { clear(s_v, bits); asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+          values_head(tv);
+          softmax();
+          values(tv);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (more > 1) ask_v(j + 2);
+        if (more) ask_v(j + 1);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
@@ -341,6 +379,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         if (none) continue;
         if (mask && !all) { clear(tv, bits); sync_lds(); }
         scores(tk, bits);
+        values_head(tv);
         softmax();
         values(tv);
       }
@@ -349,51 +388,44 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   }
 
   // ---- output.  A lane holds channels 32 dt + 8 g + 4 lk .. + 3 of its row
-#pragma unroll
-  for (int t = 0; t < QT; ++t) l[t] += __shfl_xor(l[t], 32);
-  const long unit = ((long)split * a.n + n) * a.heads + h;
+  l += __shfl_xor(l, 32);
+  const long part0 = ((((long)n * a.heads + h) * p.row_blocks + rb) * p.splits + split) * F::BQ;   // first row of the partial outputs
+  auto output = [&](int r) -> T* {
+    const int tok = r / a.group, hq = h * a.group + (r - tok * a.group);
+    return (T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head;
+  };
   if constexpr (KW == 1) {
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const int row = row0 + t * 32;
-      if (row >= p.rows) continue;
-      if (p.splits > 1) {
-        if (lk == 0) p.ml[unit * p.rows + row] = make_float2(m[t], l[t]);
-        float* dst = p.part + (unit * p.rows + row) * D + 4 * lk;
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * g) = f32x4{o[t][dt][4 * g], o[t][dt][4 * g + 1], o[t][dt][4 * g + 2], o[t][dt][4 * g + 3]};
-        continue;
-      }
-      const int tok = row / a.group, hq = h * a.group + (row - tok * a.group);
-      T* dst = (T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head;
-      const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
+    if (row >= p.rows) return;
+    if (p.splits > 1) {
+      const long at = part0 + qw * 32 + l32;
+      if (lk == 0) launch.ml[at] = make_float2(m, l);
+      float* dst = launch.part + at * D + 4 * lk;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int at = 32 * dt + 8 * g + 4 * lk;
-          const float v0 = o[t][dt][4 * g] * inv, v1 = o[t][dt][4 * g + 1] * inv, v2 = o[t][dt][4 * g + 2] * inv, v3 = o[t][dt][4 * g + 3] * inv;
-          if (at >= a.d) continue;
-          if constexpr (WIDE) *reinterpret_cast<f32x4*>(dst + at) = f32x4{v0, v1, v2, v3};
-          else *reinterpret_cast<u32x2*>(dst + at) = u32x2{pack2<T>(v0, v1), pack2<T>(v2, v3)};
-        }
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * g) = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+      return;
     }
+    T* dst = output(row);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) store_quad<T>(dst, 32 * dt + 8 * g + 4 * lk, a.d, f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]} * inv);
   } else {
     float* s_o = reinterpret_cast<float*>(smem);                          // [KW][32][RED]
     float2* s_ml = reinterpret_cast<float2*>(s_o + KW * 32 * F::RED);     // [KW][32]
     sync_tiles();
-    if (lk == 0) s_ml[kw * 32 + l32] = make_float2(m[0], l[0]);
+    if (lk == 0) s_ml[kw * 32 + l32] = make_float2(m, l);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(s_o + (kw * 32 + l32) * F::RED + 32 * dt + 8 * g + 4 * lk) = f32x4{o[0][dt][4 * g], o[0][dt][4 * g + 1], o[0][dt][4 * g + 2], o[0][dt][4 * g + 3]};
+        *reinterpret_cast<f32x4*>(s_o + (kw * 32 + l32) * F::RED + 32 * dt + 8 * g + 4 * lk) = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
     sync_lds();
     for (int i = tid; i < 32 * D / 4; i += F::NT) {
-      const int r = i / (D / 4), at = i % (D / 4) * 4, row = rb * 32 + r;
-      if (row >= p.rows || at >= a.d) continue;
+      const int r = i / (D / 4), at = i % (D / 4) * 4;
+      if (rb * 32 + r >= p.rows || at >= a.d) continue;
       float top = s_ml[r].x, den = 0.f;
 #pragma unroll
       for (int w = 1; w < KW; ++w) top = fmaxf(top, s_ml[w * 32 + r].x);
@@ -401,116 +433,117 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float2 e = s_ml[w * 32 + r];
-        const float f = e.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(e.x - top);
+        const float f = weight_of(e.x, top);
         den = fmaf(e.y, f, den);
         num += f * *reinterpret_cast<const f32x4*>(s_o + (w * 32 + r) * F::RED + at);
       }
       if (p.splits > 1) {
-        if (at == 0) p.ml[unit * p.rows + row] = make_float2(top, den);
-        *reinterpret_cast<f32x4*>(p.part + (unit * p.rows + row) * D + at) = num;
-        continue;
+        if (at == 0) launch.ml[part0 + r] = make_float2(top, den);
+        *reinterpret_cast<f32x4*>(launch.part + (part0 + r) * D + at) = num;
+      } else {
+        store_quad<T>(output(rb * 32 + r), at, a.d, num * (den == 0.f ? 0.f : 1.f / den));
       }
-      const int tok = row / a.group, hq = h * a.group + (row - tok * a.group);
-      T* dst = (T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head + at;
-      const float inv = den == 0.f ? 0.f : 1.f / den;
-      if constexpr (WIDE) *reinterpret_cast<f32x4*>(dst) = num * inv;
-      else *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<T>(num[0] * inv, num[1] * inv), pack2<T>(num[2] * inv, num[3] * inv)};
     }
   }
 }
 
-// o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), ranges in index order, eight at a time.  A thread takes four channels of a row.
+// o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) for the rows of the blocks that are split.  A thread takes four channels of a row and every groups-th
+// range, eight at a time; the groups of a row are joined in order.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_combine_kernel(CrossLaunch p) {
-  const CrossArgs& a = p.a;
-  const long i = (long)blockIdx.x * 256 + threadIdx.x, count = (long)a.n * a.heads * p.rows, r = i / (D / 4);
-  const int at = (int)(i % (D / 4)) * 4;
-  if (r >= count || at >= a.d) return;
+__global__ __launch_bounds__(256) void cross_combine_kernel(CrossLaunch launch, int bq, int groups) {
+  constexpr int QUADS = D / 4, UNITS = 256 / QUADS, B = 8;
+  __shared__ f32x4 s_num[UNITS][QUADS];
+  __shared__ float2 s_ml[UNITS];
+  const CrossArgs& a = launch.a;
+  const CrossPlan& p = launch.plan;
+  const int unit = threadIdx.x / QUADS, quad = threadIdx.x % QUADS, g = unit % groups, in_block = UNITS / groups;
+  const long r = (long)blockIdx.x * in_block + unit / groups;                     // row among those of all blocks
+  const long pb = r / bq, nh = pb / p.row_blocks;
+  const int in = (int)(r - pb * bq), n = (int)(nh / a.heads), h = (int)(nh - (long)n * a.heads), row = (int)(pb - nh * p.row_blocks) * bq + in;
+  const bool there = unit < in_block * groups && n < a.n && row < p.rows;
   float top = -INFINITY, den = 0.f;
   f32x4 num{0.f, 0.f, 0.f, 0.f};
-  constexpr int B = 8;
-  for (int s0 = 0; s0 < p.splits; s0 += B) {
-    float2 e[B];
-    f32x4 v[B];
-#pragma unroll
-    for (int b = 0; b < B; ++b) {   // (past the last: the last again, with weight zero)
-      const long s = min(s0 + b, p.splits - 1);
-      e[b] = p.ml[s * count + r];
-      v[b] = *reinterpret_cast<const f32x4*>(p.part + (s * count + r) * D + at);
-    }
-    float now = top;
-#pragma unroll
-    for (int b = 0; b < B; ++b) now = fmaxf(now, e[b].x);
-    const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
-    den *= keep;
-    num *= keep;
+  auto join = [&](float m, float l, f32x4 v) {
+    const float now = fmaxf(top, m), keep = weight_of(top, now), f = weight_of(m, now);
+    den = den * keep + l * f;
+    num = num * keep + v * f;
     top = now;
+  };
+  if (there && quad * 4 < a.d) {
+    for (int s0 = g; s0 < p.splits; s0 += B * groups) {
+      float2 e[B];
+      f32x4 v[B];
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      if (s0 + b >= p.splits) continue;
-      const float f = e[b].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(e[b].x - top);
-      den = fmaf(e[b].y, f, den);
-      num += f * v[b];
+      for (int b = 0; b < B; ++b) {
+        const long at = (pb * p.splits + min(s0 + b * groups, p.splits - 1)) * bq + in;
+        e[b] = launch.ml[at];
+        v[b] = *reinterpret_cast<const f32x4*>(launch.part + at * D + quad * 4);
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        if (s0 + b * groups < p.splits) join(e[b].x, e[b].y, v[b]);
     }
   }
-  const int row = (int)(r % p.rows), h = (int)(r / p.rows % a.heads), n = (int)(r / ((long)p.rows * a.heads));
+  if (groups > 1) {
+    if (unit < UNITS) {
+      s_num[unit][quad] = num;
+      if (quad == 0) s_ml[unit] = make_float2(top, den);
+    }
+    __syncthreads();
+    if (g == 0 && there)
+      for (int i = 1; i < groups; ++i) join(s_ml[unit + i].x, s_ml[unit + i].y, s_num[unit + i][quad]);
+  }
+  if (g != 0 || !there) return;
   const int tok = row / a.group, hq = h * a.group + (row - tok * a.group);
-  T* dst = (T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head + at;
-  const float inv = den == 0.f ? 0.f : 1.f / den;
-  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(dst) = num * inv;
-  else *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<T>(num[0] * inv, num[1] * inv), pack2<T>(num[2] * inv, num[3] * inv)};
+  store_quad<T>((T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head, quad * 4, a.d, num * (den == 0.f ? 0.f : 1.f / den));
 }
 
-// What the kernels of a type are launched with: rows per wavefront, whether wavefronts share rows.
-template <typename T, int D, int QT, int QW, int KW, int KT, int WAVES>
-int cross_launch_form(const CrossLaunch& p, hipStream_t s) {
-  using F = CrossForm<T, D, QT, QW, KW, KT>;
-  auto kern = cross_attention_kernel<T, D, QT, QW, KW, KT, WAVES>;
+template <typename T, int D, int QW, int KW, int KT, int WAVES>
+int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
+  using F = CrossForm<T, D, QW, KW, KT>;
+  auto kern = cross_attention_kernel<T, D, QW, KW, KT, WAVES>;
   static std::once_flag attr_once;
   hipError_t attr_err = hipSuccess;
   std::call_once(attr_once, [&] { attr_err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, F::kSmem); });
   WMDEC_HIP(attr_err);
-  CrossLaunch q = p;
-  q.row_blocks = (p.rows + F::BQ - 1) / F::BQ;
-  hipLaunchKernelGGL(kern, dim3((unsigned)((long)q.row_blocks * q.splits * q.a.n * q.a.heads)), dim3(F::NT), F::kSmem, s, q);
+  const CrossPlan& p = l.plan;
+  const long blocks = (long)l.a.n * l.a.heads * p.row_blocks, rows = blocks * F::BQ;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.splits)), dim3(F::NT), F::kSmem, s, l);
   WMDEC_HIP(hipGetLastError());
   if (p.splits > 1) {
-    const long threads = (long)q.a.n * q.a.heads * q.rows * (D / 4);
-    hipLaunchKernelGGL((cross_combine_kernel<T, D>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, q);
+    constexpr int units = 256 / (D / 4);
+    int groups = 1;   // as many as there are ranges, while rows are fewer than the compute units take at once
+    while (groups * 2 <= units && groups < p.splits && groups < 8 && rows * groups < 4096L * units) groups *= 2;
+    const long in_block = units / groups;
+    hipLaunchKernelGGL((cross_combine_kernel<T, D>), dim3((unsigned)((rows + in_block - 1) / in_block)), dim3(256), 0, s, l, F::BQ, groups);
     WMDEC_HIP(hipGetLastError());
   }
   return WMDEC_OK;
 }
 
+// Keys of a tile, wavefronts a SIMD: what the widest two buffers in 128 KiB allow.
 template <typename T, int D>
-int cross_launch_width(const CrossLaunch& p, bool few, hipStream_t s) {
+int cross_launch_width(const CrossLaunch& l, hipStream_t s) {
   constexpr int bytes = D * (int)sizeof(T);   // of a key
-  constexpr int KT = bytes <= 512 ? 64 : 32;
-  if constexpr (bytes <= 256) {
-    if (few) return cross_launch_form<T, D, 1, 1, 4, 128, 1>(p, s);
-  } else if constexpr (bytes <= 512) {
-    if (few) return cross_launch_form<T, D, 1, 1, 2, 64, 1>(p, s);
+  if constexpr (bytes <= 512) {
+    if (l.plan.few) return cross_launch_form<T, D, 1, 4, 128, (bytes <= 256 ? 2 : 1)>(l, s);
   }
-  if constexpr (sizeof(T) == 2 && D <= 128) {
-    if (p.rows > 128) return cross_launch_form<T, D, 2, 4, 1, KT, (D <= 64 ? 2 : 1)>(p, s);
-  }
-  return cross_launch_form<T, D, 1, 4, 1, KT, (D <= 128 ? 2 : 1)>(p, s);
+  return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (D <= 128 ? 2 : 1)>(l, s);
 }
 
-// few: at most 32 rows
 template <typename T>
-int cross_launch(const CrossLaunch& p, int width, bool few, hipStream_t s) {
-  switch (width) {
-    case 32: return cross_launch_width<T, 32>(p, few, s);
-    case 64: return cross_launch_width<T, 64>(p, few, s);
-    case 96: return cross_launch_width<T, 96>(p, few, s);
-    case 128: return cross_launch_width<T, 128>(p, few, s);
-    case 192: return cross_launch_width<T, 192>(p, few, s);
-    default: return cross_launch_width<T, 256>(p, few, s);
+int cross_launch(const CrossLaunch& l, hipStream_t s) {
+  switch (l.plan.width) {
+    case 32: return cross_launch_width<T, 32>(l, s);
+    case 64: return cross_launch_width<T, 64>(l, s);
+    case 96: return cross_launch_width<T, 96>(l, s);
+    case 128: return cross_launch_width<T, 128>(l, s);
+    case 192: return cross_launch_width<T, 192>(l, s);
+    default: return cross_launch_width<T, 256>(l, s);
   }
 }
-extern template int cross_launch<f16_t>(const CrossLaunch&, int, bool, hipStream_t);
-extern template int cross_launch<bf16_t>(const CrossLaunch&, int, bool, hipStream_t);
-extern template int cross_launch<float>(const CrossLaunch&, int, bool, hipStream_t);
+extern template int cross_launch<f16_t>(const CrossLaunch&, hipStream_t);
+extern template int cross_launch<bf16_t>(const CrossLaunch&, hipStream_t);
+extern template int cross_launch<float>(const CrossLaunch&, hipStream_t);
 
 }  // namespace wmdec

@@ -1,43 +1,50 @@
 // Attention to states of another length: o = softmax(scale * q k^T over the valid keys) v.  The kernels are in cross_device.hpp; here is what is decided on
 // sizes alone, and the f16 kernels.
+#include <algorithm>
+
 #include "cross_device.hpp"
 
 namespace wmdec {
 
-template int cross_launch<f16_t>(const CrossLaunch&, int, bool, hipStream_t);
+template int cross_launch<f16_t>(const CrossLaunch&, hipStream_t);
 
 namespace {
 
-// channels of a head that the kernels are made for
-int width_of(int d) { return d <= 128 ? (d + 31) / 32 * 32 : d <= 192 ? 192 : 256; }
-
-// Ranges of keys of a row: workgroups for every compute unit twice, of 256 keys at least.  Independent of the batch, so that the bits of a sample are.
-int splits_of(int tk, int heads, long rows) {
-  const long units = heads * (rows <= 32 ? 1 : (rows + 127) / 128);
-  const long want = (512 + units - 1) / units, most = tk / 256;
-  return (int)max(1L, min(min(want, most), (long)kCrossMaxSplits));
+// Nothing here looks at the number of samples, so that the bits of a sample do not depend on what it is batched with.
+CrossPlan plan_of(int dtype, int tk, int tq, int heads, int group, int d) {
+  CrossPlan p;
+  p.width = d <= 128 ? (d + 31) / 32 * 32 : d <= 192 ? 192 : 256;
+  p.rows = tq * group;
+  const int bytes = p.width * (int)dtype_size(dtype);   // of a key
+  auto blocks = [&](int bq) { return (long)heads * ((p.rows + bq - 1) / bq); };
+  // Few rows: the wavefronts of a workgroup share 32 rows and take a part of the keys each; so do those of more rows that would not give work to all.
+  p.few = bytes <= 512 && (p.rows <= 32 || blocks(128) <= 64);
+  const int bq = p.few ? 32 : 128;
+  p.row_blocks = (p.rows + bq - 1) / bq;
+  // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow).
+  const int tiles = p.few ? 128 * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
+  const int slots = 256 * std::min(160 * 1024 / (tiles + 4096), !p.few && p.width <= 64 ? 4 : 2);
+  p.splits = (int)std::max(1L, std::min({slots / blocks(bq), tk / 256L, (long)kCrossMaxSplits}));
+  return p;
 }
+
+size_t part_rows(const CrossPlan& p, int n, int heads) { return p.splits == 1 ? 0 : (size_t)n * heads * p.row_blocks * p.splits * (p.few ? 32 : 128); }
 
 }  // namespace
 
 size_t cross_attention_scratch_bytes(int dtype, int tk, int n, int tq, int heads, int group, int d) {
-  const long rows = (long)tq * group;
-  const int splits = splits_of(tk, heads, rows);
-  return splits == 1 ? 0 : (size_t)splits * n * heads * rows * (width_of(d) + 2) * sizeof(float);
+  const CrossPlan p = plan_of(dtype, tk, tq, heads, group, d);
+  return part_rows(p, n, heads) * (p.width + 2) * sizeof(float);
 }
 
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s) {
-  CrossLaunch p;
-  p.a = a;
-  p.rows = a.tq * a.group;
-  p.row_blocks = 0;
-  p.splits = splits_of(a.tk, a.heads, p.rows);
-  const int width = width_of(a.d);
-  p.part = (float*)a.scratch;
-  p.ml = (float2*)(p.part + (size_t)p.splits * a.n * a.heads * p.rows * width);
-  const bool few = p.rows <= 32;
-  if (dtype == WMDEC_F32) return cross_launch<float>(p, width, few, s);
-  return dtype == WMDEC_BF16 ? cross_launch<bf16_t>(p, width, few, s) : cross_launch<f16_t>(p, width, few, s);
+  CrossLaunch l;
+  l.a = a;
+  l.plan = plan_of(dtype, a.tk, a.tq, a.heads, a.group, a.d);
+  l.part = (float*)a.scratch;
+  l.ml = (float2*)(l.part + part_rows(l.plan, a.n, a.heads) * l.plan.width);
+  if (dtype == WMDEC_F32) return cross_launch<float>(l, s);
+  return dtype == WMDEC_BF16 ? cross_launch<bf16_t>(l, s) : cross_launch<f16_t>(l, s);
 }
 
 }  // namespace wmdec

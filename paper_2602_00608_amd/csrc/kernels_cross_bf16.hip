@@ -2,5 +2,5 @@
 #include "cross_device.hpp"
 
 namespace wmdec {
-template int cross_launch<bf16_t>(const CrossLaunch&, int, bool, hipStream_t);
+template int cross_launch<bf16_t>(const CrossLaunch&, hipStream_t);
 }  // namespace wmdec
