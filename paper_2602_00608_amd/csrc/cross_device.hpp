@@ -140,6 +140,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
 
   // ---- queries: chunk 2 s + lk of the lane's row
   const int row = rb * F::BQ + qw * 32 + l32;
+  const bool idle = rb * F::BQ + qw * 32 >= p.rows;   // a wavefront past the last row only loads
   u32x4 q[QS];
   {
     const int r = min(row, p.rows - 1), tok = r / a.group, hq = h * a.group + (r - tok * a.group);
@@ -378,6 +379,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         valid(j, bits);
         if (none) continue;
         if (mask && !all) { clear(tv, bits); sync_lds(); }
+        if (idle) continue;
         scores(tk, bits);
         values_head(tv);
         softmax();
