@@ -834,7 +834,7 @@ int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype
   WMDEC_REQUIRE(x_dtype == act_dtype || x_dtype == WMDEC_F32, WMDEC_ERR_UNSUPPORTED, "%s: x_dtype must be act_dtype or F32", who);
   WMDEC_REQUIRE(n > 0 && t > 0 && d > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
   WMDEC_REQUIRE(d <= kResidualNormMaxD, WMDEC_ERR_UNSUPPORTED, "%s: d %d above the limit of %d", who, d, kResidualNormMaxD);
-  WMDEC_REQUIRE((long)n * t <= (1L << 31) - 1, WMDEC_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows", who);
+  WMDEC_REQUIRE((long)n * t <= (1L << 31) - (1L << 20), WMDEC_ERR_UNSUPPORTED, "%s: more than 2^31 - 2^20 rows", who);
   WMDEC_REQUIRE(!h || x_out, WMDEC_ERR_INVALID_ARG, "%s: h given without x_out", who);
   ResidualNormArgs a;
   int rc = check_norm(who, post, &a.post);
@@ -918,8 +918,8 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
   if (rc == WMDEC_OK && k) rc = check_rope_tensor(who, k, k_strides, k_out, k_out_strides, heads_k, dtype_size(dtype), n, t, &a.k);
   if (rc != WMDEC_OK) return rc;
   WMDEC_REQUIRE(a.rot <= d, WMDEC_ERR_SHAPE, "%s: %d rotated channels in a head of %d", who, a.rot, d);
-  WMDEC_REQUIRE((long)n * t <= (1L << 31) - 1 && d <= kRopeMaxD && (long)a.q.heads + a.k.heads <= kRopeMaxHeads, WMDEC_ERR_UNSUPPORTED,
-                "%s: more than 2^31 - 1 tokens, %d heads or %d channels", who, kRopeMaxHeads, kRopeMaxD);
+  WMDEC_REQUIRE((long)n * t <= (1L << 31) - (1L << 20) && d <= kRopeMaxD && (long)a.q.heads + a.k.heads <= kRopeMaxHeads, WMDEC_ERR_UNSUPPORTED,
+                "%s: more than 2^31 - 2^20 tokens, %d heads or %d channels", who, kRopeMaxHeads, kRopeMaxD);
   WMDEC_REQUIRE(q_out != k_out && q_out != k && k_out != q, WMDEC_ERR_INVALID_ARG, "%s: an output may be its own input, nothing else may overlap", who);
   WMDEC_REQUIRE(isfinite(layout->magnitude), WMDEC_ERR_INVALID_ARG, "%s: magnitude must be finite", who);
   WMDEC_REQUIRE(element_aligned(positions, 4) && element_aligned(freq, 8), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);

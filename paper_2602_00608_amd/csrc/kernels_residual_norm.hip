@@ -4,8 +4,12 @@
 // norms' weights and biases: up to seven times four bytes a channel, more than a row of 16-bit tensors has) would be read again for every row, so a
 // thread owns eight channels of many rows and keeps what they come to in registers, two multiply-adds an element:
 //   x' = x + ((h - mean) * rstd) * ga + gb,   ga = s * g * w, gb = s * g * u;     y = ((x' - mean) * rstd) * ya + yb,   ya = w (1 + c), yb = u (1 + c) + b.
-// A row is 8 to 64 lanes of a wavefront (up to 512 channels), or whole wavefronts of a workgroup; the next rows are requested before the present ones
-// are reduced.  Moments: mean and squares about it over the values of a wavefront, joined over the wavefronts (Chan, Golub, LeVeque) behind one barrier a norm.
+// A row is 8 to 64 lanes of a wavefront (up to 512 channels), or whole wavefronts of a workgroup; the next row is requested before the present one
+// is reduced.  Moments: mean and squares about it over the values of a wavefront, joined over the wavefronts (Chan, Golub, LeVeque) behind one barrier a norm.
+// us on inputs from memory, with the rate: 2x5400 rows of 1920 in bf16 38.1 (4.36 TB/s), 4x5400 rows of 1152, fp32 beside f16, 62.7 (4.76; a copy of 4 GiB 4.89).
+// Steps: a row a workgroup 318 and 405; this form with ranges of rows, two rows at a time, in 1.3 rounds of workgroups 50.5 and 84.2; one round 42.7 and 71.0; a row at
+// a time 40.8 and 68.6; the workgroups' rows side by side, so that what is under way lies together in memory, 38.1 and 62.7.  Measured and not kept: two and
+// eight rounds of workgroups (39.8 and 69.4, 50.4 and 72.3), stores or loads that pass the caches by (42.1 and 72.4, 44.9 and 74.6).
 #include "conv_device.hpp"
 
 namespace wmdec {
@@ -16,7 +20,7 @@ constexpr int E = 8;               // channels of a vector
 
 struct Params {
   ResidualNormArgs a;
-  int tpr, segs;   // threads of a row, ranges of rows of a sample
+  int tpr, segs;   // threads of a row, workgroups of a sample
 };
 
 // A thread's eight channels of a vector are consecutive where rows are aligned; where they are not, they are `gap` apart, so that the lanes of every load and
@@ -62,15 +66,15 @@ template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long
   }
 }
 
-// VPT vectors a thread, R rows at once
-template <typename TX, typename TA, int VPT, int R, bool VEC>
+// VPT vectors a thread
+template <typename TX, typename TA, int VPT, bool VEC>
 __global__ __launch_bounds__(kMaxThreads, VPT == 1 && VEC ? 4 : 2) void residual_norm_kernel(Params p) {
-  __shared__ float4 s_red[2][2][R][kMaxThreads / 64];
+  __shared__ float4 s_red[2][2][kMaxThreads / 64];
   const ResidualNormArgs& a = p.a;
   const int d = a.d, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int groups = p.tpr < 64 ? (int)blockDim.x / p.tpr : 1, group = p.tpr < 64 ? tid / p.tpr : 0, lane = p.tpr < 64 ? tid % p.tpr : tid;
   const int n = blockIdx.x / p.segs, seg = blockIdx.x % p.segs;
-  const int row0 = (int)((long)a.t * seg / p.segs), row1 = (int)((long)a.t * (seg + 1) / p.segs);
+  const int row0 = seg * groups, step = p.segs * groups;   // (workgroups side by side: the rows under way at a time are next to each other in memory)
   const bool has_h = a.h != nullptr, has_y = a.y != nullptr;
   const int gap = min(p.tpr, 64);
   int col[VPT], count[VPT];
@@ -86,21 +90,18 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 && VEC ? 4 : 2) void residual
   TX* x_out = (TX*)a.x_out + (has_h ? (long)n * a.t * d : 0);
   TA* y = (TA*)a.y + (has_y ? (long)n * a.t * d : 0);
 
-  TX rx[R][VPT][E];
-  TA rh[R][VPT][E];
-  auto ask = [&](int first) {             // rows past the range: the last one again, not stored
+  TX rx[VPT][E];
+  TA rh[VPT][E];
+  auto ask = [&](int first) {             // past the last row: that one again, not stored
+    const long at = (long)min(first + group, a.t - 1) * d;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const long at = (long)min(first + r * groups + group, row1 - 1) * d;
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        load8<TX, VEC>(x + at + col[i], count[i], gap, rx[r][i]);
-        if (has_h) load8<TA, VEC>(h + at + col[i], count[i], gap, rh[r][i]);
-      }
+    for (int i = 0; i < VPT; ++i) {
+      load8<TX, VEC>(x + at + col[i], count[i], gap, rx[i]);
+      if (has_h) load8<TA, VEC>(h + at + col[i], count[i], gap, rh[i]);
     }
   };
   constexpr bool AHEAD = VPT < 4;         // (four vectors a thread leave no registers for the next rows)
-  if (AHEAD && row0 < row1) ask(row0);
+  if (AHEAD) ask(row0);
   __builtin_amdgcn_sched_barrier(0);
 
   float ga[VPT][E], gb[VPT][E], ya[VPT][E], yb[VPT][E];
@@ -135,123 +136,98 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 && VEC ? 4 : 2) void residual
     if (p.tpr > 32) v = swap_sum<32>(v);
     return v;
   };
-  // mean and 1 / sqrt(variance + eps) of the R rows; RMS: the mean is zero
-  auto statistics = [&](const wmdec_norm& norm, const float (&v)[R][VPT][E], int which, int parity, float (&mean)[R], float (&rstd)[R]) {
-    const bool layer = norm.kind == WMDEC_NORM_LAYER;
-    const float inv = p.tpr > 64 ? __builtin_amdgcn_rcpf(fmaxf(held, 1.f)) : inv_d;
-    float m2[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      mean[r] = 0.f;
-      if (layer) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-#pragma unroll
-          for (int e = 0; e < E; ++e) sum += v[r][i][e];
-        mean[r] = row_sum(sum) * inv;
-      }
-      float sq = 0.f;
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        float part = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float dev = v[r][i][e] - mean[r];
-          part = VEC || e < count[i] ? fmaf(dev, dev, part) : part;
-        }
-        sq += VEC && count[i] == 0 ? 0.f : part;
-      }
-      m2[r] = row_sum(sq);
-    }
-    if (p.tpr > 64) {
-      if ((tid & 63) == 0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) s_red[parity][which][r][wave] = make_float4(mean[r], m2[r], held, 0.f);
-      }
-      __syncthreads();
-      const int waves = blockDim.x >> 6;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float sum = 0.f, sq = 0.f;
-        for (int w = 0; w < waves; ++w) { const float4 q = s_red[parity][which][r][w]; sum = fmaf(q.x, q.z, sum); }
-        mean[r] = sum * inv_d;
-        for (int w = 0; w < waves; ++w) { const float4 q = s_red[parity][which][r][w]; sq += fmaf(q.z * (q.x - mean[r]), q.x - mean[r], q.y); }
-        m2[r] = sq;
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) rstd[r] = __builtin_amdgcn_rsqf(fmaf(m2[r], inv_d, norm.eps));
-  };
-
-  int parity = 0;
-  for (int first = row0; first < row1; first += R * groups, parity ^= 1) {
-    if (!AHEAD) ask(first);
-    float v[R][VPT][E], b[R][VPT][E];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
+  // mean and 1 / sqrt(variance + eps) of the row; RMS: the mean is zero
+  auto statistics = [&](const wmdec_norm& norm, const float (&v)[VPT][E], int which, int parity, float& mean, float& rstd) {
+    mean = 0.f;
+    if (norm.kind == WMDEC_NORM_LAYER) {
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          v[r][i][e] = to_float(rx[r][i][e]);
-          if (has_h) b[r][i][e] = to_float(rh[r][i][e]);
-        }
-    if (AHEAD && first + R * groups < row1) ask(first + R * groups);
+        for (int e = 0; e < E; ++e) sum += v[i][e];
+      mean = row_sum(sum) * (p.tpr > 64 ? __builtin_amdgcn_rcpf(fmaxf(held, 1.f)) : inv_d);
+    }
+    float m2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float part = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float dev = v[i][e] - mean;
+        part = VEC || e < count[i] ? fmaf(dev, dev, part) : part;
+      }
+      m2 += VEC && count[i] == 0 ? 0.f : part;
+    }
+    m2 = row_sum(m2);
+    if (p.tpr > 64) {
+      if ((tid & 63) == 0) s_red[parity][which][wave] = make_float4(mean, m2, held, 0.f);
+      __syncthreads();
+      const int waves = blockDim.x >> 6;
+      float sum = 0.f;
+      for (int w = 0; w < waves; ++w) { const float4 q = s_red[parity][which][w]; sum = fmaf(q.x, q.z, sum); }
+      mean = sum * inv_d;
+      m2 = 0.f;
+      for (int w = 0; w < waves; ++w) { const float4 q = s_red[parity][which][w]; m2 += fmaf(q.z * (q.x - mean), q.x - mean, q.y); }
+    }
+    rstd = __builtin_amdgcn_rsqf(fmaf(m2, inv_d, norm.eps));
+  };
+
+  int parity = 0;
+  for (int first = row0; first < a.t; first += step, parity ^= 1) {
+    if (!AHEAD) ask(first);
+    float v[VPT][E], b[VPT][E];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[i][e] = to_float(rx[i][e]);
+        if (has_h) b[i][e] = to_float(rh[i][e]);
+      }
+    if (AHEAD && first + step < a.t) ask(first + step);
     __builtin_amdgcn_sched_barrier(0);
-    float mean[R], rstd[R];
+    const int row = first + group;
+    const long at = (long)row * d;
+    float mean, rstd;
     if (has_h) {
       if (a.post.kind != WMDEC_NORM_NONE) {
         statistics(a.post, b, 0, parity, mean, rstd);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int i = 0; i < VPT; ++i)
 #pragma unroll
-          for (int i = 0; i < VPT; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) b[r][i][e] = (b[r][i][e] - mean[r]) * rstd[r];
+          for (int e = 0; e < E; ++e) b[i][e] = (b[i][e] - mean) * rstd;
       }
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int row = first + r * groups + group;
+      for (int i = 0; i < VPT; ++i) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[r][i][e] = round_through<TX>(v[r][i][e] + fmaf(b[r][i][e], ga[i][e], gb[i][e]));   // (what is stored is what is normalised)
-          if (row < row1) store8<TX, VEC>(x_out + (long)row * d + col[i], count[i], gap, v[r][i]);
-        }
+        for (int e = 0; e < E; ++e) v[i][e] = round_through<TX>(v[i][e] + fmaf(b[i][e], ga[i][e], gb[i][e]));   // (what is stored is what is normalised)
+        if (row < a.t) store8<TX, VEC>(x_out + at + col[i], count[i], gap, v[i]);
       }
     }
     if (!has_y) continue;
     if (a.pre.kind != WMDEC_NORM_NONE) {
       statistics(a.pre, v, 1, parity, mean, rstd);
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+      for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[r][i][e] = (v[r][i][e] - mean[r]) * rstd[r];
+        for (int e = 0; e < E; ++e) v[i][e] = (v[i][e] - mean) * rstd;
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int row = first + r * groups + group;
+    for (int i = 0; i < VPT; ++i) {
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[r][i][e] = fmaf(v[r][i][e], ya[i][e], yb[i][e]);
-        if (row < row1) store8<TA, VEC>(y + (long)row * d + col[i], count[i], gap, v[r][i]);
-      }
+      for (int e = 0; e < E; ++e) v[i][e] = fmaf(v[i][e], ya[i][e], yb[i][e]);
+      if (row < a.t) store8<TA, VEC>(y + at + col[i], count[i], gap, v[i]);
     }
   }
 }
 
-template <typename TX, typename TA, int VPT, int R, bool VEC>
+template <typename TX, typename TA, int VPT, bool VEC>
 int launch_form(const ResidualNormArgs& a, int tpr, int threads, hipStream_t s) {
   Params p{a, tpr, 1};
   const int groups = tpr < 64 ? threads / tpr : 1;
-  const int most = (a.t + groups * R - 1) / (groups * R), waves = VPT == 1 && VEC ? 16 : 8;   // wavefronts of a compute unit
+  const int most = (a.t + groups - 1) / groups, waves = VPT == 1 && VEC ? 16 : 8;   // wavefronts of a compute unit
   const int target = 256 * (waves / (threads / 64)) / a.n;   // all workgroups at once: those of a second round would run alone
   p.segs = max(1, min(most, target));
-  hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, R, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);
+  hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);
   WMDEC_HIP(hipGetLastError());
   return WMDEC_OK;
 }
@@ -261,13 +237,13 @@ int launch_width(const ResidualNormArgs& a, hipStream_t s) {
   const int vectors = (a.d + E - 1) / E;
   int tpr = 8;
   while (tpr < 64 && tpr < vectors) tpr *= 2;
-  if (vectors <= 64) return launch_form<TX, TA, 1, 2, VEC>(a, tpr, 256, s);
-  if (vectors <= kMaxThreads) return launch_form<TX, TA, 1, 2, VEC>(a, (vectors + 63) / 64 * 64, (vectors + 63) / 64 * 64, s);
+  if (vectors <= 64) return launch_form<TX, TA, 1, VEC>(a, tpr, 256, s);
+  if (vectors <= kMaxThreads) return launch_form<TX, TA, 1, VEC>(a, (vectors + 63) / 64 * 64, (vectors + 63) / 64 * 64, s);
   tpr = ((vectors + 1) / 2 + 63) / 64 * 64;
-  if (tpr <= kMaxThreads) return launch_form<TX, TA, 2, 1, VEC>(a, tpr, tpr, s);
+  if (tpr <= kMaxThreads) return launch_form<TX, TA, 2, VEC>(a, tpr, tpr, s);
   tpr = ((vectors + 3) / 4 + 63) / 64 * 64;
   static_assert(4 * kMaxThreads * E == kResidualNormMaxD, "four vectors a thread hold the widest row");
-  return launch_form<TX, TA, 4, 1, VEC>(a, tpr, tpr, s);
+  return launch_form<TX, TA, 4, VEC>(a, tpr, tpr, s);
 }
 
 template <typename TX, typename TA>

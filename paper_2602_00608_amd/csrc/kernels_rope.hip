@@ -2,6 +2,9 @@
 //
 // Bound by HBM: q and k are read and written once.  An angle belongs to a token and a pair, not to a head: it is worked out once for all heads (in 64 bits,
 // as positions times frequencies pass what fp32 resolves), and what is left an element is a multiplication and a multiply-add.
+// us on inputs from memory, with the rate: 2x5400 tokens of 30 + 30 heads of 64 in bf16 38.1 (4.36 TB/s; a copy of as many bytes 32.6), 16385 tokens of
+// 32 + 8 heads of 128 in f16 70.1 (4.79).  Steps: a thread a pair 139 and 350; angles through LDS and vectors of eight channels, four of them at a time 48.9 and
+// 77.4; workgroups side by side in memory, where a token's q and k are from LDS, one unit on its way behind the other 38.1 and 72.6.
 #include <algorithm>
 
 #include "mfma.hpp"
@@ -10,6 +13,7 @@ namespace wmdec {
 namespace {
 
 constexpr int NT = 256;
+constexpr int kMaxTokens = 256, kMaxAngles = 2048;   // of a workgroup
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 struct FreqParams { double* freq; int axes; int dim[3]; wmdec_rope_scaling sc; };
@@ -64,36 +68,44 @@ template <typename T, int W> __device__ __forceinline__ void store(T* p, const V
   }
 }
 
-// Work of a workgroup: `tokens` consecutive tokens, all heads.  Its angles are worked out once, a thread each, into LDS; then the threads walk over
-// (token, head, unit).  A unit is two vectors of W channels (or one channel and its partner): of the rotated part W / 2 or W pairs, else copied.
+// Work of a workgroup: `tokens` tokens, all heads.  Its angles are worked out once, a thread each, into LDS; then the threads walk over
+// (token, head, unit).  The tokens of a workgroup are as far apart as there are workgroups, so that what is under way at a time lies together in memory.  A unit is two vectors of W channels (or one channel and its partner): of the rotated part W / 2 or W pairs, else copied.
 struct Params {
   RopeArgs a;
   int tokens;                       // of a workgroup
   int pairs, rotated, units;        // pairs of a head, units of them, units of a head
   int du, dh, dt;                   // NT = (dt * heads + dh) * units + du: a thread's step
-  int split;                        // workgroups that share a range of tokens, each with every split-th step
+  int groups, split;                // ranges of tokens, workgroups that share one, each with every split-th step
   long total;                       // tokens of all samples
 };
 
 template <typename T, int W, bool INTERLEAVED>
 __global__ __launch_bounds__(NT) void rope_kernel(Params p) {
   extern __shared__ __align__(16) float2 s_turn[];   // [tokens][pairs] cosine, sine
+  struct Places { const T* in; T* out; };
+  __shared__ Places s_place[kMaxTokens][2];          // where a token's q and k are
   const RopeArgs& a = p.a;
   const int heads = a.q.heads + a.k.heads, tid = threadIdx.x;
-  const long first = (long)(blockIdx.x / p.split) * p.tokens;
-  const int count = (int)min((long)p.tokens, p.total - first), part = blockIdx.x % p.split;
-  const int n0 = (int)(first / a.t), t0 = (int)(first - (long)n0 * a.t);
-  auto sample_of = [&](int i, int& n, int& t) {      // of the i-th token of the workgroup
-    n = n0; t = t0 + i;
-    if (t >= a.t) { n += t / a.t; t %= a.t; }
+  const int first = blockIdx.x / p.split, part = blockIdx.x % p.split;
+  const int count = (int)((p.total - first + p.groups - 1) / p.groups);   // tokens first, first + groups, ...
+  auto token_of = [&](int i, int& n, int& t) {
+    const int token = first + i * p.groups;          // (below 2^31: checked on the host)
+    n = token / a.t; t = token - n * a.t;
   };
+  for (int i = tid; i < 2 * count; i += NT) {
+    const RopeTensor& x = i & 1 ? a.k : a.q;
+    int n, t;
+    token_of(i / 2, n, t);
+    s_place[i / 2][i & 1] = Places{(const T*)x.in + n * x.si.sample + t * x.si.token, (T*)x.out + n * x.so.sample + t * x.so.token};
+  }
+  __syncthreads();
 
-  struct Place { int u, h, t; };
-  auto advance = [&](Place& w, int du, int dh, int dt) {
-    w.u += du; w.h += dh; w.t += dt;
-    if (w.u >= p.units) { w.u -= p.units; ++w.h; }
-    if (w.h >= heads) { w.h -= heads; ++w.t; }
-  };
+  struct Unit { Vec<T, W> v[2]; T* out; const float2* turn; int c0, c1; bool live; };   // turn: null for channels that are copied
+  int wu, wh, wt;                                    // the next unit, its head, its token
+  {
+    const int i = part * NT + tid, hu = heads * p.units;
+    wt = i / hu; wh = (i - wt * hu) / p.units; wu = i - wt * hu - wh * p.units;
+  }
   // where the two vectors of a unit are; both the same channel where there is no second one
   auto channels = [&](int u, int& c0, int& c1) {
     if (u >= p.rotated) { c0 = a.rot + (u - p.rotated) * 2 * W; c1 = c0 + W < a.d ? c0 + W : c0; return; }
@@ -102,85 +114,66 @@ __global__ __launch_bounds__(NT) void rope_kernel(Params p) {
     while (j >= a.layout.axis_dim[axis] / 2) { at += a.layout.axis_dim[axis]; j -= a.layout.axis_dim[axis++] / 2; }
     c0 = at + j; c1 = c0 + a.layout.axis_dim[axis] / 2;
   };
-  auto address = [&](const Place& w, const T*& in, T*& out) {
-    int n, t;
-    sample_of(w.t, n, t);
-    const bool second = w.h >= a.q.heads;
-    const int h = second ? w.h - a.q.heads : w.h;
-    const wmdec_strides &si = second ? a.k.si : a.q.si, &so = second ? a.k.so : a.q.so;
-    in = (const T*)(second ? a.k.in : a.q.in) + n * si.sample + t * si.token + h * si.head;
-    out = (T*)(second ? a.k.out : a.q.out) + n * so.sample + t * so.token + h * so.head;
-  };
-  constexpr int U = 4;              // steps in flight
-  Place w{0, 0, 0};
-  {
-    const int i = part * NT + tid, hu = heads * p.units;
-    w.t = i / hu; w.h = (i - w.t * hu) / p.units; w.u = i - w.t * hu - w.h * p.units;
-  }
-  Vec<T, W> v[U][2];
-  Place at[U];
-  auto ask = [&]() {
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      at[i] = w;
-      if (w.t < count) {
-        const T* in; T* out; int c0, c1;
-        address(w, in, out); channels(w.u, c0, c1);
-        v[i][0] = load<T, W>(in + c0);
-        v[i][1] = load<T, W>(in + c1);
-      }
-      advance(w, p.du, p.dh, p.dt);
+  auto ask = [&](Unit& x) {
+    x.live = wt < count;
+    if (x.live) {
+      const bool second = wh >= a.q.heads;
+      const Places at = s_place[wt][second];
+      const int h = second ? wh - a.q.heads : wh;
+      channels(wu, x.c0, x.c1);
+      const T* in = at.in + h * (second ? a.k.si.head : a.q.si.head);
+      x.out = at.out + h * (second ? a.k.so.head : a.q.so.head);
+      x.turn = wu < p.rotated ? s_turn + wt * p.pairs + wu * W : nullptr;
+      x.v[0] = load<T, W>(in + x.c0);
+      x.v[1] = load<T, W>(in + x.c1);
     }
+    wu += p.du; wh += p.dh; wt += p.dt;
+    if (wu >= p.units) { wu -= p.units; ++wh; }
+    if (wh >= heads) { wh -= heads; ++wt; }
   };
-  ask();
+  auto finish = [&](Unit& x) {
+    Vec<T, W> &o0 = x.v[0], &o1 = x.v[1];
+    if (x.turn) {
+      if constexpr (INTERLEAVED && W > 1) {        // (the second vector has its pairs behind the first one's; where there is none they are not used)
+#pragma unroll
+        for (int e = 0; e < 2 * W; e += 2) {
+          Vec<T, W>& o = e < W ? o0 : o1;
+          const float2 c = x.turn[e / 2 < W / 2 || x.c1 != x.c0 ? e / 2 : 0];
+          const float v = to_float(o.v[e % W]), w = to_float(o.v[e % W + 1]);
+          o.v[e % W] = from_float<T>(v * c.x - w * c.y);
+          o.v[e % W + 1] = from_float<T>(v * c.y + w * c.x);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          const float2 c = x.turn[e];
+          const float v = to_float(o0.v[e]), w = to_float(o1.v[e]);
+          o0.v[e] = from_float<T>(v * c.x - w * c.y);
+          o1.v[e] = from_float<T>(v * c.y + w * c.x);
+        }
+      }
+    }
+    store<T, W>(x.out + x.c0, o0);
+    if (x.c1 != x.c0) store<T, W>(x.out + x.c1, o1);
+  };
+  Unit s0, s1;                      // one travels while the other is worked on
+  ask(s0);
   for (int i = tid; i < count * p.pairs; i += NT) {
     const int t = i / p.pairs, u = i - t * p.pairs;
-    int axis = 0, j = u;
+    int axis = 0, j = u, n, row;
     while (j >= a.layout.axis_dim[axis] / 2) j -= a.layout.axis_dim[axis++] / 2;
-    int n, row;
-    sample_of(t, n, row);
-    const long pos = n * a.positions_stride + (long)row * a.layout.axes + axis;
-    float2 sc = sin_cos((double)a.positions[pos] * a.freq[u]);
+    token_of(t, n, row);
+    float2 sc = sin_cos((double)a.positions[n * a.positions_stride + (long)row * a.layout.axes + axis] * a.freq[u]);
     if (a.layout.inverse) sc.x = -sc.x;
     s_turn[i] = make_float2(sc.y * a.layout.magnitude, sc.x * a.layout.magnitude);
   }
   __syncthreads();
-  while (true) {
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (at[i].t >= count) continue;
-      const T* in; T* out; int c0, c1;
-      address(at[i], in, out); channels(at[i].u, c0, c1);
-      Vec<T, W> o0 = v[i][0], o1 = v[i][1];
-      if (at[i].u < p.rotated) {
-        const float2* turn = s_turn + at[i].t * p.pairs;
-        if constexpr (INTERLEAVED && W > 1) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            Vec<T, W>& o = half ? o1 : o0;
-#pragma unroll
-            for (int e = 0; e < W; e += 2) {
-              const float2 c = turn[(half ? c1 : c0) / 2 + e / 2];
-              const float x = to_float(o.v[e]), y = to_float(o.v[e + 1]);
-              o.v[e] = from_float<T>(x * c.x - y * c.y);
-              o.v[e + 1] = from_float<T>(x * c.y + y * c.x);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < W; ++e) {
-            const float2 c = turn[at[i].u * W + e];
-            const float x = to_float(o0.v[e]), y = to_float(o1.v[e]);
-            o0.v[e] = from_float<T>(x * c.x - y * c.y);
-            o1.v[e] = from_float<T>(x * c.y + y * c.x);
-          }
-        }
-      }
-      store<T, W>(out + c0, o0);
-      if (c1 != c0) store<T, W>(out + c1, o1);
-    }
-    if (w.t >= count) break;        // (steps go upwards)
-    ask();
+  while (s0.live) {                 // (units go upwards: where one is past the end, all that follow are)
+    ask(s1);
+    finish(s0);
+    if (!s1.live) break;
+    ask(s0);
+    finish(s1);
   }
 }
 
@@ -193,11 +186,11 @@ int launch_form(const RopeArgs& a, hipStream_t s) {
   p.units = p.rotated + (a.d - a.rot + 2 * W - 1) / (2 * W);
   p.total = (long)a.n * a.t;
   const long per_token = (long)(a.q.heads + a.k.heads) * p.units;
-  // Tokens of a workgroup: an angle for every thread, or 16 steps of work where that is less, and workgroups for all compute units; few tokens with much work
-  // are shared.
-  const long fill = std::max(1L, (p.total + 1023) / 1024), angles = std::max(1, NT / p.pairs), steps = std::max(1L, 16L * NT / per_token);
-  p.tokens = (int)std::min(fill, std::max(1L, std::min(angles, steps)));
+  // 4096 workgroups where there are as many tokens (1024, one round of them: 16385 tokens of 40 heads of 128 72.6 us against 70.1, 2x5400 of 60 of 64 the same);
+  // few tokens with much work are shared.
+  p.tokens = (int)std::min((p.total + 4095) / 4096, std::max(1L, std::min((long)kMaxAngles / p.pairs, (long)kMaxTokens)));
   const long groups = (p.total + p.tokens - 1) / p.tokens, work = (p.tokens * per_token + NT - 1) / NT;
+  p.groups = (int)groups;
   p.split = (int)std::max(1L, std::min(work, 1024 / groups));
   const long step = (long)NT * p.split;
   p.du = (int)(step % p.units); p.dh = (int)(step / p.units % (a.q.heads + a.k.heads)); p.dt = (int)(step / per_token);
