@@ -527,8 +527,8 @@ int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
 template <typename T, int D>
 int cross_launch_width(const CrossLaunch& l, hipStream_t s) {
   constexpr int bytes = D * (int)sizeof(T);   // of a key
-  if constexpr (bytes <= 512) {
-    if (l.plan.few) return cross_launch_form<T, D, 1, 4, 128, (bytes <= 256 ? 2 : 1)>(l, s);
+  if constexpr (bytes <= 768) {
+    if (l.plan.few) return cross_launch_form<T, D, 1, (bytes <= 512 ? 4 : 2), (bytes <= 512 ? 128 : 64), (bytes <= 256 ? 2 : 1)>(l, s);
   }
   return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (D <= 128 ? 2 : 1)>(l, s);
 }

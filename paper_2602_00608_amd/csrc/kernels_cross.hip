@@ -18,13 +18,14 @@ CrossPlan plan_of(int dtype, int tk, int tq, int heads, int group, int d) {
   const int bytes = p.width * (int)dtype_size(dtype);   // of a key
   auto blocks = [&](int bq) { return (long)heads * ((p.rows + bq - 1) / bq); };
   // Few rows: the wavefronts of a workgroup share 32 rows and take a part of the keys each; so do those of more rows that would not give work to all.
-  p.few = bytes <= 512 && (p.rows <= 32 || blocks(128) <= 64);
+  p.few = bytes <= 768 && (p.rows <= 32 || (dtype == WMDEC_F32 && bytes <= 512 && blocks(128) <= 64));
   const int bq = p.few ? 32 : 128;
   p.row_blocks = (p.rows + bq - 1) / bq;
   // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow).
-  const int tiles = p.few ? 128 * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
+  const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
   const int slots = 256 * std::min(160 * 1024 / (tiles + 4096), !p.few && p.width <= 64 ? 4 : 2);
-  p.splits = (int)std::max(1L, std::min({slots / blocks(bq), tk / 256L, (long)kCrossMaxSplits}));
+  const long range = dtype != WMDEC_F32 ? 256 : p.few ? 128 : 64;   // fewest keys of a range
+  p.splits = (int)std::max(1L, std::min({slots / blocks(bq), tk / range, (long)kCrossMaxSplits}));
   return p;
 }
 

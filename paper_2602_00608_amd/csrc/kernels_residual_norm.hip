@@ -68,7 +68,7 @@ template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long
 
 // VPT vectors a thread
 template <typename TX, typename TA, int VPT, bool VEC>
-__global__ __launch_bounds__(kMaxThreads, VPT == 1 && VEC ? 4 : 2) void residual_norm_kernel(Params p) {
+__global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_kernel(Params p) {
   __shared__ float4 s_red[2][2][kMaxThreads / 64];
   const ResidualNormArgs& a = p.a;
   const int d = a.d, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -224,7 +224,7 @@ template <typename TX, typename TA, int VPT, bool VEC>
 int launch_form(const ResidualNormArgs& a, int tpr, int threads, hipStream_t s) {
   Params p{a, tpr, 1};
   const int groups = tpr < 64 ? threads / tpr : 1;
-  const int most = (a.t + groups - 1) / groups, waves = VPT == 1 && VEC ? 16 : 8;   // wavefronts of a compute unit
+  const int most = (a.t + groups - 1) / groups, waves = VPT == 1 ? 16 : 8;   // wavefronts of a compute unit
   const int target = 256 * (waves / (threads / 64)) / a.n;   // all workgroups at once: those of a second round would run alone
   p.segs = max(1, min(most, target));
   hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);

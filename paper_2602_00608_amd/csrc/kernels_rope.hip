@@ -46,27 +46,10 @@ __device__ __forceinline__ float2 sin_cos(double theta) {
   return make_float2(q & 2 ? -s : s, (q + 1) & 2 ? -c : c);
 }
 
-template <typename T, int W> struct Vec { T v[W]; };
-template <typename T, int W> __device__ __forceinline__ Vec<T, W> load(const T* p) {
-  Vec<T, W> r;
-  if constexpr (W == 1) r.v[0] = *p;
-  else {
-    u32x4 q[sizeof(T) * W / 16];
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) * W / 16); ++i) q[i] = reinterpret_cast<const u32x4*>(p)[i];
-    __builtin_memcpy(&r, &q, sizeof(r));
-  }
-  return r;
-}
-template <typename T, int W> __device__ __forceinline__ void store(T* p, const Vec<T, W>& r) {
-  if constexpr (W == 1) *p = r.v[0];
-  else {
-    u32x4 q[sizeof(T) * W / 16];
-    __builtin_memcpy(&q, &r, sizeof(r));
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) * W / 16); ++i) reinterpret_cast<u32x4*>(p)[i] = q[i];
-  }
-}
+// W channels next to each other, in loads and stores of up to 16 bytes
+template <typename T, int W> struct alignas(sizeof(T) * W < 16 ? sizeof(T) * W : 16) Vec { T v[W]; };
+template <typename T, int W> __device__ __forceinline__ Vec<T, W> load(const T* p) { return *reinterpret_cast<const Vec<T, W>*>(p); }
+template <typename T, int W> __device__ __forceinline__ void store(T* p, const Vec<T, W>& r) { *reinterpret_cast<Vec<T, W>*>(p) = r; }
 
 // Work of a workgroup: `tokens` tokens, all heads.  Its angles are worked out once, a thread each, into LDS; then the threads walk over
 // (token, head, unit).  The tokens of a workgroup are as far apart as there are workgroups, so that what is under way at a time lies together in memory.  A unit is two vectors of W channels (or one channel and its partner): of the rotated part W / 2 or W pairs, else copied.
@@ -186,9 +169,10 @@ int launch_form(const RopeArgs& a, hipStream_t s) {
   p.units = p.rotated + (a.d - a.rot + 2 * W - 1) / (2 * W);
   p.total = (long)a.n * a.t;
   const long per_token = (long)(a.q.heads + a.k.heads) * p.units;
-  // 4096 workgroups where there are as many tokens (1024, one round of them: 16385 tokens of 40 heads of 128 72.6 us against 70.1, 2x5400 of 60 of 64 the same);
-  // few tokens with much work are shared.
-  p.tokens = (int)std::min((p.total + 4095) / 4096, std::max(1L, std::min((long)kMaxAngles / p.pairs, (long)kMaxTokens)));
+  // 4096 workgroups where there are as many tokens (1024, one round of them: 16385 tokens of 40 heads of 128 72.6 us against 70.1, 2x5400 of 60 of 64 the same), but
+  // 1024 while four steps a thread are not reached; few tokens with much work are shared.
+  const long tokens = std::max((p.total + 4095) / 4096, std::min((p.total + 1023) / 1024, 4L * NT / per_token));
+  p.tokens = (int)std::min(tokens, std::max(1L, std::min((long)kMaxAngles / p.pairs, (long)kMaxTokens)));
   const long groups = (p.total + p.tokens - 1) / p.tokens, work = (p.tokens * per_token + NT - 1) / NT;
   p.groups = (int)groups;
   p.split = (int)std::max(1L, std::min(work, 1024 / groups));
@@ -202,18 +186,19 @@ int launch_form(const RopeArgs& a, hipStream_t s) {
 
 template <typename T>
 int launch(const RopeArgs& a, hipStream_t s) {
-  // Vectors of eight channels: every head starts on 16 bytes, the rotated part and its halves are whole vectors.
-  constexpr int W = 8;
-  auto fits = [&](const RopeTensor& t) {
-    auto part = [](const void* p, const wmdec_strides& st) {
-      return ((uintptr_t)p & 15) == 0 && st.sample * sizeof(T) % 16 == 0 && st.token * sizeof(T) % 16 == 0 && st.head * sizeof(T) % 16 == 0;
+  // Vectors of eight channels, or of four: every head starts on one, the rotated part and its halves are whole vectors.
+  auto fits = [&](int w) {
+    const size_t to = std::min<size_t>(16, w * sizeof(T));
+    auto part = [&](const void* p, const wmdec_strides& st) {
+      return (uintptr_t)p % to == 0 && st.sample * sizeof(T) % to == 0 && st.token * sizeof(T) % to == 0 && st.head * sizeof(T) % to == 0;
     };
-    return t.heads == 0 || (part(t.in, t.si) && part(t.out, t.so));
+    auto tensor = [&](const RopeTensor& t) { return t.heads == 0 || (part(t.in, t.si) && part(t.out, t.so)); };
+    bool ok = a.d % w == 0 && a.rot % w == 0 && tensor(a.q) && tensor(a.k);
+    for (int i = 0; i < a.layout.axes; ++i) ok = ok && (a.layout.interleaved || a.layout.axis_dim[i] % (2 * w) == 0);
+    return ok;
   };
-  bool vec = a.d % W == 0 && a.rot % W == 0 && fits(a.q) && fits(a.k);
-  for (int i = 0; i < a.layout.axes; ++i) vec = vec && (a.layout.interleaved || a.layout.axis_dim[i] % (2 * W) == 0);
-  if (a.layout.interleaved) return vec ? launch_form<T, W, true>(a, s) : launch_form<T, 1, true>(a, s);
-  return vec ? launch_form<T, W, false>(a, s) : launch_form<T, 1, false>(a, s);
+  if (a.layout.interleaved) return fits(8) ? launch_form<T, 8, true>(a, s) : fits(4) ? launch_form<T, 4, true>(a, s) : launch_form<T, 1, true>(a, s);
+  return fits(8) ? launch_form<T, 8, false>(a, s) : fits(4) ? launch_form<T, 4, false>(a, s) : launch_form<T, 1, false>(a, s);
 }
 
 }  // namespace
