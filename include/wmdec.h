@@ -312,7 +312,7 @@ int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype
  * the gradient of the operator.  q, k: [n, t, heads, d] through strides in
  * elements, channels contiguous (parts of a fused projection need no copy); k may
  * be NULL.  Outputs may be the inputs themselves (same pointer and strides); no
- * other overlap.  positions: int32 [t][axes], positions_stride elements from
+ * other overlap, and no stride of zero over several tokens, heads or samples.  positions: int32 [t][axes], positions_stride elements from
  * sample to sample (0: the same for all).  1 to 3 axes.  Rotations are exact to
  * fp32 for every int32 position; one rounding to dtype. */
 typedef enum { WMDEC_ROPE_PLAIN = 0, WMDEC_ROPE_LINEAR = 1, WMDEC_ROPE_BASE = 2, WMDEC_ROPE_RAMP = 3 } wmdec_rope_scaling_kind;
@@ -349,13 +349,13 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
  * q, o: [n,tq,heads_q,d], k, v: [n,tk,heads_kv,d] of dtype through strides in
  * elements, channels contiguous.  d: a multiple of 8 (16-bit types) or 4 (F32), at
  * most 256; pointers and strides multiples of 16 bytes; 128 tokens of k or v span
- * less than 2 GiB.  scale > 0.  o must not overlap the inputs.
+ * less than 2 GiB.  scale > 0.  o must not overlap the inputs or itself.
  * Scores, softmax and sums are fp32; 16-bit types round the probabilities to dtype
  * for the second product.  F32 is fp32 throughout.  A sample's bits do not depend
  * on what it is batched with.
  * workspace: wmdec_cross_attention_workspace_bytes(...) bytes (may be 0) of
  * 16-byte aligned device memory, no initialisation; one or two kernels. */
-size_t wmdec_cross_attention_workspace_bytes(int dtype, int tk, int n, int tq, int heads_q, int heads_kv, int d);
+size_t wmdec_cross_attention_workspace_bytes(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d);
 int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const void* k, const wmdec_strides* k_strides,
                           const void* v, const wmdec_strides* v_strides, void* o, const wmdec_strides* o_strides, int dtype,
                           float scale, const int* key_lens, const unsigned char* key_mask, int n, int tq, int tk,

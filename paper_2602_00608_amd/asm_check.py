@@ -14,6 +14,8 @@ within STORE_WAIT wait states, that may be what is stored.  The compiler leaves 
 them behind the store (store_vector), which holds as long as the compiler does not copy the data out of its registers in between.
 
 Spilled vector registers, in the kernels that are laid out to fill the register file.
+
+M0 in kernels that load tiles into LDS in inline assembly: it is theirs alone, as the compiler does not know that they write it.
 """
 import re
 
@@ -156,11 +158,18 @@ def _spills(text, kernel, keys=("vgpr_spill_count", "private_segment_fixed_size"
     return faults
 
 
-def check_source(text, scores=None, spills=None):
-    """Faults of a device assembly file: its stores, the matrix instructions in inline assembly of kernel `scores`, the spills of kernel `spills`."""
+def check_m0(lines):
+    """Uses of M0 other than the address of a load into LDS, as texts."""
+    return ["M0 is used: `%s`" % op for op in _Code(lines).ops if re.search(r"\bm0\b", op) and not op.startswith("s_add_u32 m0,")]
+
+
+def check_source(text, scores=None, spills=None, m0=None):
+    """Faults of a device assembly file: its stores, the matrix instructions in inline assembly of kernel `scores`, the spills of kernel `spills`, M0 in kernel `m0`."""
     faults = ["%s: %s" % (name, f) for name, lines in functions(text) for f in check_stores(lines)]
     if scores:
         faults += check(text, scores)
+    if m0:
+        faults += ["%s: %s" % (name, f) for name, lines in functions(text) if m0 in name for f in check_m0(lines)]
     return faults + (_spills(text, spills) if spills else [])
 
 

@@ -25,8 +25,8 @@ SOURCES = ["api.cpp", "kernels_gn.hip", "kernels_conv_direct.hip", "kernels_conv
 # what asm_check looks for beside the stores of every source: kernels with matrix instructions in inline assembly, kernels that must not spill
 CHECKED = {"kernels_attn.hip": {"scores": "flash_attn_kernel"}, "kernels_conv_rows.hip": {"spills": "conv_mfma_kernel"},
            "kernels_conv_rows_bf16.hip": {"spills": "conv_mfma_kernel"},
-           "kernels_cross.hip": {"spills": "cross_attention_kernel"}, "kernels_cross_bf16.hip": {"spills": "cross_attention_kernel"},
-           "kernels_cross_f32.hip": {"spills": "cross_attention_kernel"}}
+           "kernels_cross.hip": {"spills": "cross_attention_kernel", "m0": "cross_attention_kernel"}, "kernels_cross_bf16.hip": {"spills": "cross_attention_kernel", "m0": "cross_attention_kernel"},
+           "kernels_cross_f32.hip": {"spills": "cross_attention_kernel", "m0": "cross_attention_kernel"}}
 
 # sources that include another one
 INCLUDES = {"kernels_conv_rows_bf16.hip": "kernels_conv_rows.hip"}

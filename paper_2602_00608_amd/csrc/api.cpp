@@ -892,6 +892,9 @@ static bool strides_in_range(const wmdec_strides& s, int n, int t, int heads) {
   return s.sample >= 0 && s.token >= 0 && s.head >= 0 && (double)n * s.sample + (double)t * s.token + (double)heads * s.head < 0x1p58;
 }
 
+// an output has a place of its own for every token and head
+static bool distinct(const wmdec_strides& s, int n, int t, int heads) { return (n == 1 || s.sample > 0) && (t == 1 || s.token > 0) && (heads == 1 || s.head > 0); }
+
 static int check_rope_tensor(const char* who, const void* in, const wmdec_strides* si, void* out, const wmdec_strides* so, int heads, size_t es, int n, int tokens,
                              RopeTensor* t) {
   WMDEC_REQUIRE(in && si && out && so, WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
@@ -900,6 +903,7 @@ static int check_rope_tensor(const char* who, const void* in, const wmdec_stride
   WMDEC_REQUIRE(strides_in_range(*si, n, tokens, heads) && strides_in_range(*so, n, tokens, heads), WMDEC_ERR_INVALID_ARG, "%s: a stride is negative or too large", who);
   WMDEC_REQUIRE(in != out || (si->sample == so->sample && si->token == so->token && si->head == so->head), WMDEC_ERR_INVALID_ARG,
                 "%s: in place the output has the input's strides", who);
+  WMDEC_REQUIRE(distinct(*so, n, tokens, heads), WMDEC_ERR_INVALID_ARG, "%s: an output stride is zero", who);
   t->in = in; t->out = out; t->si = *si; t->so = *so; t->heads = heads;
   return WMDEC_OK;
 }
@@ -930,9 +934,9 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
 }
 
 // ---- attention to states of another length
-size_t wmdec_cross_attention_workspace_bytes(int dtype, int tk, int n, int tq, int heads_q, int heads_kv, int d) {
+size_t wmdec_cross_attention_workspace_bytes(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d) {
   if (!valid_dtype(dtype) || tk < 0 || n <= 0 || tq <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q % heads_kv || d <= 0 || d > kCrossMaxD) return 0;
-  return cross_attention_scratch_bytes(dtype, tk, n, tq, heads_kv, heads_q / heads_kv, d);
+  return cross_attention_scratch_bytes(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
 }
 
 static int check_cross_tensor(const char* who, const void* p, const wmdec_strides* s, int n, int tokens, int heads, size_t es) {
@@ -960,11 +964,11 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
   if (rc != WMDEC_OK) return rc;
   WMDEC_REQUIRE(128 * k_strides->token * es < (1L << 31) && 128 * v_strides->token * es < (1L << 31), WMDEC_ERR_UNSUPPORTED, "%s: 128 tokens of k or v span 2 GiB or more", who);
   WMDEC_REQUIRE(isfinite(scale) && scale > 0.f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
-  WMDEC_REQUIRE(o != q && o != k && o != v, WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs", who);
+  WMDEC_REQUIRE(o != q && o != k && o != v && distinct(*o_strides, n, tq, heads_q), WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs or itself", who);
   WMDEC_REQUIRE(element_aligned(key_lens, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
   const long rows = (long)tq * (heads_q / heads_kv);
   WMDEC_REQUIRE(rows <= (1L << 31) - 512 && tk <= (1L << 31) - 512 && (long)n * heads_kv * (rows / 32 + 1) <= (1L << 31) / kCrossMaxSplits, WMDEC_ERR_UNSUPPORTED, "%s: too many rows", who);
-  const size_t need = cross_attention_scratch_bytes(dtype, tk, n, tq, heads_kv, heads_q / heads_kv, d);
+  const size_t need = cross_attention_scratch_bytes(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
   WMDEC_REQUIRE(need == 0 || (workspace && aligned16(workspace) && workspace_bytes >= need), WMDEC_ERR_WORKSPACE,
                 "%s: workspace needs %zu 16-byte aligned bytes, got %zu", who, need, workspace ? workspace_bytes : (size_t)0);
   CrossArgs a;

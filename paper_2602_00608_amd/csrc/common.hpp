@@ -232,7 +232,7 @@ struct CrossArgs {
   void* scratch = nullptr;
 };
 constexpr int kCrossMaxD = 256, kCrossMaxSplits = 64;   // splits: ranges of keys of one row
-size_t cross_attention_scratch_bytes(int dtype, int tk, int n, int tq, int heads, int group, int d);
+size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d);
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s);
 
 // kernels_attn.hip: attention over the t tokens of a sample, head dimension 512 (q, k, v in the fragment order described there)

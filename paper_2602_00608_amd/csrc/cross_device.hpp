@@ -9,7 +9,7 @@
 // 16-byte chunk c of key r lies at chunk c ^ turn(r) of its row in LDS: the eight lanes of a pass over K (eight keys, one chunk) and the sixteen over V (four
 // keys, two chunks) then have banks of their own.  The loads bring the chunks in that order, as a lane chooses what it reads and not where it lands.
 #pragma once
-#include <mutex>
+#include <atomic>
 
 #include "conv_device.hpp"
 
@@ -504,10 +504,14 @@ template <typename T, int D, int QW, int KW, int KT, int WAVES>
 int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
   using F = CrossForm<T, D, QW, KW, KT>;
   auto kern = cross_attention_kernel<T, D, QW, KW, KT, WAVES>;
-  static std::once_flag attr_once;
-  hipError_t attr_err = hipSuccess;
-  std::call_once(attr_once, [&] { attr_err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, F::kSmem); });
-  WMDEC_HIP(attr_err);
+  static std::atomic<unsigned long long> known{0};   // devices that the kernel's LDS has been asked for on
+  int device = 0;
+  WMDEC_HIP(hipGetDevice(&device));
+  const unsigned long long bit = 1ull << (device & 63);
+  if (!(known.load() & bit)) {
+    WMDEC_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
+    known.fetch_or(bit);
+  }
   const CrossPlan& p = l.plan;
   const long blocks = (long)l.a.n * l.a.heads * p.row_blocks, rows = blocks * F::BQ;
   hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.splits)), dim3(F::NT), F::kSmem, s, l);

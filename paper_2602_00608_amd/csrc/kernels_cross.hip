@@ -11,7 +11,7 @@ template int cross_launch<f16_t>(const CrossLaunch&, hipStream_t);
 namespace {
 
 // Nothing here looks at the number of samples, so that the bits of a sample do not depend on what it is batched with.
-CrossPlan plan_of(int dtype, int tk, int tq, int heads, int group, int d) {
+CrossPlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   CrossPlan p;
   p.width = d <= 128 ? (d + 31) / 32 * 32 : d <= 192 ? 192 : 256;
   p.rows = tq * group;
@@ -24,7 +24,7 @@ CrossPlan plan_of(int dtype, int tk, int tq, int heads, int group, int d) {
   // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow).
   const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
   const int slots = 256 * std::min(160 * 1024 / (tiles + 4096), !p.few && p.width <= 64 ? 4 : 2);
-  const long range = dtype != WMDEC_F32 ? 256 : p.few ? 128 : 64;   // fewest keys of a range
+  const long range = dtype != WMDEC_F32 || (p.few && bytes <= 512) ? 256 : p.few ? 128 : 64;   // fewest keys of a range: two tiles, or what is worth a launch
   p.splits = (int)std::max(1L, std::min({slots / blocks(bq), tk / range, (long)kCrossMaxSplits}));
   return p;
 }
@@ -33,15 +33,15 @@ size_t part_rows(const CrossPlan& p, int n, int heads) { return p.splits == 1 ? 
 
 }  // namespace
 
-size_t cross_attention_scratch_bytes(int dtype, int tk, int n, int tq, int heads, int group, int d) {
-  const CrossPlan p = plan_of(dtype, tk, tq, heads, group, d);
+size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d) {
+  const CrossPlan p = plan_of(dtype, tq, tk, heads, group, d);
   return part_rows(p, n, heads) * (p.width + 2) * sizeof(float);
 }
 
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s) {
   CrossLaunch l;
   l.a = a;
-  l.plan = plan_of(dtype, a.tk, a.tq, a.heads, a.group, a.d);
+  l.plan = plan_of(dtype, a.tq, a.tk, a.heads, a.group, a.d);
   l.part = (float*)a.scratch;
   l.ml = (float2*)(l.part + part_rows(l.plan, a.n, a.heads) * l.plan.width);
   if (dtype == WMDEC_F32) return cross_launch<float>(l, s);

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
     }
   }
 
-  const float inv_d = 1.f / (float)d;
+  const float inv_d = 1.f / (float)d, inv_held = p.tpr > 64 ? 1.f / fmaxf(held, 1.f) : inv_d;
   auto row_sum = [&](float v) {           // over the lanes of a row, or of a wavefront of it
     v = lane_group_sum<8>(v);
     if (p.tpr > 8) v += mirror16(v);
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
       for (int i = 0; i < VPT; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) sum += v[i][e];
-      mean = row_sum(sum) * (p.tpr > 64 ? __builtin_amdgcn_rcpf(fmaxf(held, 1.f)) : inv_d);
+      mean = row_sum(sum) * inv_held;
     }
     float m2 = 0.f;
 #pragma unroll

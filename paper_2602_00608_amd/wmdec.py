@@ -337,7 +337,7 @@ def rope(q, k, positions, freq, axis_dims, q_out, k_out, interleaved=False, inve
 
 def cross_attention_workspace_bytes(q, k):
     n, tq, hq, d = q.shape
-    return lib().wmdec_cross_attention_workspace_bytes(dtype_enum(q), k.shape[1], n, tq, hq, k.shape[2], d)
+    return lib().wmdec_cross_attention_workspace_bytes(dtype_enum(q), n, tq, k.shape[1], hq, k.shape[2], d)
 
 
 def cross_attention(q, k, v, o, scale, key_lens=None, key_mask=None, workspace=None):

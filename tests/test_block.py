@@ -9,7 +9,7 @@ import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
 
 from oracle import ref
-from paper_2602_00608_amd import wmdec
+from paper_2602_00608_amd import asm_check, wmdec
 
 
 # ------------------------------------------------------------------ oracle
@@ -107,7 +107,7 @@ def test_residual_norm_refuses(status, changes):
 
 
 S = wmdec._CStrides
-ROPE = dict(q=P, qs=S(0, 256, 64), qo=2 * P, qos=S(0, 256, 64), hq=4, k=3 * P, ks=S(0, 128, 64), ko=4 * P, kos=S(0, 128, 64), hk=2, dtype=1, positions=5 * P,
+ROPE = dict(q=P, qs=S(768, 256, 64), qo=2 * P, qos=S(768, 256, 64), hq=4, k=3 * P, ks=S(384, 128, 64), ko=4 * P, kos=S(384, 128, 64), hk=2, dtype=1, positions=5 * P,
             positions_stride=0, freq=6 * P, layout=wmdec._CRopeLayout(1, (ctypes.c_int * 3)(64, 0, 0), 0, 0, 1.0), n=1, t=3, d=64, stream=None)
 
 
@@ -124,6 +124,7 @@ def _layout(axes=1, dims=(64, 0, 0), magnitude=1.0):
     (wmdec.ERR_UNSUPPORTED, dict(layout=_layout(1, (4098, 0, 0)), d=8192)), (wmdec.ERR_UNSUPPORTED, dict(d=16385)), (wmdec.ERR_UNSUPPORTED, dict(hq=16384)),
     (wmdec.ERR_INVALID_ARG, dict(qs=S(0, -256, 64))), (wmdec.ERR_INVALID_ARG, dict(qs=S(0, 1 << 60, 64))),
     (wmdec.ERR_INVALID_ARG, dict(qo=P, qos=S(0, 512, 64))), (wmdec.ERR_INVALID_ARG, dict(qo=4 * P)), (wmdec.ERR_INVALID_ARG, dict(qo=3 * P)), (wmdec.ERR_INVALID_ARG, dict(ko=P)),
+    (wmdec.ERR_INVALID_ARG, dict(qos=S(0, 256, 0))), (wmdec.ERR_INVALID_ARG, dict(kos=S(0, 0, 64))),
     (wmdec.ERR_INVALID_ARG, dict(q=P + 1)), (wmdec.ERR_SHAPE, dict(n=2, positions_stride=2)), (wmdec.ERR_UNSUPPORTED, dict(n=65536, t=65536)),
 ])
 def test_rope_refuses(status, changes):
@@ -153,7 +154,7 @@ CROSS = dict(q=P, qs=S(768, 256, 64), k=2 * P, ks=S(2560, 128, 64), v=3 * P, vs=
     (wmdec.ERR_INVALID_ARG, dict(k=2 * P + 8)), (wmdec.ERR_INVALID_ARG, dict(ks=S(2560, 132, 64))), (wmdec.ERR_INVALID_ARG, dict(vs=S(2560, 128, 60))),
     (wmdec.ERR_INVALID_ARG, dict(qs=S(-768, 256, 64))), (wmdec.ERR_UNSUPPORTED, dict(ks=S(0, 1 << 23, 64))),
     (wmdec.ERR_INVALID_ARG, dict(scale=0.0)), (wmdec.ERR_INVALID_ARG, dict(scale=-1.0)), (wmdec.ERR_INVALID_ARG, dict(scale=math.inf)), (wmdec.ERR_INVALID_ARG, dict(scale=math.nan)),
-    (wmdec.ERR_INVALID_ARG, dict(o=P)), (wmdec.ERR_INVALID_ARG, dict(o=3 * P)), (wmdec.ERR_INVALID_ARG, dict(lens=6 * P + 2)), (wmdec.ERR_UNSUPPORTED, dict(tk=(1 << 31) - 1)),
+    (wmdec.ERR_INVALID_ARG, dict(o=P)), (wmdec.ERR_INVALID_ARG, dict(o=3 * P)), (wmdec.ERR_INVALID_ARG, dict(os=S(768, 0, 64))), (wmdec.ERR_INVALID_ARG, dict(os=S(0, 256, 64))), (wmdec.ERR_INVALID_ARG, dict(lens=6 * P + 2)), (wmdec.ERR_UNSUPPORTED, dict(tk=(1 << 31) - 1)),
     (wmdec.ERR_UNSUPPORTED, dict(n=1 << 20, tq=1 << 20)),
 ])
 def test_cross_attention_refuses(status, changes):
@@ -162,12 +163,13 @@ def test_cross_attention_refuses(status, changes):
 
 def test_cross_attention_workspace_is_asked_for():
     size = wmdec.lib().wmdec_cross_attention_workspace_bytes
-    need = size(wmdec.BF16, 32768, 1, 1, 32, 8, 128)
-    if need:
-        big = dict(CROSS, n=1, tq=1, tk=32768, hq=32, hk=8, d=128, ks=S(0, 1024, 128), vs=S(0, 1024, 128), qs=S(0, 0, 128), os=S(0, 0, 128))
-        for ws, have in ((None, 1 << 40), (5 * P, need - 1), (5 * P + 8, 1 << 40)):
-            assert wmdec.lib().wmdec_cross_attention(*dict(big, ws=ws, bytes=have).values()) == wmdec.ERR_WORKSPACE
-    for bad in ((7, 5, 1, 1, 4, 2, 64), (1, -1, 1, 1, 4, 2, 64), (1, 5, 0, 1, 4, 2, 64), (1, 5, 1, 1, 4, 3, 64), (1, 5, 1, 1, 4, 2, 512)):
+    need = size(wmdec.BF16, 1, 1, 32768, 32, 8, 128)
+    assert need > 0
+    big = dict(CROSS, n=1, tq=1, tk=32768, hq=32, hk=8, d=128, ks=S(0, 1024, 128), vs=S(0, 1024, 128), qs=S(0, 0, 128), os=S(0, 0, 128))
+    for ws, have in ((None, 1 << 40), (5 * P, need - 1), (5 * P + 8, 1 << 40)):
+        assert wmdec.lib().wmdec_cross_attention(*dict(big, ws=ws, bytes=have).values()) == wmdec.ERR_WORKSPACE
+    assert size(wmdec.BF16, 7, 1, 32768, 32, 8, 128) == 7 * need and size(wmdec.BF16, 1, 5400, 512, 30, 30, 64) == 0
+    for bad in ((7, 1, 1, 5, 4, 2, 64), (1, 1, 1, -1, 4, 2, 64), (1, 0, 1, 5, 4, 2, 64), (1, 1, 1, 5, 4, 3, 64), (1, 1, 1, 5, 4, 2, 512)):
         assert size(*bad) == 0
 
 
@@ -250,3 +252,12 @@ def _call_cross(q=None, k=None, v=None, o=None, **more):
 def test_cross_attention_binding_refuses(call, error):
     with pytest.raises(error):
         call()
+
+
+# ------------------------------------------------------------------ compiled code
+def test_other_uses_of_m0_are_found():
+    load = ["s_add_u32 m0, s4, 0x400", "s_nop 0", "buffer_load_dwordx4 v2, s[8:11], s3 offen lds"]
+    assert asm_check.check_m0(load) == []
+    assert len(asm_check.check_m0(load + ["s_mov_b32 m0, s5"])) == 1 and len(asm_check.check_m0(load + ["v_readlane_b32 s3, v2, m0"])) == 1
+    text = "\n".join(["_Z6kernel:"] + ["\t" + l for l in load + ["s_mov_b32 m0, -1", "s_endpgm"]] + [".Lfunc_end0:"])
+    assert len(asm_check.check_source(text, m0="kernel")) == 1 and asm_check.check_source(text, m0="other") == []
