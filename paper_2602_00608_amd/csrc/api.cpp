@@ -854,6 +854,8 @@ int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype
   a.gate = gate; a.scale = scale; a.shift = shift;
   a.res_scale = res_scale; a.mod_stride = n == 1 ? 0 : (long)mod_stride;
   a.n = n; a.t = t; a.d = d;
+  if (a.mod_stride == 0 || (!gate && !scale && !shift)) { a.n = 1; a.t = n * t; a.mod_stride = 0; }   // the same vectors for all rows
+  WMDEC_REQUIRE(a.n <= kResidualNormMaxSamples, WMDEC_ERR_UNSUPPORTED, "%s: vectors for more than %d samples", who, kResidualNormMaxSamples);
   return launch_residual_norm(a, x_dtype, act_dtype, (hipStream_t)stream);
 }
 
@@ -962,12 +964,14 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
   if (rc == WMDEC_OK) rc = check_cross_tensor(who, v, v_strides, n, tk, heads_kv, es);
   if (rc == WMDEC_OK) rc = check_cross_tensor(who, o, o_strides, n, tq, heads_q, es);
   if (rc != WMDEC_OK) return rc;
-  WMDEC_REQUIRE(128 * k_strides->token * es < (1L << 31) && 128 * v_strides->token * es < (1L << 31), WMDEC_ERR_UNSUPPORTED, "%s: 128 tokens of k or v span 2 GiB or more", who);
+  const long most = (1L << 31) / (128 * (long)es);
+  WMDEC_REQUIRE(k_strides->token < most && v_strides->token < most, WMDEC_ERR_UNSUPPORTED, "%s: 128 tokens of k or v span 2 GiB or more", who);
   WMDEC_REQUIRE(isfinite(scale) && scale > 0.f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
   WMDEC_REQUIRE(o != q && o != k && o != v && distinct(*o_strides, n, tq, heads_q), WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs or itself", who);
   WMDEC_REQUIRE(element_aligned(key_lens, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
   const long rows = (long)tq * (heads_q / heads_kv);
-  WMDEC_REQUIRE(rows <= (1L << 31) - 512 && tk <= (1L << 31) - 512 && (long)n * heads_kv * (rows / 32 + 1) <= (1L << 31) / kCrossMaxSplits, WMDEC_ERR_UNSUPPORTED, "%s: too many rows", who);
+  WMDEC_REQUIRE(rows <= (1L << 31) - 512 && tk <= (1L << 31) - 512 && cross_attention_fits(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d), WMDEC_ERR_UNSUPPORTED,
+                "%s: too many rows", who);
   const size_t need = cross_attention_scratch_bytes(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
   WMDEC_REQUIRE(need == 0 || (workspace && aligned16(workspace) && workspace_bytes >= need), WMDEC_ERR_WORKSPACE,
                 "%s: workspace needs %zu 16-byte aligned bytes, got %zu", who, need, workspace ? workspace_bytes : (size_t)0);

@@ -206,7 +206,7 @@ struct ResidualNormArgs {
   long mod_stride = 0;
   int n = 0, t = 0, d = 0;
 };
-constexpr int kResidualNormMaxD = 16384;
+constexpr int kResidualNormMaxD = 16384, kResidualNormMaxSamples = 1 << 22;   // samples with vectors of their own (a workgroup each at least, of up to 512 threads)
 int launch_residual_norm(const ResidualNormArgs& a, int x_dtype, int act_dtype, hipStream_t s);
 
 // kernels_rope.hip
@@ -232,6 +232,7 @@ struct CrossArgs {
   void* scratch = nullptr;
 };
 constexpr int kCrossMaxD = 256, kCrossMaxSplits = 64;   // splits: ranges of keys of one row
+bool cross_attention_fits(int dtype, int n, int tq, int tk, int heads, int group, int d);   // into launches of less than 2^32 threads
 size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d);
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s);
 

@@ -33,6 +33,12 @@ size_t part_rows(const CrossPlan& p, int n, int heads) { return p.splits == 1 ? 
 
 }  // namespace
 
+bool cross_attention_fits(int dtype, int n, int tq, int tk, int heads, int group, int d) {
+  const CrossPlan p = plan_of(dtype, tq, tk, heads, group, d);
+  const double blocks = (double)n * heads * p.row_blocks;
+  return blocks * p.splits < 0x1p24 && (p.splits == 1 || blocks * (p.few ? 32 : 128) < 0x1p26);   // workgroups of 256 threads; rows that are joined, four of them
+}
+
 size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d) {
   const CrossPlan p = plan_of(dtype, tq, tk, heads, group, d);
   return part_rows(p, n, heads) * (p.width + 2) * sizeof(float);

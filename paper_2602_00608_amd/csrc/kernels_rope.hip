@@ -178,7 +178,7 @@ int launch_form(const RopeArgs& a, hipStream_t s) {
   p.split = (int)std::max(1L, std::min(work, 1024 / groups));
   const long step = (long)NT * p.split;
   p.du = (int)(step % p.units); p.dh = (int)(step / p.units % (a.q.heads + a.k.heads)); p.dt = (int)(step / per_token);
-  WMDEC_REQUIRE(groups * p.split < (1L << 31), WMDEC_ERR_UNSUPPORTED, "rope: too many tokens");
+  WMDEC_REQUIRE(groups * p.split < (1L << 24), WMDEC_ERR_UNSUPPORTED, "rope: too many tokens");
   hipLaunchKernelGGL((rope_kernel<T, W, INTERLEAVED>), dim3((unsigned)(groups * p.split)), dim3(NT), p.tokens * p.pairs * sizeof(float2), s, p);
   WMDEC_HIP(hipGetLastError());
   return WMDEC_OK;

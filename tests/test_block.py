@@ -161,6 +161,16 @@ def test_cross_attention_refuses(status, changes):
     assert wmdec.lib().wmdec_cross_attention(*dict(CROSS, **changes).values()) == status and "cross_attention" in wmdec.last_error()
 
 
+def test_launches_of_too_many_threads_are_refused():
+    """A launch has less than 2^32 threads: samples with vectors of their own, tokens with a workgroup each, rows, and rows whose ranges of keys are joined."""
+    assert _norm(n=(1 << 22) + 1, t=1) == wmdec.ERR_UNSUPPORTED
+    layout = wmdec._CRopeLayout(1, (ctypes.c_int * 3)(4096, 0, 0), 0, 0, 1.0)
+    wide = S(0, 3 * 4096, 4096)
+    assert wmdec.lib().wmdec_rope(*dict(ROPE, layout=layout, d=4096, t=1 << 24, hq=2, hk=1, qs=wide, qos=wide, ks=wide, kos=wide).values()) == wmdec.ERR_UNSUPPORTED
+    for changes in (dict(n=1 << 23, tq=1, tk=20), dict(n=1 << 21, tq=1, tk=1 << 20, hq=1, hk=1), dict(n=1 << 20, tq=33, tk=4096, hq=1, hk=1)):
+        assert wmdec.lib().wmdec_cross_attention(*dict(CROSS, **changes).values()) == wmdec.ERR_UNSUPPORTED, changes
+
+
 def test_cross_attention_workspace_is_asked_for():
     size = wmdec.lib().wmdec_cross_attention_workspace_bytes
     need = size(wmdec.BF16, 1, 1, 32768, 32, 8, 128)

@@ -159,6 +159,22 @@ def test_residual_norm_one_vector_for_all_samples_and_rows_alike():
     assert all(torch.equal(a, outs[0][0]) and torch.equal(b, outs[0][1]) for a, b in outs)
 
 
+def test_residual_norm_rows_of_many_samples():
+    """Samples that share their vectors, or have none, count as one; the bits are those of samples with equal vectors."""
+    r = rng(14)
+    x, h = dev(r.standard_normal((777, 1, 96)), "f16"), dev(r.standard_normal((777, 1, 96)), "f16")
+    w, m = G.dev_f32(1 + 0.1 * r.standard_normal(96)), G.dev_f32(0.3 * r.standard_normal((1, 96)))
+    spec = wmdec.Norm("rms", 1e-6, w)
+    got = []
+    for vectors in (m.expand(777, 96), m.expand(777, 96).contiguous()):
+        xo, y = torch.empty_like(x), torch.empty_like(x)
+        wmdec.residual_norm(x, h, spec, vectors, 0.5, xo, spec, vectors, vectors, y)
+        got.append((xo, y))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    run_norm("f16", "f16", 777, 1, 96, "rms", "layer", seed=15)
+    run_norm("f32", "bf16", 777, 3, 95, "layer", "rms", mod="none", seed=16)
+
+
 def test_residual_norm_not_a_number_stays_in_its_row():
     x, h = torch.randn((1, 40, 1920), device="cuda"), torch.randn((1, 40, 1920), device="cuda")
     x[0, 7, 3], h[0, 9, 1919], x[0, 11, 0] = float("nan"), float("inf"), float("inf")
