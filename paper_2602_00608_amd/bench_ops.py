@@ -1,8 +1,8 @@
-"""Per-operator timing of the C-ABI entry points at the decoder's layer shapes (one MI355X).
+"""Per-operator timing of the C-ABI entry points at the decoder's layer shapes and around a transformer block (one MI355X).
 
-    python -m paper_2602_00608_amd.bench_ops [--dtype f16|bf16] [--reps 20]      (or run the file directly)
+    python -m paper_2602_00608_amd.bench_ops [--dtype f16|bf16] [--reps 20] [--block]      (or run the file directly)
 
-Prints one line per operator: microseconds per call, algorithmic TFLOP/s or GB/s, and the fraction of the
+--block: only the operators of a transformer block.  Prints one line per operator: microseconds per call, algorithmic TFLOP/s or GB/s, and the fraction of the
 published MI355X peak (2516.6 TFLOP/s dense f16/bf16 MFMA, 8000 GB/s HBM).  Two timings per operator, both with HIP
 events on the current stream and inputs resident in HBM:
   warm  `reps` back-to-back calls on the same tensors (tensors up to a few hundred MB partly stay in the last-level
@@ -65,6 +65,7 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--dtype", default="f16", choices=["f16", "bf16"])
     ap.add_argument("--reps", type=int, default=20)
+    ap.add_argument("--block", action="store_true")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         sys.exit("bench_ops: no GPU visible; the HIP path has no CPU fallback")
@@ -88,6 +89,9 @@ def main():
                  (work / warm / 1e6 if unit == "TFLOP/s" else work / warm / 1e3) / peak * 100,
                  cold, work / cold / 1e6 if unit == "TFLOP/s" else work / cold / 1e3, unit,
                  (work / cold / 1e6 if unit == "TFLOP/s" else work / cold / 1e3) / peak * 100, peak), flush=True)
+
+    if args.block:
+        return block_operators(dt, line, args.reps)
 
     # cin, cout, h_out, w_out, kernel, upsample, normalise + SiLU on load, residual
     convs = [(128, 128, 480, 720, 3, 0, 1, 1), (256, 128, 480, 720, 3, 0, 1, 0), (256, 256, 240, 360, 3, 0, 1, 1),
@@ -193,6 +197,41 @@ def main():
         nbytes = wf.numel() * 2
         line("adaln fused (1 launch)", "batch %d %d->3x%d" % (batch, d, d), fused, nbytes, "GB/s", PEAK_GBPS)
         line("adaln 3 launches", "batch %d %d->3x%d" % (batch, d, d), sep, nbytes, "GB/s", PEAK_GBPS)
+
+    block_operators(dt, line, args.reps)
+
+
+def block_operators(dt, line, reps):
+    """Gated residual and norms, rotary positions, attention to other states: 5400 tokens are a 60x90 latent."""
+    def normal(*shape):
+        return torch.randn(shape, device="cuda").to(dt)
+
+    for n, t, d, xt in ((1, 1, 1920, dt), (2, 5400, 1920, dt), (4, 5400, 1152, torch.float32)):
+        x, h = torch.randn((n, t, d), device="cuda").to(xt), normal(n, t, d)
+        xo, y, mod = torch.empty_like(x), torch.empty_like(h), torch.randn((n, 3 * d), device="cuda")
+        shift, scale, gate = mod[:, :d], mod[:, d:2 * d], mod[:, 2 * d:]
+        pre = wmdec.Norm("layer", 1e-6)
+        us = timeit(lambda: wmdec.residual_norm(x, h, None, gate, 1.0, xo, pre, scale, shift, y), reps)
+        nbytes = 2 * (x.numel() * x.element_size() + h.numel() * 2)
+        line("residual_norm" + (" (fp32 x)" if xt != dt else ""), "%dx%d of %d" % (n, t, d), us, nbytes, "GB/s", PEAK_GBPS)
+
+    for n, t, hq, hk, d, dims in ((1, 1, 30, 30, 64, (16, 24, 24)), (2, 5400, 30, 30, 64, (16, 24, 24)), (1, 16384, 32, 8, 128, (128,))):
+        q, k = normal(n, t, hq, d), normal(n, t, hk, d)
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        freq = torch.empty(sum(dims) // 2, dtype=torch.float64, device="cuda")
+        wmdec.rope_frequencies(dims, freq)
+        pos = torch.randint(0, 4096, (t, len(dims)), dtype=torch.int32, device="cuda")
+        us = timeit(lambda: wmdec.rope(q, k, pos, freq, dims, qo, ko), reps)
+        line("rope (%d axes)" % len(dims), "%dx%d, %d+%d of %d" % (n, t, hq, hk, d), us, 2 * 2 * (q.numel() + k.numel()), "GB/s", PEAK_GBPS)
+
+    for n, tq, tk, hq, hk, d in ((2, 1, 77, 30, 30, 64), (16, 1, 4096, 32, 8, 128), (2, 5400, 512, 30, 30, 64), (1, 5400, 5400, 30, 30, 64), (1, 8192, 8192, 32, 8, 128)):
+        q, k, v = normal(n, tq, hq, d), normal(n, tk, hk, d), normal(n, tk, hk, d)
+        o = torch.empty_like(q)
+        ws = torch.empty(max(16, wmdec.cross_attention_workspace_bytes(q, k)), dtype=torch.uint8, device="cuda")
+        us = timeit(lambda: wmdec.cross_attention(q, k, v, o, d ** -0.5, workspace=ws), reps)
+        flops, nbytes = 4.0 * n * hq * tq * tk * d, 2 * (2 * q.numel() + 2 * k.numel())
+        unit = "TFLOP/s" if flops / nbytes >= 315 else "GB/s"
+        line("cross_attention", "%dx%dx%d, %d/%d of %d" % (n, tq, tk, hq, hk, d), us, flops if unit == "TFLOP/s" else nbytes, unit, PEAK_TFLOPS if unit == "TFLOP/s" else PEAK_GBPS)
 
 
 if __name__ == "__main__":

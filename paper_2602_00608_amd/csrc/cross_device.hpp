@@ -8,6 +8,19 @@
 //
 // 16-byte chunk c of key r lies at chunk c ^ turn(r) of its row in LDS: the eight lanes of a pass over K (eight keys, one chunk) and the sixteen over V (four
 // keys, two chunks) then have banks of their own.  The loads bring the chunks in that order, as a lane chooses what it reads and not where it lands.
+//
+// What bounds it.  Few rows: the one read of the keys and values; two workgroups of 32 rows a compute unit, with 128 KB of tiles under way.  Many rows in
+// 16 bits: the power that the matrix cores may draw, and at 64 channels the exponentials, which take as many cycles as the products (32 rows and 64 keys of a
+// wavefront: 16 products of 32 cycles, 32 exponentials of 8 beside 32 each of multiply-add, add and half a maximum and a conversion).  fp32: its products.
+// Rates: one token of 32 heads against 16 x 4096 keys of 8 heads of 128 in bf16 55.3 us = 4.86 TB/s; 8192x8192 of 32 / 8 heads of 128 1123 us = 979 TFLOP/s (a large
+// library product on this card 1090 to 1150); 5400x5400 of 30 heads of 64 in f16 290 to 304 us = 736 to 771, of 96 heads 870 to 890 (1290 workgroups are 1.26 rounds of
+// the 1024 that run at once); fp32 4000x2000 of 8 heads of 128 263 us = 125 of 155.
+// Steps, us for 5400x5400 of 30 of 64 f16, 2 x 5400x512 of 30 of 64 bf16 (two lengths), 1 token against 4 x 32768 (ragged) of 8 of 128: a wavefront a row 92950, 9854,
+// 50355; matrix cores, tiles through LDS, transposed reads 298, 66, 128; tiles by instructions that the compiler does not wait for 298, 66, 110; 128 rows a workgroup
+// and the XCDs divided within a sample 297, 50, 65; wavefronts past the last row idle 290, 50, 65.
+// Measured and not kept: 64 rows a wavefront (128 channels 818 TFLOP/s against 1005: half the wavefronts), wave priorities around the products, the compiler's own
+// interleaving of them, sums by dot products (4 cycles against 2), a loop over pairs of tiles, ranges for the last round's blocks alone (partial outputs cost what
+// they gain).
 #pragma once
 #include <atomic>
 
@@ -450,7 +463,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
 }
 
 // o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) for the rows of the blocks that are split.  A thread takes four channels of a row and every groups-th
-// range, eight at a time; the groups of a row are joined in order.
+// range, eight at a time; the groups of a row are joined in order.  Bound by latency: one trip for up to 8 * groups ranges, 3 to 6 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_combine_kernel(CrossLaunch launch, int bq, int groups) {
   constexpr int QUADS = D / 4, UNITS = 256 / QUADS, B = 8;

@@ -17,13 +17,19 @@ CrossPlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   p.rows = tq * group;
   const int bytes = p.width * (int)dtype_size(dtype);   // of a key
   auto blocks = [&](int bq) { return (long)heads * ((p.rows + bq - 1) / bq); };
-  // Few rows: the wavefronts of a workgroup share 32 rows and take a part of the keys each; so do those of more rows that would not give work to all.
-  p.few = bytes <= 768 && (p.rows <= 32 || (dtype == WMDEC_F32 && bytes <= 512 && blocks(128) <= 64));
+  // Few rows: the wavefronts of a workgroup share 32 rows and take a part of the keys each.  us, shared / 128 rows: 4 rows a key head against 16 x 4096 keys of 8 heads
+  // of 128 channels in bf16 57.9 / 64.9, 32 against 8 x 4096 of 8 of 64 in f16 21.9 / 26.8; 48 rows 28.6 / 28.8, and 100 x 4 against 2 x 2048 of 4 of 128 32.3 / 28.3.
+  // In fp32 also more rows whose blocks of 128 would not give work to all: 333x301 of 8 heads of 72 (24 blocks) 34 / 46, 1000x1000 of 12 of 64 (96) 44 / 59, 2000x500
+  // of 8 of 64 (128) 26 / 42; but 3000x3000 of 8 of 64 (192) 230 / 220, 700x700 of 12 of 96 (72) 56 / 47, 2 x 700x700 of 32 of 128 (192) 205 / 186.
+  p.few = bytes <= 768 && (p.rows <= 32 || (dtype == WMDEC_F32 && bytes <= 512 && blocks(128) <= (bytes <= 256 ? 128 : 64)));
   const int bq = p.few ? 32 : 128;
   p.row_blocks = (p.rows + bq - 1) / bq;
   // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow).
+  // us without / with ranges: 4 rows a key head against 32768 keys of 8 heads of 128 in bf16 247 / 28, 200 rows against 4096 of 8 of 64 in f16 62.5 / 17.2.
   const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
   const int slots = 256 * std::min(160 * 1024 / (tiles + 4096), !p.few && p.width <= 64 ? 4 : 2);
+  // (at 128 and 512 keys instead of 256 the second takes 20.2 and 18.5; fp32, 128 and 64 instead of 256: 5 rows against 4 x 699 keys of 10 heads of 256 113 / 71, but with
+  // shared rows of up to 512 bytes 333x301 of 8 of 72 20 / 31)
   const long range = dtype != WMDEC_F32 || (p.few && bytes <= 512) ? 256 : p.few ? 128 : 64;   // fewest keys of a range: two tiles, or what is worth a launch
   p.splits = (int)std::max(1L, std::min({slots / blocks(bq), tk / range, (long)kCrossMaxSplits}));
   return p;
