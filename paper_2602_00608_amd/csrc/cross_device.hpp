@@ -51,7 +51,7 @@ template <int CH> __device__ __forceinline__ int chunk_turn(int row) {   // CH: 
 
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // (NaN if one is: one instruction for three)
 
-constexpr int kMaskKeys = 32768;      // keys whose mask is staged as bits at a time
+constexpr int kMaskKeys = 2048;       // keys whose mask is read at a time; the places of the valid ones among them, as 16 bits
 
 // D: channels, rounded up to a multiple of 32; QW x KW wavefronts of 32 rows and 1 / KW of a tile's keys
 template <typename T, int D, int QW, int KW, int KT>
@@ -59,9 +59,9 @@ struct CrossForm {
   static constexpr int EC = kChunkElems<T>, CH = D / EC, NW = QW * KW, NT = 64 * NW, SUB = KT / KW, NS = SUB / 32, LOADS = KT * CH / NT, BQ = 32 * QW;
   static constexpr int TILE = KT * D, NB = KW == 1 ? 2 : 1;   // buffers of keys, and of values
   static constexpr int RED = D + 4;   // floats from row to row of the outputs that are joined
-  static constexpr int kTiles = 2 * NB * TILE * (int)sizeof(T), kRed = KW == 1 ? 0 : KW * 32 * (RED + 2) * 4, kLow = kTiles > kRed ? kTiles : kRed, kSmem = kLow + kMaskKeys / 8;
+  static constexpr int kTiles = 2 * NB * TILE * (int)sizeof(T), kRed = KW == 1 ? 0 : KW * 32 * (RED + 2) * 4, kLow = kTiles > kRed ? kTiles : kRed, kMask = kMaskKeys * 2 + kMaskKeys / 64 * 4;   // (the last only with a mask)
   static_assert(D % 32 == 0 && KT % (32 * KW) == 0 && KT * CH % NT == 0 && (KW == 1 || QW == 1));
-  static_assert(kSmem <= 160 * 1024 && LOADS < 64);
+  static_assert(kLow + kMask <= 160 * 1024 && LOADS < 64);
 };
 
 // Tiles are asked for and waited for in assembly: the compiler would wait for all of them in front of every transposed read.  No registers are written.
@@ -88,7 +88,8 @@ template <typename T> __device__ __forceinline__ void store_quad(T* row, int at,
 
 constexpr float kCrossSlack = 8.0f;   // log2 of how far a tile's maximum may exceed the reference before that moves
 
-template <typename T, int D, int QW, int KW, int KT, int WAVES>
+// MASKED: tiles are made of the valid keys alone, whose places are worked out for up to kMaskKeys keys at a time
+template <typename T, int D, int QW, int KW, int KT, int WAVES, bool MASKED>
 __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(CrossLaunch launch) {
   using F = CrossForm<T, D, QW, KW, KT>;
   constexpr int EC = F::EC, CH = F::CH, NW = F::NW, NS = F::NS, LOADS = F::LOADS, TILE = F::TILE, NB = F::NB, QS = CH / 2, ND = D / 32;
@@ -97,7 +98,8 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   extern __shared__ __align__(16) unsigned char smem[];
   T* s_k = reinterpret_cast<T*>(smem);      // [NB] tiles
   T* s_v = s_k + NB * TILE;
-  unsigned* s_bits = reinterpret_cast<unsigned*>(smem + F::kLow);   // the mask, 32 keys a word
+  unsigned short* s_place = reinterpret_cast<unsigned short*>(smem + F::kLow);   // [kMaskKeys] valid keys
+  int* s_count = reinterpret_cast<int*>(smem + F::kLow + kMaskKeys * 2);          // [kMaskKeys / 64] how many of 64 keys are valid
   const CrossArgs& a = launch.a;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lk = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = wave / KW, kw = wave % KW;
@@ -113,13 +115,13 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits);
   const int len = a.lens ? min(max(a.lens[n], 0), a.tk) : a.tk;
   const int tiles = (len + KT - 1) / KT, first = (int)((long)split * tiles / p.splits), nt = (int)((long)(split + 1) * tiles / p.splits) - first;
+  const int begin = first * KT, end = min((long)len, (long)(first + nt) * KT);   // keys of the range
 
   // ---- tiles.  A load is 64 consecutive chunks of a tile; chunks past the last channel and keys past the last one are read past the buffer's end
   const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const char* kp = (const char*)a.k + (n * a.ks.sample + h * a.ks.head) * (long)sizeof(T);
   const char* vp = (const char*)a.v + (n * a.vs.sample + h * a.vs.head) * (long)sizeof(T);
   const int kstep = (int)(a.ks.token * (long)sizeof(T)), vstep = (int)(a.vs.token * (long)sizeof(T));   // (128 of them are below 2^31: checked on the host)
-  const unsigned char* mask = a.mask ? a.mask + (long)n * a.tk : nullptr;
   auto slot0 = [&](int i) { return OWN ? wave * F::SUB * CH + i * 64 : (i * NW + wave) * 64; };
   // Offsets of the loads: every PER-th one has the same chunks of keys that are a multiple of eight further, a scalar part of the address.
   constexpr int ROWS = 64 % CH == 0 ? 64 / CH * (OWN ? 1 : NW) : 0;   // keys from a load to the next; 0: loads end inside a key
@@ -128,23 +130,26 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int r = (slot0(i) + lane) / CH, c = ((slot0(i) + lane) % CH) ^ chunk_turn<CH>(r);
-    koff[i] = c * EC < a.d ? (unsigned)(r * kstep + c * 16) : kPastEnd;
-    voff[i] = c * EC < a.d ? (unsigned)(r * vstep + c * 16) : kPastEnd;
+    koff[i] = c * EC < a.d ? (unsigned)((MASKED ? 0 : r * kstep) + c * 16) : kPastEnd;
+    voff[i] = c * EC < a.d ? (unsigned)((MASKED ? 0 : r * vstep) + c * 16) : kPastEnd;
   }
+  int k0 = begin, count = 0;   // the keys at work: `count` from k0 on, or the valid ones among those from k0 on
   auto ask = [&](const char* base, int step, const unsigned (&off)[PER], int at, int j) {
-    const int k0 = (first + j) * KT, left = len - k0;
-    const uint64_t from = (uint64_t)(base + (long)k0 * step);
+    const int left = count - j * KT;
+    const uint64_t from = (uint64_t)(base + (k0 + (MASKED ? 0L : (long)j * KT)) * step);
     const u32x4 buffer{(unsigned)from, (unsigned)(from >> 32) & 0xffffu, kPastEnd - 1, 0x00020000u};
     const unsigned to = lds + (at + (NB == 2 ? j & 1 : 0) * TILE) * (int)sizeof(T) + slot0(0) * 16;
     unsigned more = 0;
     static_for<LOADS>([&](auto i_c) {
       constexpr int i = decltype(i_c)::value;
-      if constexpr (i > 0 && i % PER == 0) {
+      if constexpr (!MASKED && i > 0 && i % PER == 0) {
         more += PER * ROWS * step;
         asm volatile("" : "+s"(more));   // (one after the other: worked out beforehand for all loads they do not fit the scalar registers)
       }
       unsigned o = off[i % PER];
-      if (left < KT) o = (slot0(i) + lane) / CH < left ? o : kPastEnd;
+      const int r = (slot0(i) + lane) / CH;
+      if constexpr (MASKED) o = r < left ? o + s_place[j * KT + r] * (unsigned)step : kPastEnd;   // (below 2^32: a place times the step is below 2^31)
+      else if (left < KT) o = r < left ? o : kPastEnd;
       load_to_lds<i * (OWN ? 1 : NW) * 1024>(buffer, o, more, to);
     });
   };
@@ -247,8 +252,10 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
       if (bits[ns] != ~0u) {
         const unsigned b = bits[ns] >> (4 * lk);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!((b >> (8 * (r / 4) + r % 4)) & 1)) s[ns][r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) {   // -inf where the bit is not set, in two instructions: the bit spread over the word, and a choice by it
+          const unsigned is = (unsigned)((int)(b << (31 - 8 * (r / 4) - r % 4)) >> 31);
+          s[ns][r] = __uint_as_float((is & __float_as_uint(s[ns][r])) | (~is & 0xff800000u));
+        }
       }
   };
   // The reference moves when a maximum exceeds it by 2^kCrossSlack; until then probabilities may reach that, well inside the 16-bit types.
@@ -310,43 +317,53 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     }
   };
 
-  // The mask of up to kMaskKeys keys is staged at a time; without one all keys are one block.
-  constexpr int MB = kMaskKeys / KT;
-  for (int b0 = 0; b0 < nt;) {
-    const int b1 = mask ? min(nt, b0 + MB) : nt;
-    if (mask) {
-      if (b0) sync_tiles();   // (the bits before have been read)
-      const int k0 = (first + b0) * KT, words = ((b1 - b0) * KT + 63) / 64;
-      for (int w = wave; w < words; w += NW) {
-        const int key = k0 + w * 64 + lane;
-        const unsigned long long bit = __ballot(key < len && mask[min(key, len - 1)] != 0);
-        if (lane == 0) *reinterpret_cast<u32x2*>(s_bits + 2 * w) = u32x2{(unsigned)bit, (unsigned)(bit >> 32)};
+  const int stage = min(kMaskKeys, (int)((kPastEnd - 1) / (unsigned)max(max(kstep, vstep), 1)) & -64);   // (at least 64; all of them within a buffer)
+  while (k0 < end) {   // without a mask once
+    const int here = MASKED ? min(end - k0, stage) : end - k0;
+    if constexpr (MASKED) {
+      constexpr int WORDS = kMaskKeys / 64 / NW;
+      const unsigned char* mask = a.mask + (long)n * a.tk + k0;
+      if (k0 != begin) sync_tiles();   // (the places before have been read)
+      bool set[WORDS];
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const int key = (i * NW + wave) * 64 + lane;
+        set[i] = mask[min(key, here - 1)] != 0 && key < here;
+      }
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const int valid = __popcll(__ballot(set[i]));
+        if (lane == 0) s_count[i * NW + wave] = valid;
       }
       sync_lds();
+      const int own = s_count[l32];
+      int upto = own;                  // valid keys up to the 64 of number l32
+#pragma unroll
+      for (int step = 1; step < kMaskKeys / 64; step *= 2) {
+        const int before = __shfl_up(upto, step, kMaskKeys / 64);
+        if (l32 >= step) upto += before;
+      }
+      count = __builtin_amdgcn_readlane(upto, kMaskKeys / 64 - 1);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const int at = __builtin_amdgcn_readlane(upto - own, i * NW + wave);
+        const unsigned long long word = __ballot(set[i]);
+        if (set[i]) s_place[at + __builtin_amdgcn_mbcnt_hi((unsigned)(word >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)word, 0))] = (unsigned short)((i * NW + wave) * 64 + lane);
+      }
+      sync_lds();
+    } else {
+      count = here;
     }
+    const int nb = (count + KT - 1) / KT;
     // valid keys of the wavefront's part of tile j
-    bool none, all;
+    bool none;
     auto valid = [&](int j, unsigned (&bits)[NS]) {
-      none = true; all = true;
+      none = true;
 #pragma unroll
       for (int ns = 0; ns < NS; ++ns) {
-        const int at = kw * F::SUB + ns * 32, left = len - (first + j) * KT - at;
-        unsigned u = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
-        if (mask) u &= __builtin_amdgcn_readfirstlane(s_bits[((j - b0) * KT + at) / 32]);
-        bits[ns] = u;
-        none = none && u == 0;
-        all = all && u == ~0u;
-      }
-    };
-    // what a masked value holds times a probability of zero need not be zero (keys past the last one are zeros already)
-    auto clear = [&](T* tile, const unsigned (&bits)[NS]) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int r = (slot0(i) + lane) / CH - kw * F::SUB;
-        unsigned u = bits[0];
-#pragma unroll
-        for (int ns = 1; ns < NS; ++ns) u = r / 32 == ns ? bits[ns] : u;
-        if (!((u >> (r & 31)) & 1)) *reinterpret_cast<u32x4*>(tile + (slot0(i) + lane) * EC) = u32x4{0, 0, 0, 0};
+        const int left = count - j * KT - kw * F::SUB - ns * 32;
+        bits[ns] = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+        none = none && bits[ns] == 0;
       }
     };
     unsigned bits[NS];
@@ -358,13 +375,12 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     if constexpr (OWN) {
       // One buffer of either, asked for again as soon as it has been read: the next keys travel behind the softmax and the values, the next values behind the
       // scores.  (Two buffers each: half the workgroups a compute unit, and slower throughout, 16 x 4096 keys of 8 heads of 128 channels 74.0 us against 55.3.)
-      ask_k(b0);
-      ask_v(b0);
+      if (nb) { ask_k(0); ask_v(0); }
       queries_landed();
       static_assert(!OWN || NS == 1, "a wavefront has 32 keys of a tile");
       T *tk = s_k + kw * F::SUB * D, *tv = s_v + kw * F::SUB * D;
-      for (int j = b0; j < b1; ++j) {
-        const bool more = j + 1 < b1;
+      for (int j = 0; j < nb; ++j) {
+        const bool more = j + 1 < nb;
         valid(j, bits);
         wait_loads<LOADS>();
         if (!none) scores(tk, bits);
@@ -372,7 +388,6 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         if (more) { ask_k(j + 1); wait_loads<LOADS>(); }
         else wait_loads<0>();
         if (!none) {
-          if (mask && !all) { clear(s_v, bits); asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
           values_head(tv);
           softmax();
           values(tv);
@@ -382,16 +397,13 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      ask_k(b0);
-      ask_v(b0);
+      if (nb) { ask_k(0); ask_v(0); }
       queries_landed();
-      for (int j = b0; j < b1; ++j) {
+      for (int j = 0; j < nb; ++j) {
         sync_tiles();       // the tile has landed, and every wavefront is done with the other buffer
         T *tk = s_k + (j & 1) * TILE, *tv = s_v + (j & 1) * TILE;
-        if (j + 1 < b1) { ask_k(j + 1); ask_v(j + 1); }
+        if (j + 1 < nb) { ask_k(j + 1); ask_v(j + 1); }
         valid(j, bits);
-        if (none) continue;
-        if (mask && !all) { clear(tv, bits); sync_lds(); }
         if (idle) continue;
         scores(tk, bits);
         values_head(tv);
@@ -399,7 +411,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         values(tv);
       }
     }
-    b0 = b1;
+    k0 += here;
   }
 
   // ---- output.  A lane holds channels 32 dt + 8 g + 4 lk .. + 3 of its row
@@ -513,21 +525,22 @@ __global__ __launch_bounds__(256) void cross_combine_kernel(CrossLaunch launch, 
   store_quad<T>((T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head, quad * 4, a.d, num * (den == 0.f ? 0.f : 1.f / den));
 }
 
-template <typename T, int D, int QW, int KW, int KT, int WAVES>
-int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
+template <typename T, int D, int QW, int KW, int KT, int WAVES, bool MASKED>
+int cross_launch_kernel(const CrossLaunch& l, hipStream_t s) {
   using F = CrossForm<T, D, QW, KW, KT>;
-  auto kern = cross_attention_kernel<T, D, QW, KW, KT, WAVES>;
+  constexpr int smem = F::kLow + (MASKED ? F::kMask : 0);
+  auto kern = cross_attention_kernel<T, D, QW, KW, KT, WAVES, MASKED>;
   static std::atomic<unsigned long long> known{0};   // devices that the kernel's LDS has been asked for on
   int device = 0;
   WMDEC_HIP(hipGetDevice(&device));
   const unsigned long long bit = 1ull << (device & 63);
   if (!(known.load() & bit)) {
-    WMDEC_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
+    WMDEC_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, smem));
     known.fetch_or(bit);
   }
   const CrossPlan& p = l.plan;
   const long blocks = (long)l.a.n * l.a.heads * p.row_blocks, rows = blocks * F::BQ;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.splits)), dim3(F::NT), F::kSmem, s, l);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.splits)), dim3(F::NT), smem, s, l);
   WMDEC_HIP(hipGetLastError());
   if (p.splits > 1) {
     constexpr int units = 256 / (D / 4);
@@ -540,14 +553,19 @@ int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
   return WMDEC_OK;
 }
 
+template <typename T, int D, int QW, int KW, int KT, int WAVES>
+int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
+  return l.a.mask ? cross_launch_kernel<T, D, QW, KW, KT, WAVES, true>(l, s) : cross_launch_kernel<T, D, QW, KW, KT, WAVES, false>(l, s);
+}
+
 // Keys of a tile, wavefronts a SIMD: what the widest two buffers in 128 KiB allow.
 template <typename T, int D>
 int cross_launch_width(const CrossLaunch& l, hipStream_t s) {
   constexpr int bytes = D * (int)sizeof(T);   // of a key
   if constexpr (bytes <= 768) {
-    if (l.plan.few) return cross_launch_form<T, D, 1, (bytes <= 512 ? 4 : 2), (bytes <= 512 ? 128 : 64), (bytes <= 256 ? 2 : 1)>(l, s);
+    if (l.plan.few) return cross_launch_form<T, D, 1, (bytes <= 512 ? 4 : 2), (bytes <= 512 ? 128 : 64), (bytes <= (sizeof(T) == 2 ? 320 : 256) ? 2 : 1)>(l, s);
   }
-  return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (D <= 128 ? 2 : 1)>(l, s);
+  return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (sizeof(T) == 2 ? (D <= 64 ? 4 : D <= 160 ? 2 : 1) : D <= 128 ? 2 : 1)>(l, s);
 }
 
 template <typename T>
@@ -557,6 +575,7 @@ int cross_launch(const CrossLaunch& l, hipStream_t s) {
     case 64: return cross_launch_width<T, 64>(l, s);
     case 96: return cross_launch_width<T, 96>(l, s);
     case 128: return cross_launch_width<T, 128>(l, s);
+    case 160: return cross_launch_width<T, 160>(l, s);
     case 192: return cross_launch_width<T, 192>(l, s);
     default: return cross_launch_width<T, 256>(l, s);
   }

@@ -13,7 +13,7 @@ namespace {
 // Nothing here looks at the number of samples, so that the bits of a sample do not depend on what it is batched with.
 CrossPlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   CrossPlan p;
-  p.width = d <= 128 ? (d + 31) / 32 * 32 : d <= 192 ? 192 : 256;
+  p.width = d <= 192 ? (d + 31) / 32 * 32 : 256;
   p.rows = tq * group;
   const int bytes = p.width * (int)dtype_size(dtype);   // of a key
   auto blocks = [&](int bq) { return (long)heads * ((p.rows + bq - 1) / bq); };
@@ -24,10 +24,10 @@ CrossPlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   p.few = bytes <= 768 && (p.rows <= 32 || (dtype == WMDEC_F32 && bytes <= 512 && blocks(128) <= (bytes <= 256 ? 128 : 64)));
   const int bq = p.few ? 32 : 128;
   p.row_blocks = (p.rows + bq - 1) / bq;
-  // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow).
+  // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow; a mask takes 4 KB more, which 160 channels in 16 bits do not have twice).
   // us without / with ranges: 4 rows a key head against 32768 keys of 8 heads of 128 in bf16 247 / 28, 200 rows against 4096 of 8 of 64 in f16 62.5 / 17.2.
   const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
-  const int slots = 256 * std::min(160 * 1024 / (tiles + 4096), !p.few && p.width <= 64 ? 4 : 2);
+  const int slots = 256 * std::min(160 * 1024 / tiles, !p.few && p.width <= 64 ? 4 : 2);
   // (at 128 and 512 keys instead of 256 the second takes 20.2 and 18.5; fp32, 128 and 64 instead of 256: 5 rows against 4 x 699 keys of 10 heads of 256 113 / 71, but with
   // shared rows of up to 512 bytes 333x301 of 8 of 72 20 / 31)
   const long range = dtype != WMDEC_F32 || (p.few && bytes <= 512) ? 256 : p.few ? 128 : 64;   // fewest keys of a range: two tiles, or what is worth a launch

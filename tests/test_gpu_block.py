@@ -410,6 +410,53 @@ def test_cross_masks(dtype, d, tq):
     run_cross(dtype, 5, tq, tk, 4, 2, d, lens=[333, 333, 60, 150, 299], mask=mask.astype(np.uint8) * 255, seed=3)
 
 
+@pytest.mark.parametrize("tq", [1, 33])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_cross_masks_of_long_states(dtype, tq):
+    """Many heads, so that a range of keys is as long as they are or half as long: its mask is read in parts, of which the second has nothing, or one key."""
+    mask = rng(10).random((1, 5003)) < 0.5
+    mask[:, 2048:4096] = False
+    run_cross(dtype, 1, tq, 5003, 512, 512, 8, mask=mask, seed=4)
+    mask[:, 4095] = True
+    run_cross(dtype, 1, tq, 5003, 512, 512, 8, lens=[4999], mask=mask, seed=5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_cross_masked_keys_might_as_well_not_be_there(dtype):
+    """The same bits as without the masked keys, where all keys are one range."""
+    for tq, d in ((1, 64), (200, 64), (4, 128), (40, 160), (90, 256)):
+        q, k, v = (torch.randn(s, device="cuda").to(G.TORCH[dtype]) for s in ((2, tq, 4, d), (2, 127, 2, d), (2, 127, 2, d)))
+        keep = torch.zeros(127, dtype=torch.bool, device="cuda")
+        keep[torch.randperm(127, device="cuda")[:83]] = True
+        outs = []
+        for kk, vv, mask in ((k, v, keep.expand(2, 127).contiguous()), (k[:, keep].contiguous(), v[:, keep].contiguous(), None),
+                             (k[:, keep].contiguous(), v[:, keep].contiguous(), torch.ones((2, 83), dtype=torch.bool, device="cuda"))):
+            o = torch.empty_like(q)
+            need = wmdec.cross_attention_workspace_bytes(q, kk)
+            wmdec.cross_attention(q, kk, vv, o, 0.1, key_mask=mask, workspace=torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"))
+            outs.append(o)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_cross_masked_keys_far_apart():
+    """8 MB from token to token: less than 256 of them are within reach of one address."""
+    tk, step, d = 300, 1 << 22, 64
+    big = torch.zeros(tk * step, dtype=torch.float16, device="cuda")
+    k, v = (big[at:].as_strided((1, tk, 2, d), (tk * step, step, d, 1)) for at in (0, 4 * d))
+    k.copy_(torch.randn((1, tk, 2, d), device="cuda"))
+    v.copy_(torch.randn((1, tk, 2, d), device="cuda"))
+    mask = torch.rand((1, tk), device="cuda") < 0.7
+    for tq in (1, 64):
+        q = torch.randn((1, tq, 2, d), device="cuda").half()
+        o, near = torch.empty_like(q), torch.empty_like(q)
+        need = wmdec.cross_attention_workspace_bytes(q, k)
+        for kk, vv, out in ((k, v, o), (k.contiguous(), v.contiguous(), near)):
+            wmdec.cross_attention(q, kk, vv, out, 0.1, key_mask=mask, workspace=torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"))
+        want, weighted = ref.cross_attention(host(q), host(k), host(v), float(np.float32(0.1)), None, mask.cpu().numpy())
+        for out in (o, near):
+            assert_within(host(out), want, cross_tolerance("f16", host(q), host(k), want, weighted, 0.1, tk, host(v)))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_cross_grouped_heads_and_long_states(dtype):
     for tq, hq, hk in ((1, 32, 8), (1, 7, 1), (5, 8, 1), (3, 40, 2), (2, 128, 1)):
