@@ -279,8 +279,10 @@ int wmdec_adaln_fused_projection(const void* c, int c_dtype, const void* w_fused
  * x, x_out: dense [n,t,d] of x_dtype; h, y: of act_dtype.  x_dtype is act_dtype or
  * F32 (a residual stream in fp32 beside 16-bit blocks).  x_out may be x, and y may
  * be h (or x, where h is NULL and the types are the same); nothing else may
- * overlap.  All arithmetic is fp32.  d at most 16384.  Pointers need the alignment of their elements;
- * rows that are 16-byte aligned (d % 8 == 0) are read in vectors. */
+ * overlap.  All arithmetic is fp32.  d at most 16384, n * t at
+ * most 2^31 - 2^20, n at most 2^22 where samples have vectors of their own.
+ * Pointers need the alignment of their elements; rows that are 16-byte aligned
+ * (d % 8 == 0) are read in vectors. */
 typedef enum { WMDEC_NORM_NONE = 0, WMDEC_NORM_LAYER = 1, WMDEC_NORM_RMS = 2 } wmdec_norm_kind;
 typedef struct {
   int kind;
@@ -312,9 +314,11 @@ int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype
  * the gradient of the operator.  q, k: [n, t, heads, d] through strides in
  * elements, channels contiguous (parts of a fused projection need no copy); k may
  * be NULL.  Outputs may be the inputs themselves (same pointer and strides); no
- * other overlap, and no stride of zero over several tokens, heads or samples.  positions: int32 [t][axes], positions_stride elements from
- * sample to sample (0: the same for all).  1 to 3 axes.  Rotations are exact to
- * fp32 for every int32 position; one rounding to dtype. */
+ * other overlap, and no stride of zero over several tokens, heads or samples.
+ * positions: int32 [t][axes], positions_stride elements from sample to sample (0:
+ * the same for all).  1 to 3 axes, at most 4096 rotated of 16384 channels, 16384
+ * heads of q and k, 2^31 - 2^20 tokens.  Rotations are exact to fp32 for every int32
+ * position; one rounding to dtype. */
 typedef enum { WMDEC_ROPE_PLAIN = 0, WMDEC_ROPE_LINEAR = 1, WMDEC_ROPE_BASE = 2, WMDEC_ROPE_RAMP = 3 } wmdec_rope_scaling_kind;
 typedef struct {
   int kind;
@@ -349,7 +353,9 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
  * q, o: [n,tq,heads_q,d], k, v: [n,tk,heads_kv,d] of dtype through strides in
  * elements, channels contiguous.  d: a multiple of 8 (16-bit types) or 4 (F32), at
  * most 256; pointers and strides multiples of 16 bytes; 128 tokens of k or v span
- * less than 2 GiB.  scale > 0.  o must not overlap the inputs or itself.
+ * less than 2 GiB.  A launch of 2^24 workgroups (32 or 128 rows of a key head and a
+ * range of its keys each) or more is refused.  scale > 0.  o must not overlap the
+ * inputs or itself.
  * Scores, softmax and sums are fp32; 16-bit types round the probabilities to dtype
  * for the second product.  F32 is fp32 throughout.  A sample's bits do not depend
  * on what it is batched with.

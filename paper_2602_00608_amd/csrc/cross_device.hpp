@@ -1,6 +1,7 @@
 // The kernel of kernels_cross.hip: attention of rows (a token of one of the query heads that share a key head) to the keys of a sample.
 //
-// Tiles of KT keys and values stream through two LDS buffers, straight from memory (16 bytes a lane), while the tile before is worked on.  Per 32 keys a
+// Tiles of KT keys and values stream through LDS, straight from memory (16 bytes a lane), while the tile before is worked on.  With a mask a tile is made of
+// valid keys alone: a lane chooses what it reads, so their places are worked out first and the others are neither read nor reckoned with.  Per 32 keys a
 // wavefront forms S^T = K Q^T (keys along the accumulator's registers, one row a lane), the softmax against a running maximum, and O^T += V^T P^T with the
 // probabilities as they are in their registers: an accumulator's keys of lane half lk are 8 (r / 4) + 4 lk + r % 4, so V^T is read from LDS in that order of
 // keys (16-bit types: transposed on the way, four keys of one channel a lane).  fp32 takes the same steps with 32x32x2 products.
@@ -12,14 +13,17 @@
 // What bounds it.  Few rows: the one read of the keys and values; two workgroups of 32 rows a compute unit, with 128 KB of tiles under way.  Many rows in
 // 16 bits: the power that the matrix cores may draw, and at 64 channels the exponentials, which take as many cycles as the products (32 rows and 64 keys of a
 // wavefront: 16 products of 32 cycles, 32 exponentials of 8 beside 32 each of multiply-add, add and half a maximum and a conversion).  fp32: its products.
-// Rates: one token of 32 heads against 16 x 4096 keys of 8 heads of 128 in bf16 55.3 us = 4.86 TB/s; 8192x8192 of 32 / 8 heads of 128 1123 us = 979 TFLOP/s (a large
-// library product on this card 1090 to 1150); 5400x5400 of 30 heads of 64 in f16 290 to 304 us = 736 to 771, of 96 heads 870 to 890 (1290 workgroups are 1.26 rounds of
+// Rates: one token of 32 heads against 16 x 4096 keys of 8 heads of 128 in bf16 55.3 us = 4.86 TB/s; 8192x8192 of 32 / 8 heads of 128 1045 us = 1050 TFLOP/s (a large
+// library product on this card 1090 to 1150); 5400x5400 of 30 heads of 64 280 to 300 us = 746 to 800, of 96 heads 870 to 890 (1290 workgroups are 1.26 rounds of
 // the 1024 that run at once); fp32 4000x2000 of 8 heads of 128 263 us = 125 of 155.
 // Steps, us for 5400x5400 of 30 of 64 f16, 2 x 5400x512 of 30 of 64 bf16 (two lengths), 1 token against 4 x 32768 (ragged) of 8 of 128: a wavefront a row 92950, 9854,
 // 50355; matrix cores, tiles through LDS, transposed reads 298, 66, 128; tiles by instructions that the compiler does not wait for 298, 66, 110; 128 rows a workgroup
-// and the XCDs divided within a sample 297, 50, 65; wavefronts past the last row idle 290, 50, 65.
+// and the XCDs divided within a sample 297, 50, 65; wavefronts past the last row idle 290, 50, 65.  With a fifth of the keys masked, by a mask on the scores and zeros in place of masked values / by tiles of valid
+// keys: 5400x5400 of 30 of 64 in bf16 361 / 240 (280 without a mask), 4096x4096 of 16 of 128 168 / 119, 333x301 of 8 of 72 in fp32 20.0 / 16.4.  160 channels as 192 / as
+// themselves, with two workgroups a compute unit: 4000x4000 of 30 heads in f16 528 / 338.
 // Measured and not kept: 64 rows a wavefront (128 channels 818 TFLOP/s against 1005: half the wavefronts), wave priorities around the products, the compiler's own
-// interleaving of them, sums by dot products (4 cycles against 2), a loop over pairs of tiles, ranges for the last round's blocks alone (partial outputs cost what
+// interleaving of them, sums by dot products (4 cycles against 2), a loop over pairs of tiles, tiles of 32 keys and three workgroups a compute unit at 128 channels (8192x8192 1026
+// against 1045, but 4096x4096 of 16 heads 168 against 158), ranges for the last round's blocks alone (partial outputs cost what
 // they gain).
 #pragma once
 #include <atomic>
