@@ -110,10 +110,21 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   // workgroup id -> (sample, key head, range of keys, row block); within a sample the ids of one XCD (id % 8) are neighbours and share their keys.  (Neighbours over
   // all samples: an XCD had one sample's work, and where samples have different lengths those with long ones ran alone.)
   const CrossPlan& p = launch.plan;
-  const int per_sample = a.heads * p.splits * p.row_blocks, n = blockIdx.x / per_sample;
+  const int per_sample = a.heads * p.splits * p.row_blocks, turn = blockIdx.x / per_sample;
+  // Samples of many blocks come longest first (a short one's workgroups end the launch sooner together).
+  int n = turn;
+  if (KW == 1 && a.lens && a.n > 1 && a.n <= 64) {
+    const int mine = lane < a.n ? min(max(a.lens[lane], 0), a.tk) : -1;
+    int before = 0;
+    for (int j = 0; j < a.n; ++j) {
+      const int other = __builtin_amdgcn_readlane(mine, j);
+      before += other > mine || (other == mine && j < lane);
+    }
+    n = __builtin_ctzll(__ballot(before == turn));
+  }
   int L;
   {
-    const int i = blockIdx.x - n * per_sample, per = per_sample / 8, rem = per_sample % 8, x = i % 8, j = i / 8;
+    const int i = blockIdx.x - turn * per_sample, per = per_sample / 8, rem = per_sample % 8, x = i % 8, j = i / 8;
     L = x * per + (x < rem ? x : rem) + j;
   }
   const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits);
