@@ -1,6 +1,7 @@
 // Attention to states of another length: o = softmax(scale * q k^T over the valid keys) v.  The kernels are in cross_device.hpp; here is what is decided on
 // sizes alone, and the f16 kernels.
 #include <algorithm>
+#include <cmath>
 
 #include "cross_device.hpp"
 
@@ -24,14 +25,23 @@ CrossPlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   p.few = bytes <= 768 && (p.rows <= 32 || (dtype == WMDEC_F32 && bytes <= 512 && blocks(128) <= (bytes <= 256 ? 128 : 64)));
   const int bq = p.few ? 32 : 128;
   p.row_blocks = (p.rows + bq - 1) / bq;
-  // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers allow; a mask takes 4 KB more, which 160 channels in 16 bits do not have twice).
-  // us without / with ranges: 4 rows a key head against 32768 keys of 8 heads of 128 in bf16 247 / 28, 200 rows against 4096 of 8 of 64 in f16 62.5 / 17.2.
+  // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers
+  // allow; a mask takes 4 KB more, which 160 channels in 16 bits do not have twice).
+  // us without / with ranges: 4 rows a key head against 32768 keys of 8 heads of 128 in bf16 247 / 28, 200 rows against 4096 of 8 of 64 in f16 62.5 / 18.1.
   const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
   const int slots = 256 * std::min(160 * 1024 / tiles, !p.few && p.width <= 64 ? 4 : 2);
-  // (at 128 and 512 keys instead of 256 the second takes 20.2 and 18.5; fp32, 128 and 64 instead of 256: 5 rows against 4 x 699 keys of 10 heads of 256 113 / 71, but with
-  // shared rows of up to 512 bytes 333x301 of 8 of 72 20 / 31)
+  // (bf16, 128, 256 or 512 keys: 4 x 1024 of 8 of 128 11.7, 12.2, 12.8; fp32, 128 and 64 instead of 256: 5 rows against 4 x 699 keys of 10 heads of 256 113 / 71, but
+  // with shared rows of up to 512 bytes 333x301 of 8 of 72 20 / 31)
   const long range = dtype != WMDEC_F32 || (p.few && bytes <= 512) ? 256 : p.few ? 128 : 64;   // fewest keys of a range: two tiles, or what is worth a launch
   p.splits = (int)std::max(1L, std::min({slots / blocks(bq), tk / range, (long)kCrossMaxSplits}));
+  if (!p.few && p.splits > 1) {
+    // Partial outputs of 128 rows weigh: s ranges take a / s for their keys, b * s for writing and reading what they leave, and the second launch.  (b counts half as
+    // much again as one sample alone has, for batches.)  us, ranges as slots allow / so: f16 1000x1000 of 16 / 4 heads of 128 39 / 28, four samples 82 / 46, 2000x2000 of 8
+    // of 128 46 / 48, three samples 95 / 72, 700x3000 of 4 of 96 27 / 25, three 54 / 45, 150x8000 of 4 of 64 15.2 / 16.7; fp32 257x893 of 8 / 2 of 160 37 / 40, three 80 / 74.
+    const double a = (dtype == WMDEC_F32 ? 1e-3 : 1.8e-4) * tk * p.width, b = 1.2e-6 * 512 * p.width * blocks(bq);   // us
+    p.splits = std::min(p.splits, (int)std::sqrt(a / b));
+    if (p.splits < 2 || a - a / p.splits < 5 + b * p.splits) p.splits = 1;
+  }
   return p;
 }
 
