@@ -580,7 +580,7 @@ int cross_launch_width(const CrossLaunch& l, hipStream_t s) {
   if constexpr (bytes <= 768) {
     if (l.plan.few) return cross_launch_form<T, D, 1, (bytes <= 512 ? 4 : 2), (bytes <= 512 ? 128 : 64), (bytes <= (sizeof(T) == 2 ? 320 : 256) ? 2 : 1)>(l, s);
   }
-  return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (sizeof(T) == 2 ? (D <= 64 ? 4 : D <= 160 ? 2 : 1) : D <= 128 ? 2 : 1)>(l, s);
+  return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (sizeof(T) == 2 ? (D <= 64 ? 4 : D <= 160 ? 2 : 1) : D <= 160 ? 2 : 1)>(l, s);
 }
 
 template <typename T>
