@@ -19,7 +19,7 @@
 // Steps, us for 5400x5400 of 30 of 64 f16, 2 x 5400x512 of 30 of 64 bf16 (two lengths), 1 token against 4 x 32768 (ragged) of 8 of 128: a wavefront a row 92950, 9854,
 // 50355; matrix cores, tiles through LDS, transposed reads 298, 66, 128; tiles by instructions that the compiler does not wait for 298, 66, 110; 128 rows a workgroup
 // and the XCDs divided within a sample 297, 50, 65; wavefronts past the last row idle 290, 50, 65.  With a fifth of the keys masked, by a mask on the scores and zeros in place of masked values / by tiles of valid
-// keys: 5400x5400 of 30 of 64 in bf16 361 / 240 (280 without a mask), 4096x4096 of 16 of 128 168 / 119, 333x301 of 8 of 72 in fp32 20.0 / 16.4.  160 channels as 192 / as
+// keys: 5400x5400 of 30 of 64 in bf16 361 / 240 (280 without a mask), 4096x4096 of 16 of 128 168 / 117, 333x301 of 8 of 72 in fp32 20.0 / 15.3.  160 channels as 192 / as
 // themselves, with two workgroups a compute unit: 4000x4000 of 30 heads in f16 528 / 338.
 // Measured and not kept: 64 rows a wavefront (128 channels 818 TFLOP/s against 1005: half the wavefronts), wave priorities around the products, the compiler's own
 // interleaving of them, sums by dot products (4 cycles against 2), a loop over pairs of tiles, tiles of 32 keys and three workgroups a compute unit at 128 channels (8192x8192 1026
@@ -149,7 +149,18 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     voff[i] = c * EC < a.d ? (unsigned)((MASKED ? 0 : r * vstep) + c * 16) : kPastEnd;
   }
   int k0 = begin, count = 0;   // the keys at work: `count` from k0 on, or the valid ones among those from k0 on
-  auto ask = [&](const char* base, int step, const unsigned (&off)[PER], int at, int j) {
+  constexpr int PLACES = MASKED ? LOADS : 1;
+  // Outputs and queries of 256 channels leave no registers for a lane's chunks and keys: worked out for every tile, from a lane number that the compiler does not know.
+  constexpr bool AGAIN = MASKED && !WIDE && D == 256 && !OWN;
+  auto keys_of = [&](int j, int& ln, unsigned (&place)[PLACES]) {
+    ln = lane;
+    if constexpr (AGAIN) asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(ln));
+    if constexpr (MASKED) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) place[i] = s_place[j * KT + (slot0(i) + ln) / CH];   // (past the last one: below kMaskKeys still, and not used)
+    }
+  };
+  auto ask = [&](const char* base, int step, const unsigned (&off)[PER], int at, int j, int ln, const unsigned (&place)[PLACES]) {
     const int left = count - j * KT;
     const uint64_t from = (uint64_t)(base + (k0 + (MASKED ? 0L : (long)j * KT)) * step);
     const u32x4 buffer{(unsigned)from, (unsigned)(from >> 32) & 0xffffu, kPastEnd - 1, 0x00020000u};
@@ -161,15 +172,35 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         more += PER * ROWS * step;
         asm volatile("" : "+s"(more));   // (one after the other: worked out beforehand for all loads they do not fit the scalar registers)
       }
-      unsigned o = off[i % PER];
-      const int r = (slot0(i) + lane) / CH;
-      if constexpr (MASKED) o = r < left ? o + s_place[j * KT + r] * (unsigned)step : kPastEnd;   // (below 2^32: a place times the step is below 2^31)
+      const int r = (slot0(i) + ln) / CH;
+      unsigned o;
+      if constexpr (AGAIN) {
+        const int c = ((slot0(i) + ln) % CH) ^ chunk_turn<CH>(r);
+        o = c * EC < a.d ? (unsigned)(c * 16) : kPastEnd;
+      } else {
+        o = off[i % PER];
+      }
+      if constexpr (MASKED) o = r < left ? o + place[i] * (unsigned)step : kPastEnd;   // (below 2^32: a place times the step is below 2^31)
       else if (left < KT) o = r < left ? o : kPastEnd;
       load_to_lds<i * (OWN ? 1 : NW) * 1024>(buffer, o, more, to);
     });
   };
-  auto ask_k = [&](int j) { ask(kp, kstep, koff, 0, j); };
-  auto ask_v = [&](int j) { ask(vp, vstep, voff, NB * TILE, j); };
+  auto ask_one = [&](bool values, int j) {
+    int ln;
+    unsigned place[PLACES];
+    keys_of(j, ln, place);
+    if (values) ask(vp, vstep, voff, NB * TILE, j, ln, place);
+    else ask(kp, kstep, koff, 0, j, ln, place);
+  };
+  auto ask_k = [&](int j) { ask_one(false, j); };
+  auto ask_v = [&](int j) { ask_one(true, j); };
+  auto ask_both = [&](int j) {
+    int ln;
+    unsigned place[PLACES];
+    keys_of(j, ln, place);
+    ask(kp, kstep, koff, 0, j, ln, place);
+    ask(vp, vstep, voff, NB * TILE, j, ln, place);
+  };
 
   // ---- queries: chunk 2 s + lk of the lane's row
   const int row = rb * F::BQ + qw * 32 + l32;
@@ -412,12 +443,12 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      if (nb) { ask_k(0); ask_v(0); }
+      if (nb) ask_both(0);
       queries_landed();
       for (int j = 0; j < nb; ++j) {
         sync_tiles();       // the tile has landed, and every wavefront is done with the other buffer
         T *tk = s_k + (j & 1) * TILE, *tv = s_v + (j & 1) * TILE;
-        if (j + 1 < nb) { ask_k(j + 1); ask_v(j + 1); }
+        if (j + 1 < nb) ask_both(j + 1);
         valid(j, bits);
         if (idle) continue;
         scores(tk, bits);
@@ -573,14 +604,16 @@ int cross_launch_form(const CrossLaunch& l, hipStream_t s) {
   return l.a.mask ? cross_launch_kernel<T, D, QW, KW, KT, WAVES, true>(l, s) : cross_launch_kernel<T, D, QW, KW, KT, WAVES, false>(l, s);
 }
 
-// Keys of a tile, wavefronts a SIMD: what the widest two buffers in 128 KiB allow.
+// Keys of a tile, wavefronts a SIMD.  Where 128 rows have a workgroup: 64 keys in 16 bits while the tiles of two workgroups fit a compute unit (up to 160 channels), else 32
+// (us, 64 keys and one workgroup / 32 and two: 3 x 4096x4096 of 16 heads of 256 in bf16 1088 / 792, 3 x 3000x3000 of 16 of 192 in f16 459 / 362).  fp32: 64 up to 128 channels,
+// where 32 and two workgroups gain nothing (2000x2000 of 8 of 128 154 / 150, 3 x 2402x1124 of 8 / 2 of 72 111 / 129), else 32.
 template <typename T, int D>
 int cross_launch_width(const CrossLaunch& l, hipStream_t s) {
   constexpr int bytes = D * (int)sizeof(T);   // of a key
   if constexpr (bytes <= 768) {
     if (l.plan.few) return cross_launch_form<T, D, 1, (bytes <= 512 ? 4 : 2), (bytes <= 512 ? 128 : 64), (bytes <= (sizeof(T) == 2 ? 320 : 256) ? 2 : 1)>(l, s);
   }
-  return cross_launch_form<T, D, 4, 1, (bytes <= 512 ? 64 : 32), (sizeof(T) == 2 ? (D <= 64 ? 4 : D <= 160 ? 2 : 1) : D <= 160 ? 2 : 1)>(l, s);
+  return cross_launch_form<T, D, 4, 1, (bytes <= (sizeof(T) == 2 ? 320 : 512) ? 64 : 32), (sizeof(T) == 2 && D <= 64 ? 4 : bytes <= 640 ? 2 : 1)>(l, s);
 }
 
 template <typename T>

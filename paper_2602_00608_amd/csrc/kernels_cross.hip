@@ -28,7 +28,7 @@ CrossPlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   // Ranges of keys, where blocks are fewer than workgroups run at once: as many as tiles fit into the LDS of a compute unit (and four, or what the registers
   // allow; a mask takes 4 KB more, which 160 channels in 16 bits do not have twice).
   // us without / with ranges: 4 rows a key head against 32768 keys of 8 heads of 128 in bf16 247 / 28, 200 rows against 4096 of 8 of 64 in f16 62.5 / 18.1.
-  const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= 512 ? 64 : 32) * 4 * bytes;
+  const int tiles = p.few ? (bytes <= 512 ? 128 : 64) * 2 * bytes : (bytes <= (dtype == WMDEC_F32 ? 512 : 320) ? 64 : 32) * 4 * bytes;
   const int slots = 256 * std::min(160 * 1024 / tiles, !p.few && p.width <= 64 ? 4 : 2);
   // (bf16, 128, 256 or 512 keys: 4 x 1024 of 8 of 128 11.7, 12.2, 12.8; fp32, 128 and 64 instead of 256: 5 rows against 4 x 699 keys of 10 heads of 256 113 / 71, but
   // with shared rows of up to 512 bytes 333x301 of 8 of 72 20 / 31)
