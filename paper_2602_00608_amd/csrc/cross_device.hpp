@@ -7,8 +7,9 @@
 // keys (16-bit types: transposed on the way, four keys of one channel a lane).  fp32 takes the same steps with 32x32x2 products.
 // The wavefronts of a workgroup take 32 rows each (QW of them), or, where there are few rows, the same rows and a part of a tile's keys (KW), joined at the end.
 //
-// 16-byte chunk c of key r lies at chunk c ^ turn(r) of its row in LDS: the eight lanes of a pass over K (eight keys, one chunk) and the sixteen over V (four
-// keys, two chunks) then have banks of their own.  The loads bring the chunks in that order, as a lane chooses what it reads and not where it lands.
+// 16-byte chunk c of key r lies at chunk c ^ turn(r) of its row in LDS: eight neighbouring lanes over K (eight keys, one chunk) and sixteen over V (four keys, two
+// chunks) then have banks of their own.  (Twice as many lanes do not: a third of the LDS cycles at 64 channels and half at 128 are conflicts.  A turn of 32 keys that
+// frees V of them, half of those at 128, is no faster: 3 x 4096x4096 of 16 heads 474 / 474 us.)  The loads bring the chunks in that order, as a lane chooses what it reads and not where it lands.
 //
 // What bounds it.  Few rows: the one read of the keys and values; two workgroups of 32 rows a compute unit, with 128 KB of tiles under way.  Many rows in
 // 16 bits: the power that the matrix cores may draw, and at 64 channels the exponentials, which take as many cycles as the products (32 rows and 64 keys of a
