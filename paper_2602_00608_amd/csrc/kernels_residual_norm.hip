@@ -57,12 +57,13 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int
       if (e < count) p[e * gap] = t[e];
   }
 }
-// eight of a vector that may be missing
+// Eight of a vector that may be missing.  Places past the row's end get zeros either way: what a norm makes of them (minus its mean) is multiplied by these, and
+// has to be nothing in the next norm's sums.
 template <bool VEC> __device__ __forceinline__ void vector8(const float* p, long at, int count, int gap, float missing, float (&v)[E]) {
   if (p) load8<float, VEC>(p + at, count, gap, v);
   else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = missing;
+    for (int e = 0; e < E; ++e) v[e] = (VEC ? count > 0 : e < count) ? missing : 0.f;
   }
 }
 

@@ -127,6 +127,16 @@ def test_residual_norm_parts(post, pre, mod):
         run_norm("bf16", "bf16", 2, 5, d, "none", pre, residual=False, mod=mod, seed=7)
 
 
+@pytest.mark.parametrize("xdt, adt", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("f32", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("d", [7, 40, 72, 320, 379, 1000, 1001, 1152, 1920, 4104, 8200])
+def test_residual_norm_of_a_bare_post_norm(xdt, adt, d):
+    """No weight, no bias, no gate: what a row's last lanes hold past its channels is no part of the next norm."""
+    for post, pre in (("layer-", "layer"), ("layer-", "layer-"), ("layer-", "rms-"), ("rms-", "layer-")):
+        for mean in (0.0, 5.0):
+            for offset in (0, 1):
+                run_norm(xdt, adt, 2, 5, d, post, pre, mod=None, mean=mean, offset=offset, seed=20)
+
+
 def test_residual_norm_unaligned_in_place_and_far_from_zero():
     for offset in (1, 4, 8):
         run_norm("bf16", "bf16", 2, 5, 640, "layer", "layer", offset=offset, seed=8)
