@@ -305,6 +305,19 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
         }
       }
   };
+  // The reference is a rounded product.  From 2^24 on a fused multiply-add would find the largest score half a step of the reference away from it, 1 and more: its
+  // probability is not 1 but anything between none and infinity.  There the products are rounded like the reference, and then subtracted.
+  bool far = false;   // (of any of the wavefront's rows)
+  auto round_and_subtract = [&](float ref) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = s[ns][r] * c;
+        s[ns][r] = x - ref;
+      }
+  };
   // The reference moves when a maximum exceeds it by 2^kCrossSlack; until then probabilities may reach that, well inside the 16-bit types.
   auto softmax = [&]() {
     float mx = maximum(maximum(s[0][0], s[0][1]), s[0][2]);
@@ -316,18 +329,24 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     if (__ballot(moves)) {
       const float to = moves ? mx : m, factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
       m = to;
+      far = __ballot(fabsf(m) >= 0x1p24f && m != -INFINITY) != 0;
       l *= factor;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= factor;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    float ref = m == -INFINITY ? 0.f : m, by = c;
+    if (far) {
+      round_and_subtract(ref);
+      by = 1.f;
+      ref = 0.f;
+    }
 #pragma unroll
     for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[ns][r] = __builtin_amdgcn_exp2f(fmaf(s[ns][r], c, -ref));
+        s[ns][r] = __builtin_amdgcn_exp2f(fmaf(s[ns][r], by, -ref));
         l += s[ns][r];
       }
   };

@@ -504,6 +504,33 @@ def test_cross_scores_of_any_size(dtype):
             assert_within(host(o), want, cross_tolerance(dtype, q, k, want, weighted, 1.0, tk, v))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tq, tk", [(1, 1), (1, 700), (150, 700), (300, 70)])
+def test_cross_scores_past_24_bits(dtype, tq, tk):
+    """Scores so large that fp32 holds no fraction of them.  Keys that are alike have the same score to the bit, those of the other sign are out of reach, so the
+    output is the plain mean of the values with the higher score; rows with ordinary scores stand between.  (No bound of the scores' own error: those that count are
+    alike.  What is left is the sum and quotient in fp32 and the roundings to dtype, as in cross_tolerance.)"""
+    r = rng(310)
+    h, d = 2, 64
+    v = G.stored(r.standard_normal((1, tk, h, d)), dtype)
+    sign = np.where(r.random((1, tk, 1, 1)) < 0.5, 1.0, -1.0) * np.ones((1, tk, h, d))
+    for size, scale in ((7.68e10, 1.0), (7.68e10, 0.3), (3.1e9, 0.125), (3.1e9, 0.0884), (4.7e8, 0.7), (4.7e8, 1.0)) + (((1e30, 0.9), (1e36, 0.11)) if dtype != "f16" else ()):
+        size, scale = math.sqrt(size / d), float(np.float32(scale))
+        for signs in (sign, np.ones_like(sign), -np.ones_like(sign)):
+            q, k = G.stored(np.full((1, tq, h, d), size), dtype), G.stored(size * signs, dtype)
+            q[:, 1::3] /= np.float32(2.0) ** np.ceil(2 * np.log2(np.float32(size)) + 9)         # (a power of two; scores below 1, where they do not vanish)
+            q = G.stored(q, dtype)
+            qd, kd, vd = dev(q, dtype), dev(k, dtype), dev(v, dtype)
+            o = torch.empty_like(qd)
+            need = wmdec.cross_attention_workspace_bytes(qd, kd)
+            wmdec.cross_attention(qd, kd, vd, o, scale, workspace=torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"))
+            want, weighted = ref.cross_attention(q, k, v, scale)
+            tol = HALF[dtype] * np.abs(want) + TINY[dtype] + ((math.sqrt(tk) + 64) * 2 * U + (HALF[dtype] * 1.01 if dtype != "f32" else 0.0) + 2 * (d + 8) * U) * weighted
+            if dtype == "f16":
+                tol = tol + TINY["f16"] * float(np.abs(v).sum(1).max())
+            assert_within(host(o), want, tol)
+
+
 def test_cross_not_a_number_in_valid_places():
     for tq, dtype in ((1, "bf16"), (100, "bf16"), (1, "f32"), (100, "f32")):
         q, k, v = (torch.randn(s, device="cuda").to(G.TORCH[dtype]) for s in ((1, tq, 2, 64), (1, 90, 2, 64), (1, 90, 2, 64)))
