@@ -27,6 +27,7 @@
 // against 1045, but 4096x4096 of 16 heads 168 against 158), ranges for the last round's blocks alone (partial outputs cost what
 // they gain).
 #pragma once
+#include <algorithm>
 #include <atomic>
 
 #include "conv_device.hpp"
@@ -540,55 +541,59 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
   }
 }
 
-// o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) for the rows of the blocks that are split.  A thread takes four channels of a row and every groups-th
-// range, eight at a time; the groups of a row are joined in order.  Bound by latency: one trip for up to 8 * groups ranges, 3 to 6 us.
+// o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) for the rows of the blocks that are split (`total` of all key heads, `bq` a block).  A thread takes four
+// channels of a row and every groups-th range, eight at a time; the groups of a row are joined in order.  Bound by latency: one trip.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_combine_kernel(CrossLaunch launch, int bq, int groups) {
+__global__ __launch_bounds__(256) void cross_combine_kernel(CrossLaunch launch, int bq, int groups, unsigned total) {
   constexpr int QUADS = D / 4, UNITS = 256 / QUADS, B = 8;
   __shared__ f32x4 s_num[UNITS][QUADS];
   __shared__ float2 s_ml[UNITS];
   const CrossArgs& a = launch.a;
   const CrossPlan& p = launch.plan;
   const int unit = threadIdx.x / QUADS, quad = threadIdx.x % QUADS, g = unit % groups, in_block = UNITS / groups;
-  const long r = (long)blockIdx.x * in_block + unit / groups;                     // row among those of all blocks
-  const long pb = r / bq, nh = pb / p.row_blocks;
-  const int in = (int)(r - pb * bq), n = (int)(nh / a.heads), h = (int)(nh - (long)n * a.heads), row = (int)(pb - nh * p.row_blocks) * bq + in;
-  const bool there = unit < in_block * groups && n < a.n && row < p.rows;
-  float top = -INFINITY, den = 0.f;
-  f32x4 num{0.f, 0.f, 0.f, 0.f};
-  auto join = [&](float m, float l, f32x4 v) {
-    const float now = fmaxf(top, m), keep = weight_of(top, now), f = weight_of(m, now);
-    den = den * keep + l * f;
-    num = num * keep + v * f;
-    top = now;
-  };
-  if (there && quad * 4 < a.d) {
-    for (int s0 = g; s0 < p.splits; s0 += B * groups) {
-      float2 e[B];
-      f32x4 v[B];
+  for (unsigned r0 = blockIdx.x * in_block; r0 < total; r0 += gridDim.x * in_block) {
+    const unsigned r = r0 + unit / groups, nh = r / p.rows;                          // row among those of all key heads, its sample and key head
+    const int row = (int)(r - nh * p.rows), n = nh / a.heads, h = nh - n * a.heads, in = row % bq;
+    const long pb = (long)nh * p.row_blocks + row / bq;
+    const bool there = unit < in_block * groups && r < total;
+    float top = -INFINITY, den = 0.f;
+    f32x4 num{0.f, 0.f, 0.f, 0.f};
+    auto join = [&](float m, float l, f32x4 v) {
+      const float now = fmaxf(top, m), keep = weight_of(top, now), f = weight_of(m, now);
+      den = den * keep + l * f;
+      num = num * keep + v * f;
+      top = now;
+    };
+    if (there && quad * 4 < a.d) {
+      for (int s0 = g; s0 < p.splits; s0 += B * groups) {
+        float2 e[B];
+        f32x4 v[B];
 #pragma unroll
-      for (int b = 0; b < B; ++b) {
-        const long at = (pb * p.splits + min(s0 + b * groups, p.splits - 1)) * bq + in;
-        e[b] = launch.ml[at];
-        v[b] = *reinterpret_cast<const f32x4*>(launch.part + at * D + quad * 4);
+        for (int b = 0; b < B; ++b) {
+          const long at = (pb * p.splits + min(s0 + b * groups, p.splits - 1)) * bq + in;
+          e[b] = launch.ml[at];
+          v[b] = *reinterpret_cast<const f32x4*>(launch.part + at * D + quad * 4);
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+          if (s0 + b * groups < p.splits) join(e[b].x, e[b].y, v[b]);
       }
-#pragma unroll
-      for (int b = 0; b < B; ++b)
-        if (s0 + b * groups < p.splits) join(e[b].x, e[b].y, v[b]);
+    }
+    if (groups > 1) {
+      if (unit < UNITS) {
+        s_num[unit][quad] = num;
+        if (quad == 0) s_ml[unit] = make_float2(top, den);
+      }
+      __syncthreads();
+      if (g == 0 && there)
+        for (int i = 1; i < groups; ++i) join(s_ml[unit + i].x, s_ml[unit + i].y, s_num[unit + i][quad]);
+      __syncthreads();   // (read before the next rows' are written)
+    }
+    if (g == 0 && there) {
+      const int tok = row / a.group, hq = h * a.group + (row - tok * a.group);
+      store_quad<T>((T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head, quad * 4, a.d, num * (den == 0.f ? 0.f : 1.f / den));
     }
   }
-  if (groups > 1) {
-    if (unit < UNITS) {
-      s_num[unit][quad] = num;
-      if (quad == 0) s_ml[unit] = make_float2(top, den);
-    }
-    __syncthreads();
-    if (g == 0 && there)
-      for (int i = 1; i < groups; ++i) join(s_ml[unit + i].x, s_ml[unit + i].y, s_num[unit + i][quad]);
-  }
-  if (g != 0 || !there) return;
-  const int tok = row / a.group, hq = h * a.group + (row - tok * a.group);
-  store_quad<T>((T*)a.o + n * a.os.sample + tok * a.os.token + hq * a.os.head, quad * 4, a.d, num * (den == 0.f ? 0.f : 1.f / den));
 }
 
 template <typename T, int D, int QW, int KW, int KT, int WAVES, bool MASKED>
@@ -605,15 +610,17 @@ int cross_launch_kernel(const CrossLaunch& l, hipStream_t s) {
     known.fetch_or(bit);
   }
   const CrossPlan& p = l.plan;
-  const long blocks = (long)l.a.n * l.a.heads * p.row_blocks, rows = blocks * F::BQ;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * p.splits)), dim3(F::NT), smem, s, l);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)l.a.n * l.a.heads * p.row_blocks * p.splits)), dim3(F::NT), smem, s, l);
   WMDEC_HIP(hipGetLastError());
   if (p.splits > 1) {
     constexpr int units = 256 / (D / 4);
-    int groups = 1;   // as many as there are ranges, while rows are fewer than the compute units take at once
-    while (groups * 2 <= units && groups < p.splits && groups < 8 && rows * groups < 4096L * units) groups *= 2;
-    const long in_block = units / groups;
-    hipLaunchKernelGGL((cross_combine_kernel<T, D>), dim3((unsigned)((rows + in_block - 1) / in_block)), dim3(256), 0, s, l, F::BQ, groups);
+    // As many groups as there are eights of ranges; nothing that depends on the number of samples, as the groups decide which ranges are added before which.  us, with
+    // as many as there are ranges / so: 700x3000 of 4 heads of 96 in f16 (6 ranges) 22.4 / 18.7, four samples 52.8 / 36.0, 16 x 4096 keys of 8 of 128 (16) 60.3 / 59.6,
+    // 32768 keys (64) 34.1 / 34.1.
+    int groups = 1;
+    while (groups * 2 <= units && groups * 8 < p.splits) groups *= 2;
+    const long total = (long)l.a.n * l.a.heads * p.rows, in_block = units / groups, most = 8192;   // rows (below 2^26: cross_attention_fits); rows and most workgroups of a launch
+    hipLaunchKernelGGL((cross_combine_kernel<T, D>), dim3((unsigned)std::min(most, (total + in_block - 1) / in_block)), dim3(256), 0, s, l, F::BQ, groups, (unsigned)total);
     WMDEC_HIP(hipGetLastError());
   }
   return WMDEC_OK;

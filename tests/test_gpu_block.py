@@ -611,6 +611,38 @@ def test_cross_bits_of_a_sample_do_not_depend_on_the_batch():
                 assert torch.equal(run(slice(i, i + 1))[0], whole[i])
 
 
+@pytest.mark.parametrize("dtype, n, tq, tk, hq, hk, d", [("f16", 32, 1, 8192, 32, 8, 128), ("f32", 32, 1, 8192, 32, 8, 128), ("f16", 4, 700, 3000, 4, 4, 96), ("f32", 12, 9, 5000, 8, 2, 40)])
+def test_cross_ranges_are_joined_alike_in_every_batch(dtype, n, tq, tk, hq, hk, d):
+    """Many ranges of keys, and samples enough to make the join's launch another one."""
+    q, k, v = (torch.randn(s, device="cuda").to(G.TORCH[dtype]) for s in ((n, tq, hq, d), (n, tk, hk, d), (n, tk, hk, d)))
+
+    def run(s):
+        o = torch.empty_like(q[s])
+        need = wmdec.cross_attention_workspace_bytes(q[s], k[s])
+        assert need
+        wmdec.cross_attention(q[s], k[s], v[s], o, d ** -0.5, workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"))
+        return o
+    whole = run(slice(0, n))
+    for i in (0, 1, n // 2, n - 1):
+        assert torch.equal(run(slice(i, i + 1))[0], whole[i]), i
+
+
+def test_cross_more_rows_of_many_ranges_than_a_joining_launch_takes_at_once():
+    """65 samples of 4 key heads and 32 rows each, 17 ranges of keys: 8320 rows with a workgroup each, in a launch of at most 8192."""
+    q, k, v = (torch.randn(s, device="cuda").half() for s in ((65, 4, 32, 256), (1, 4400, 4, 256), (1, 4400, 4, 256)))
+    k, v = k.expand(65, -1, -1, -1), v.expand(65, -1, -1, -1)
+
+    def run(s):
+        o = torch.empty_like(q[s])
+        wmdec.cross_attention(q[s], k[s], v[s], o, 0.0625, workspace=torch.empty(wmdec.cross_attention_workspace_bytes(q[s], k[s]), dtype=torch.uint8, device="cuda"))
+        return o
+    whole = run(slice(0, 65))
+    for i in (0, 31, 63, 64):
+        assert torch.equal(run(slice(i, i + 1))[0], whole[i]), i
+    want, weighted = ref.cross_attention(host(q[64:]), host(k[:1]), host(v[:1]), 0.0625)
+    assert_within(host(whole[64:]), want, cross_tolerance("f16", host(q[64:]), host(k[:1]), want, weighted, 0.0625, 4400, host(v[:1])))
+
+
 def test_workspace_too_small_is_refused():
     q, k = torch.zeros((1, 1, 32, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 32768, 8, 128), dtype=torch.bfloat16, device="cuda")
     need = wmdec.cross_attention_workspace_bytes(q, k)
