@@ -35,10 +35,12 @@ __global__ void rope_frequencies_kernel(FreqParams p) {
 }
 
 // sin and cos of the angle theta: quarter turns and the rest within an eighth of a turn, in 64 bits, then Taylor's polynomials in fp32 (the terms left out
-// are below 2^-29 of the sine and 2^-33).
+// are below 2^-28 of the sine and 2^-32 of the cosine).  The quarter turns are taken off by fused steps with pi / 2 in two parts
+// (the reduction of Cody and Waite), in which their product is not rounded.  (The fraction of theta / (pi / 2): up to 5 steps of 2^-24 off at 2^31.)
+constexpr double kQuarterTurn = kTwoPi / 4, kQuarterTurnRest = 6.123233995736766e-17;   // pi / 2 and what is left of it
 __device__ __forceinline__ float2 sin_cos(double theta) {
-  const double quarters = theta * (4.0 / kTwoPi), whole = rint(quarters);
-  const float r = (float)((quarters - whole) * (kTwoPi / 4.0)), z = r * r;
+  const double whole = rint(theta * (4.0 / kTwoPi));
+  const float r = (float)fma(-whole, kQuarterTurnRest, fma(-whole, kQuarterTurn, theta)), z = r * r;
   const float sn = fmaf(r * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), r);
   const float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
   const int q = (int)(long)whole & 3;

@@ -347,6 +347,20 @@ def test_rope_past_32_bit_offsets():
     assert not x[0, :2].any()
 
 
+def test_rope_far_turns_are_exact_to_fp32():
+    """The pair (1, 0) comes back as (cos, sin) of theta = position * frequency in 64 bits.  The rest within an eighth of a turn (at most 0.79) is rounded
+    once to fp32, 0.79 U; the last step of the polynomial rounds once, a step of at most 1, U / 2 below 1 counted as U; its terms before and those left out
+    come to 0.31 U (r^3 / 6 at most 0.081 with four roundings, 2^-28.6 of 0.71); the products by 1 and 0 and their sum round nothing.  2.1 U."""
+    r = rng(151)
+    pos = np.concatenate([r.integers(2 ** 30, 2 ** 31, 20000), -r.integers(2 ** 30, 2 ** 31, 20000), np.array([2 ** 31 - 1, -2 ** 31, 0, 1])]).reshape(1, -1, 1)
+    f = ref.rope_frequencies((64,))
+    x = np.zeros((1, pos.size, 1, 64), np.float32)
+    x[..., :32] = 1.0
+    out = torch.empty(x.shape, device="cuda")
+    wmdec.rope(dev(x, "f32"), None, torch.from_numpy(pos.astype(np.int32)).cuda(), torch.from_numpy(f).cuda(), (64,), out, None)
+    assert_within(host(out), ref.rope(x, pos, f, (64,)), 2.1 * U)
+
+
 # ------------------------------------------------------------------ attention to states of another length
 def cross_tolerance(dtype, q, k, want, weighted, scale, tk, v):
     """weighted: the softmax weights times |v|.  Half a step for the output; half a step for every probability in 16 bits (and half of the
