@@ -359,8 +359,9 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
  * Scores, softmax and sums are fp32; 16-bit types round the probabilities to dtype
  * for the second product.  F32 is fp32 throughout.  A sample's bits do not depend
  * on what it is batched with.
- * workspace: wmdec_cross_attention_workspace_bytes(...) bytes (may be 0) of
- * 16-byte aligned device memory, no initialisation; one or two kernels. */
+ * workspace: wmdec_cross_attention_workspace_bytes(...) bytes (may be 0, and is for
+ * sizes that the call refuses) of 16-byte aligned device memory, no initialisation;
+ * one or two kernels. */
 size_t wmdec_cross_attention_workspace_bytes(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d);
 int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const void* k, const wmdec_strides* k_strides,
                           const void* v, const wmdec_strides* v_strides, void* o, const wmdec_strides* o_strides, int dtype,

@@ -936,8 +936,17 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
 }
 
 // ---- attention to states of another length
+static bool cross_width(int dtype, int d) { return d * dtype_size(dtype) % 16 == 0 && d <= kCrossMaxD; }
+// (rows of a key head and keys are checked before anything is reckoned with them in 32 bits)
+static bool cross_fits(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d) {
+  const long most = (1L << 31) - 512;
+  return (long)tq * (heads_q / heads_kv) <= most && tk <= most && cross_attention_fits(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
+}
+
 size_t wmdec_cross_attention_workspace_bytes(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d) {
-  if (!valid_dtype(dtype) || tk < 0 || n <= 0 || tq <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q % heads_kv || d <= 0 || d > kCrossMaxD) return 0;
+  if (!valid_dtype(dtype) || tk < 0 || n <= 0 || tq <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q % heads_kv || d <= 0 || !cross_width(dtype, d) ||
+      !cross_fits(dtype, n, tq, tk, heads_q, heads_kv, d))
+    return 0;
   return cross_attention_scratch_bytes(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
 }
 
@@ -958,7 +967,7 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
   WMDEC_REQUIRE(n > 0 && tq > 0 && tk >= 0 && heads_q > 0 && heads_kv > 0 && d > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
   WMDEC_REQUIRE(heads_q % heads_kv == 0, WMDEC_ERR_SHAPE, "%s: %d query heads are no multiple of %d key heads", who, heads_q, heads_kv);
   const size_t es = dtype_size(dtype);
-  WMDEC_REQUIRE(d * es % 16 == 0 && d <= kCrossMaxD, WMDEC_ERR_UNSUPPORTED, "%s: d %d must be a multiple of %d and at most %d", who, d, (int)(16 / es), kCrossMaxD);
+  WMDEC_REQUIRE(cross_width(dtype, d), WMDEC_ERR_UNSUPPORTED, "%s: d %d must be a multiple of %d and at most %d", who, d, (int)(16 / es), kCrossMaxD);
   int rc = check_cross_tensor(who, q, q_strides, n, tq, heads_q, es);
   if (rc == WMDEC_OK) rc = check_cross_tensor(who, k, k_strides, n, tk, heads_kv, es);
   if (rc == WMDEC_OK) rc = check_cross_tensor(who, v, v_strides, n, tk, heads_kv, es);
@@ -969,9 +978,7 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
   WMDEC_REQUIRE(isfinite(scale) && scale > 0.f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
   WMDEC_REQUIRE(o != q && o != k && o != v && distinct(*o_strides, n, tq, heads_q), WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs or itself", who);
   WMDEC_REQUIRE(element_aligned(key_lens, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
-  const long rows = (long)tq * (heads_q / heads_kv);
-  WMDEC_REQUIRE(rows <= (1L << 31) - 512 && tk <= (1L << 31) - 512 && cross_attention_fits(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d), WMDEC_ERR_UNSUPPORTED,
-                "%s: too many rows", who);
+  WMDEC_REQUIRE(cross_fits(dtype, n, tq, tk, heads_q, heads_kv, d), WMDEC_ERR_UNSUPPORTED, "%s: too many rows", who);
   const size_t need = cross_attention_scratch_bytes(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
   WMDEC_REQUIRE(need == 0 || (workspace && aligned16(workspace) && workspace_bytes >= need), WMDEC_ERR_WORKSPACE,
                 "%s: workspace needs %zu 16-byte aligned bytes, got %zu", who, need, workspace ? workspace_bytes : (size_t)0);

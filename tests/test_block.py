@@ -2,6 +2,9 @@
 the library and its binding refuse (no GPU needed)."""
 import ctypes
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -181,6 +184,20 @@ def test_cross_attention_workspace_is_asked_for():
     assert size(wmdec.BF16, 7, 1, 32768, 32, 8, 128) == 7 * need and size(wmdec.BF16, 1, 5400, 512, 30, 30, 64) == 0
     for bad in ((7, 1, 1, 5, 4, 2, 64), (1, 1, 1, -1, 4, 2, 64), (1, 0, 1, 5, 4, 2, 64), (1, 1, 1, 5, 4, 3, 64), (1, 1, 1, 5, 4, 2, 512)):
         assert size(*bad) == 0
+
+
+def test_cross_attention_workspace_of_what_is_refused_is_nothing():
+    """Rows past 31 bits, keys past them, launches past 2^32 threads and widths that are no multiple of 16 bytes.  (In a process of its own: the size of 2^30 tokens of four
+    heads once ended it by a division by zero.)"""
+    cases = [(wmdec.BF16, 1, 1 << 30, 5000, 4, 1, 64), (wmdec.BF16, 1, 1 << 29, 5000, 4, 1, 64), (wmdec.F32, 2, (1 << 31) - 1, 5000, 64, 2, 128), (wmdec.F16, 1, 3, (1 << 31) - 1, 4, 2, 64),
+             (wmdec.F16, 1 << 23, 1, 20, 4, 2, 64), (wmdec.BF16, 1 << 21, 1, 1 << 20, 1, 1, 64), (wmdec.BF16, 1, 1, 32768, 4, 2, 60), (wmdec.F32, 1, 1, 32768, 4, 2, 66)]
+    code = "from paper_2602_00608_amd import wmdec; print([wmdec.lib().wmdec_cross_attention_workspace_bytes(*c) for c in %r])" % (cases,)
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert out.returncode == 0 and out.stdout.strip() == str([0] * len(cases)), (out.returncode, out.stdout, out.stderr[-500:])
+    for c in cases:
+        dtype, n, tq, tk, hq, hk, d = c
+        assert wmdec.lib().wmdec_cross_attention(*dict(CROSS, dtype=dtype, n=n, tq=tq, tk=tk, hq=hq, hk=hk, d=d).values()) == wmdec.ERR_UNSUPPORTED, c
+    assert wmdec.lib().wmdec_cross_attention_workspace_bytes(wmdec.F32, 1, 1, 32768, 4, 2, 60) > 0
 
 
 # ------------------------------------------------------------------ refusals of the binding
