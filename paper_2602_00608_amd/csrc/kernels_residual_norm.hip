@@ -4,7 +4,7 @@
 // norms' weights and biases: up to seven times four bytes a channel, more than a row of 16-bit tensors has) would be read again for every row, so a
 // thread owns eight channels of many rows and keeps what they come to in registers, two multiply-adds an element:
 //   x' = x + ((h - mean) * rstd) * ga + gb,   ga = s * g * w, gb = s * g * u;     y = ((x' - mean) * rstd) * ya + yb,   ya = w (1 + c), yb = u (1 + c) + b.
-// A row is 8 to 64 lanes of a wavefront (up to 512 channels), or whole wavefronts of a workgroup; the next row is requested before the present one
+// A row is 8 to 64 lanes of a wavefront (up to 512 channels, four rows of them and more a workgroup), or whole wavefronts of one; the next row is requested before the present one
 // is reduced.  Moments: mean and squares about it over the values of a wavefront, joined over the wavefronts (Chan, Golub, LeVeque) behind one barrier a norm.
 // us on inputs from memory, with the rate: 2x5400 rows of 1920 in bf16 38.1 (4.36 TB/s), 4x5400 rows of 1152, fp32 beside f16, 62.7 (4.76; a copy of 4 GiB 4.89).
 // Steps: a row a workgroup 318 and 405; this form with ranges of rows, two rows at a time, in 1.3 rounds of workgroups 50.5 and 84.2; one round 42.7 and 71.0; a row at
@@ -73,7 +73,8 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
   __shared__ float4 s_red[2][2][kMaxThreads / 64];
   const ResidualNormArgs& a = p.a;
   const int d = a.d, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int groups = p.tpr < 64 ? (int)blockDim.x / p.tpr : 1, group = p.tpr < 64 ? tid / p.tpr : 0, lane = p.tpr < 64 ? tid % p.tpr : tid;
+  const bool shared = p.tpr <= 64;        // rows of a wavefront's lanes
+  const int groups = shared ? (int)blockDim.x / p.tpr : 1, group = shared ? tid / p.tpr : 0, lane = shared ? tid % p.tpr : tid;
   const int n = blockIdx.x / p.segs, seg = blockIdx.x % p.segs;
   const int row0 = seg * groups, step = p.segs * groups;   // (workgroups side by side: the rows under way at a time are next to each other in memory)
   const bool has_h = a.h != nullptr, has_y = a.y != nullptr;
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
   float held = 0.f;                       // values of this wavefront in a row
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    col[i] = VEC ? (i * p.tpr + lane) * E : i * p.tpr * E + (p.tpr < 64 ? lane : wave * 64 * E + (tid & 63));
+    col[i] = VEC ? (i * p.tpr + lane) * E : i * p.tpr * E + (shared ? lane : wave * 64 * E + (tid & 63));
     count[i] = min(VEC ? max(d - col[i], 0) : max(d - col[i] + gap - 1, 0) / gap, E);
     held += (float)min(max(d - (i * p.tpr + wave * 64) * E, 0), 64 * E);
   }
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
     }
   }
 
-  const float inv_d = 1.f / (float)d, inv_held = p.tpr > 64 ? 1.f / fmaxf(held, 1.f) : inv_d;
+  const float inv_d = 1.f / (float)d, inv_held = shared ? inv_d : 1.f / fmaxf(held, 1.f);
   auto row_sum = [&](float v) {           // over the lanes of a row, or of a wavefront of it
     v = lane_group_sum<8>(v);
     if (p.tpr > 8) v += mirror16(v);
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
       m2 += VEC && count[i] == 0 ? 0.f : part;
     }
     m2 = row_sum(m2);
-    if (p.tpr > 64) {
+    if (!shared) {
       if ((tid & 63) == 0) s_red[parity][which][wave] = make_float4(mean, m2, held, 0.f);
       __syncthreads();
       const int waves = blockDim.x >> 6;
@@ -224,8 +225,12 @@ __global__ __launch_bounds__(kMaxThreads, VPT == 1 ? 4 : 2) void residual_norm_k
 template <typename TX, typename TA, int VPT, bool VEC>
 int launch_form(const ResidualNormArgs& a, int tpr, int threads, hipStream_t s) {
   Params p{a, tpr, 1};
-  const int groups = tpr < 64 ? threads / tpr : 1;
-  const int most = (a.t + groups - 1) / groups, waves = VPT == 1 ? 16 : 8;   // wavefronts of a compute unit
+  const int groups = tpr <= 64 ? threads / tpr : 1;
+  const int most = (a.t + groups - 1) / groups;
+  // Wavefronts of a compute unit; four where each has a row of more than 3 KB to itself (448 and 512 channels in fp32).  us, 16 / 4: fp32 20000 rows of 512 36.1 / 33.7,
+  // 100000 rows 161.7 / 143.9, 2 x 5400 of 448 22.2 / 20.3; but 100000 of 320 105.8 / 113.6, fp32 beside bf16 20000 of 448 25.4 / 26.4, bf16 20000 of 512 19.6 / 24.7.
+  const long row_bytes = (long)a.d * (sizeof(TX) + (a.h ? sizeof(TA) : 0));
+  const int waves = tpr == 64 && row_bytes > 3072 ? 4 : VPT == 1 ? 16 : 8;
   const int target = 256 * (waves / (threads / 64)) / a.n;   // all workgroups at once: those of a second round would run alone
   p.segs = max(1, min(most, target));
   hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);

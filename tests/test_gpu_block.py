@@ -153,6 +153,17 @@ def test_residual_norm_many_rows():
         run_norm("bf16", "bf16", n, t, d, "none", "layer", seed=12)
 
 
+@pytest.mark.parametrize("d", [256, 257, 264, 379, 384, 504, 511, 512, 513])
+def test_residual_norm_rows_of_a_whole_wavefront(d):
+    """Up to 512 channels a row is a wavefront's and a workgroup has four of them: numbers of rows that are no multiple of that, one and several rounds of them."""
+    for xdt, adt in (("bf16", "bf16"), ("f32", "f16")):
+        for n, t in ((1, 1), (1, 3), (3, 5), (2, 2051), (1, 9001)):
+            run_norm(xdt, adt, n, t, d, "layer-", "layer", seed=17)
+        for offset in (0, 1):
+            run_norm(xdt, adt, 2, 6, d, "rms", "layer-", mod=None, offset=offset, seed=18)
+            run_norm(xdt, adt, 1, 7, d, "none", "rms", residual=False, offset=offset, seed=19)
+
+
 def test_residual_norm_one_vector_for_all_samples_and_rows_alike():
     """gate, scale and shift expanded over the samples (stride 0); a row's bits depend neither on its place nor on the other rows."""
     r = rng(13)
