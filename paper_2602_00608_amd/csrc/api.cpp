@@ -975,7 +975,7 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
   if (rc != WMDEC_OK) return rc;
   const long most = (1L << 31) / (128 * (long)es);
   WMDEC_REQUIRE(k_strides->token < most && v_strides->token < most, WMDEC_ERR_UNSUPPORTED, "%s: 128 tokens of k or v span 2 GiB or more", who);
-  WMDEC_REQUIRE(isfinite(scale) && scale > 0.f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  WMDEC_REQUIRE(scale > 0.f && scale <= 2e38f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and at most 2e38", who);   // (times log2(e) still finite)
   WMDEC_REQUIRE(o != q && o != k && o != v && distinct(*o_strides, n, tq, heads_q), WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs or itself", who);
   WMDEC_REQUIRE(element_aligned(key_lens, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
   WMDEC_REQUIRE(cross_fits(dtype, n, tq, tk, heads_q, heads_kv, d), WMDEC_ERR_UNSUPPORTED, "%s: too many rows", who);

@@ -186,6 +186,13 @@ def test_cross_attention_workspace_is_asked_for():
         assert size(*bad) == 0
 
 
+def test_cross_attention_refuses_a_scale_that_the_kernel_cannot_hold():
+    """The kernel multiplies it by log2(e): from 2.36e38 on that is infinite, and a score of zero not a number."""
+    for scale in (2.1e38, 2.4e38, 3.4e38, math.inf, math.nan, 0.0, -1e-30):
+        assert wmdec.lib().wmdec_cross_attention(*dict(CROSS, scale=scale).values()) == wmdec.ERR_INVALID_ARG, scale
+    assert wmdec.lib().wmdec_cross_attention(*dict(CROSS, scale=1.9e38, q=None).values()) == wmdec.ERR_INVALID_ARG and "null" in wmdec.last_error()
+
+
 def test_cross_attention_workspace_of_what_is_refused_is_nothing():
     """Rows past 31 bits, keys past them, launches past 2^32 threads and widths that are no multiple of 16 bytes.  (In a process of its own: the size of 2^30 tokens of four
     heads once ended it by a division by zero.)"""
