@@ -7,8 +7,9 @@ published MI355X peak (2516.6 TFLOP/s dense f16/bf16 MFMA, 8000 GB/s HBM).  Two 
 events on the current stream and inputs resident in HBM:
   warm  `reps` back-to-back calls on the same tensors (tensors up to a few hundred MB partly stay in the last-level
         cache between calls);
-  cold  between two calls a 2 GiB buffer is streamed (read and written), which evicts every cache level; the time
-        of the streaming kernel alone, measured the same way, is subtracted.
+  cold  before a call a 2 GiB buffer is streamed (read and written), which evicts every cache level; the time
+        of the streaming kernel alone, measured in turn with it, is subtracted (medians); a difference within the
+        stream's own spread is no reading and is printed as "-".
 A 16-bit upsampling convolution is priced at the nine products per input pixel it executes (1/4 of the nine-tap figure).  Inputs are seeded N(0,1) tensors and 1/sqrt(fan_in) weights; real activations toggle fewer bits,
 so inside decoder_run the same convolutions run somewhat faster.
 """
@@ -45,7 +46,6 @@ def timeit(fn, reps):
         fn()
     torch.cuda.synchronize()
     warm = _events(fn, reps)
-    creps = max(3, reps // 4)
     flush = timeit.flush
 
     def evict():
@@ -55,10 +55,32 @@ def timeit(fn, reps):
         evict()
         fn()
     evict()
-    torch.cuda.synchronize()
-    base = _events(evict, creps)
-    cold = _events(cold_call, creps) - base
-    return warm, cold
+    alone, both = [], []
+    for _ in range(max(8, reps // 2)):   # (several at a time: a first call after a wait is slower)
+        alone.append(_events(evict, 4))
+        both.append(_events(cold_call, 4))
+    return warm, difference(alone, both)
+
+
+def difference(alone, both):
+    """Median of `both` less that of `alone`, or None where it is not above what half of the readings of `alone` lie within."""
+    alone, both = sorted(alone), sorted(both)
+    n = len(alone)
+    cold = both[len(both) // 2] - alone[n // 2]
+    return cold if cold > alone[3 * n // 4] - alone[n // 4] else None
+
+
+def figures(us, work, unit, peak):
+    """Time, rate and share of the peak of one reading, which may be none."""
+    if us is None:
+        return "%8s us %8s %s (%5s)" % ("-", "-", unit, "-")
+    rate = work / us / (1e6 if unit == "TFLOP/s" else 1e3)
+    return "%8.1f us %8.1f %s (%4.1f%%)" % (us, rate, unit, rate / peak * 100)
+
+
+def line(name, shape, us, work, unit, peak):
+    warm, cold = us
+    print("%-30s %-22s warm %s   cold %s of %.0f" % (name, shape, figures(warm, work, unit, peak), figures(cold, work, unit, peak), peak), flush=True)
 
 
 def main():
@@ -81,14 +103,6 @@ def main():
         rstd = torch.empty(n * groups, dtype=torch.float32, device="cuda")
         wmdec.gn_stats(x, groups, eps, mean, rstd, ws)
         return mean, rstd, ws
-
-    def line(name, shape, us, work, unit, peak):
-        warm, cold = us
-        print("%-30s %-22s warm %8.1f us %8.1f %s (%4.1f%%)   cold %8.1f us %8.1f %s (%4.1f%% of %.0f)"
-              % (name, shape, warm, work / warm / 1e6 if unit == "TFLOP/s" else work / warm / 1e3, unit,
-                 (work / warm / 1e6 if unit == "TFLOP/s" else work / warm / 1e3) / peak * 100,
-                 cold, work / cold / 1e6 if unit == "TFLOP/s" else work / cold / 1e3, unit,
-                 (work / cold / 1e6 if unit == "TFLOP/s" else work / cold / 1e3) / peak * 100, peak), flush=True)
 
     if args.block:
         return block_operators(dt, line, args.reps)

@@ -12,7 +12,7 @@ import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
 
 from oracle import ref
-from paper_2602_00608_amd import asm_check, wmdec
+from paper_2602_00608_amd import asm_check, bench_ops, wmdec
 
 
 # ------------------------------------------------------------------ oracle
@@ -295,3 +295,12 @@ def test_other_uses_of_m0_are_found():
     assert len(asm_check.check_m0(load + ["s_mov_b32 m0, s5"])) == 1 and len(asm_check.check_m0(load + ["v_readlane_b32 s3, v2, m0"])) == 1
     text = "\n".join(["_Z6kernel:"] + ["\t" + l for l in load + ["s_mov_b32 m0, -1", "s_endpgm"]] + [".Lfunc_end0:"])
     assert len(asm_check.check_source(text, m0="kernel")) == 1 and asm_check.check_source(text, m0="other") == []
+
+
+# ------------------------------------------------------------------ timing
+def test_a_cold_time_within_the_spread_of_what_is_subtracted_is_no_reading():
+    alone = [450.0, 447.0, 452.0, 455.0, 449.0, 451.0, 446.0, 453.0]
+    assert bench_ops.difference(alone, [v - 1.0 for v in alone]) is None and bench_ops.difference(alone, [v + 3.0 for v in alone]) is None
+    assert bench_ops.difference(alone, [v + 40.0 for v in alone]) == 40.0
+    assert bench_ops.figures(None, 1e9, "GB/s", 8000.0).split() == ["-", "us", "-", "GB/s", "(", "-)"]
+    assert bench_ops.figures(100.0, 4e8, "GB/s", 8000.0).split() == ["100.0", "us", "4000.0", "GB/s", "(50.0%)"]
