@@ -317,7 +317,8 @@ int wmdec_residual_norm(const void* x, int x_dtype, const void* h, int act_dtype
  * other overlap, and no stride of zero over several tokens, heads or samples.
  * positions: int32 [t][axes], positions_stride elements from sample to sample (0:
  * the same for all).  1 to 3 axes, at most 4096 rotated of 16384 channels, 16384
- * heads of q and k, 2^31 - 2^20 tokens.  Rotations by theta as
+ * heads of q and k, 2^31 - 2^20 tokens; a launch of 2^24 workgroups (256 tokens, or as
+ * many as have 2048 pairs in a head, each) or more is refused.  Rotations by theta as
  * fp64 holds it are good to fp32 for every int32 position; one rounding to dtype. */
 typedef enum { WMDEC_ROPE_PLAIN = 0, WMDEC_ROPE_LINEAR = 1, WMDEC_ROPE_BASE = 2, WMDEC_ROPE_RAMP = 3 } wmdec_rope_scaling_kind;
 typedef struct {

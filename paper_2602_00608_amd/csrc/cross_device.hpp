@@ -14,12 +14,12 @@
 // What bounds it.  Few rows: the one read of the keys and values; two workgroups of 32 rows a compute unit, with 128 KB of tiles under way.  Many rows in
 // 16 bits: the power that the matrix cores may draw, and at 64 channels the exponentials, which take as many cycles as the products (32 rows and 64 keys of a
 // wavefront: 16 products of 32 cycles, 32 exponentials of 8 beside 32 each of multiply-add, add and half a maximum and a conversion).  fp32: its products.
-// Rates: one token of 32 heads against 16 x 4096 keys of 8 heads of 128 in bf16 55.3 us = 4.86 TB/s; 8192x8192 of 32 / 8 heads of 128 1045 us = 1050 TFLOP/s (a large
-// library product on this card 1090 to 1150); 5400x5400 of 30 heads of 64 280 to 300 us = 746 to 800, of 96 heads 870 to 890 (1290 workgroups are 1.26 rounds of
-// the 1024 that run at once); fp32 4000x2000 of 8 heads of 128 263 us = 125 of 155.
+// Rates: one token of 32 heads against 16 x 4096 keys of 8 heads of 128 48.1 us = 5.58 TB/s on the inputs of the call before, 58.9 on others; 8192x8192 of 32 / 8 heads
+// of 128 1040 to 1150 us = 1060 to 950 TFLOP/s (a large library product on this card 1090 to 1150); 5400x5400 of 30 heads of 64 280 to 310 us = 720 to 800, of 96
+// heads 870 to 890 (1290 workgroups are 1.26 rounds of the 1024 that run at once); fp32 4000x2000 of 8 heads of 128 266 us = 123 of 155.
 // Steps, us for 5400x5400 of 30 of 64 f16, 2 x 5400x512 of 30 of 64 bf16 (two lengths), 1 token against 4 x 32768 (ragged) of 8 of 128: a wavefront a row 92950, 9854,
 // 50355; matrix cores, tiles through LDS, transposed reads 298, 66, 128; tiles by instructions that the compiler does not wait for 298, 66, 110; 128 rows a workgroup
-// and the XCDs divided within a sample 297, 50, 65; wavefronts past the last row idle 290, 50, 65.  With a fifth of the keys masked, by a mask on the scores and zeros in place of masked values / by tiles of valid
+// and the XCDs divided within a sample 297, 50, 65; wavefronts past the last row idle 290, 50, 65; ranges joined by as many threads as there are rows 62 of the last.  With a fifth of the keys masked, by a mask on the scores and zeros in place of masked values / by tiles of valid
 // keys: 5400x5400 of 30 of 64 in bf16 361 / 240 (280 without a mask), 4096x4096 of 16 of 128 168 / 117, 333x301 of 8 of 72 in fp32 20.0 / 15.3.  160 channels as 192 / as
 // themselves, with two workgroups a compute unit: 4000x4000 of 30 heads in f16 528 / 338.
 // Measured and not kept: 64 rows a wavefront (128 channels 818 TFLOP/s against 1005: half the wavefronts), wave priorities around the products, the compiler's own
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     };
     if constexpr (OWN) {
       // One buffer of either, asked for again as soon as it has been read: the next keys travel behind the softmax and the values, the next values behind the
-      // scores.  (Two buffers each: half the workgroups a compute unit, and slower throughout, 16 x 4096 keys of 8 heads of 128 channels 74.0 us against 55.3.)
+      // scores.  (Two buffers each: half the workgroups a compute unit, and slower throughout, the main launch of 16 x 4096 keys of 8 heads of 128 channels by 19 us.)
       if (nb) { ask_k(0); ask_v(0); }
       queries_landed();
       static_assert(!OWN || NS == 1, "a wavefront has 32 keys of a tile");
