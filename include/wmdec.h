@@ -355,8 +355,9 @@ int wmdec_rope(const void* q, const wmdec_strides* q_strides, void* q_out, const
  * elements, channels contiguous.  d: a multiple of 8 (16-bit types) or 4 (F32), at
  * most 256; pointers and strides multiples of 16 bytes; 128 tokens of k or v span
  * less than 2 GiB.  A launch of 2^24 workgroups (32 or 128 rows of a key head and a
- * range of its keys each) or more is refused.  0 < scale <= 2e38.  o must not overlap
- * the inputs or itself.
+ * range of its keys each) or more is refused, and one of 2^26 such rows or more
+ * where keys are divided into ranges (a workspace is asked for).  0 < scale <= 2e38.
+ * o must not overlap the inputs or itself.
  * Scores, softmax and sums are fp32; 16-bit types round the probabilities to dtype
  * for the second product.  F32 is fp32 throughout.  A sample's bits do not depend
  * on what it is batched with.

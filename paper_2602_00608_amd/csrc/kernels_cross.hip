@@ -56,7 +56,7 @@ size_t part_rows(const CrossPlan& p, int n, int heads) { return p.splits == 1 ? 
 bool cross_attention_fits(int dtype, int n, int tq, int tk, int heads, int group, int d) {
   const CrossPlan p = plan_of(dtype, tq, tk, heads, group, d);
   const double blocks = (double)n * heads * p.row_blocks;
-  return blocks * p.splits < 0x1p24 && (p.splits == 1 || blocks * (p.few ? 32 : 128) < 0x1p26);   // workgroups of 256 threads; rows that are joined, four of them
+  return blocks * p.splits < 0x1p24 && (p.splits == 1 || blocks * (p.few ? 32 : 128) < 0x1p26);   // workgroups of 256 threads; rows that are joined, numbered in 32 bits
 }
 
 size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d) {
