@@ -227,10 +227,10 @@ int launch_form(const ResidualNormArgs& a, int tpr, int threads, hipStream_t s) 
   Params p{a, tpr, 1};
   const int groups = tpr <= 64 ? threads / tpr : 1;
   const int most = (a.t + groups - 1) / groups;
-  // Wavefronts of a compute unit; four where each has a row of more than 3 KB to itself (448 and 512 channels in fp32).  us, 16 / 4: fp32 20000 rows of 512 36.1 / 33.7,
+  // Wavefronts of a compute unit; four where each has a row of more than 3200 bytes to itself (from 401 channels on in fp32).  us, 16 / 4: fp32 20000 rows of 512 36.1 / 33.7,
   // 100000 rows 161.7 / 143.9, 2 x 5400 of 448 22.2 / 20.3; but 100000 of 320 105.8 / 113.6, fp32 beside bf16 20000 of 448 25.4 / 26.4, bf16 20000 of 512 19.6 / 24.7.
   const long row_bytes = (long)a.d * (sizeof(TX) + (a.h ? sizeof(TA) : 0));
-  const int waves = tpr == 64 && row_bytes > 3072 ? 4 : VPT == 1 ? 16 : 8;
+  const int waves = tpr == 64 && row_bytes > 3200 ? 4 : VPT == 1 ? 16 : 8;
   const int target = 256 * (waves / (threads / 64)) / a.n;   // all workgroups at once: those of a second round would run alone
   p.segs = max(1, min(most, target));
   hipLaunchKernelGGL((residual_norm_kernel<TX, TA, VPT, VEC>), dim3((unsigned)a.n * p.segs), dim3(threads), 0, s, p);
