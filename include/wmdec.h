@@ -371,6 +371,80 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
                           int heads_q, int heads_kv, int d, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * A cache of keys and values in four bits, for blocks that attend to the frames or
+ * tokens before (the paper's world model conditions every latent on those before it,
+ * Alg. 1; it does not say how they are kept).
+ *
+ * Format.  32 consecutive channels of a head of a token (the last block of a head
+ * may be shorter) share a power of two 2^e; a value is a sign and one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 times 2^e.  With m the largest magnitude of the block,
+ *   e = floor(log2(m)) - 2, one more if m >= 1.75 * 2^floor(log2(m)),
+ * kept within -125 .. 125, or .. 13 if the source is F16 (what is read back in F16 is
+ * then finite).  A value is the nearest of these, ties to the even place in the
+ * list, 6 * 2^e for what is above.  A block with a value that is not finite is held
+ * as not a number.  All of this is exact: equal states are held as equal bits.  BF16
+ * and F32 read back exactly what is held, F16 what came from F16 (else rounded to it).
+ *
+ * Pages.  cache->data is `pages` pages of wmdec_cache_page_bytes(page_tokens, heads, d)
+ * bytes (16-byte aligned, no initialisation; the layout inside a page is private to
+ * the library, a page may be copied or moved as a whole).  Token p of sample i lies in
+ * page table->pages[i * stride + p / page_tokens] (int32 device memory, `count` entries a
+ * sample; stride 0: the same pages for all samples), at place p % page_tokens.  A page number
+ * outside 0 .. pages - 1 is no page: what would be written there is dropped, what
+ * would be read is zeros, and its keys do not count; so for tokens past the row's end.  Samples may
+ * share pages that are read; of two tokens that one call writes to the same place, either may be what is held of each block
+ * there, and calls that write and read the same pages have to be ordered on one stream.
+ * d: a multiple of 8, at most 256; page_tokens 1 to 65536; heads at most 16384; a page
+ * less than 2 GiB (wmdec_cache_page_bytes is 0 for sizes that are refused); count *
+ * page_tokens at most 2^31 - 2048.
+ *
+ * wmdec_cache_write stores the t tokens of k and v [n,t,heads,d] as tokens
+ * first[i] .. first[i] + t - 1 of sample i (first: int32 [n], NULL: 0; positions below 0
+ * are dropped).  counts (int32 [n], NULL: t): only the first counts[i] tokens of sample i.
+ * wmdec_cache_read is the way back, rounded once to dtype; rows of k and v from counts[i] on are
+ * left as they were.  k or v may be NULL.  Strides in elements, channels
+ * contiguous, pointers and strides multiples of 16 bytes; outputs overlap nothing.
+ * A call of 2^26 wavefronts (a head and 8 to 64 tokens of a sample each) or more is refused.
+ *
+ * wmdec_cache_attention: o = softmax over the keys (scale * q k^T) v of tq queries per
+ * sample to its first lens[i] tokens in the cache (int32 [n]; clamped to 0 .. tk and to
+ * what its row of the table holds).  tk is the host's bound on lens: it decides how the keys are divided, so
+ * a close one is faster, and the result's last bits depend on it.  counts as above: sample i has its first counts[i]
+ * queries only, and later rows of o are left as they were.  causal: the queries are the last tokens of the
+ * sample, query j sees keys 0 .. lens[i] - counts[i] + j (call it after wmdec_cache_write
+ * of the same tokens).  heads_q is a multiple of cache->heads; query head i reads key
+ * head i / (heads_q / heads).  A query that sees no key, or whose scores are all -inf, gets zeros.
+ * q, o: [n,tq,heads_q,d] of dtype as above; 0 < scale <= 2e38; o overlaps nothing.  Scores, softmax and sums are
+ * fp32; BF16 and F16 round the probabilities to dtype for the second product, F32 is
+ * fp32 throughout; F16 takes keys and values as wmdec_cache_read gives them in F16.  A sample's bits do not depend on
+ * what it is batched with.  workspace:
+ * wmdec_cache_attention_workspace_bytes(...) bytes (may be 0, and is for sizes that the
+ * call refuses), 16-byte aligned, no initialisation; one or two kernels.  A launch of 2^24 workgroups (16
+ * rows of a key head or more, and a range of its keys each) or more is refused, and
+ * one of 2^26 rows or more where keys are divided into ranges. */
+typedef struct {
+  void* data;
+  int pages, page_tokens, heads, d;
+} wmdec_cache;
+typedef struct {
+  const int* pages;
+  long long stride;
+  int count;
+} wmdec_cache_table;
+size_t wmdec_cache_page_bytes(int page_tokens, int heads, int d);
+int wmdec_cache_write(const wmdec_cache* cache, const wmdec_cache_table* table, const int* first, const int* counts,
+                      const void* k, const wmdec_strides* k_strides, const void* v, const wmdec_strides* v_strides,
+                      int dtype, int n, int t, void* stream);
+int wmdec_cache_read(const wmdec_cache* cache, const wmdec_cache_table* table, const int* first, const int* counts,
+                     void* k, const wmdec_strides* k_strides, void* v, const wmdec_strides* v_strides,
+                     int dtype, int n, int t, void* stream);
+size_t wmdec_cache_attention_workspace_bytes(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d);
+int wmdec_cache_attention(const void* q, const wmdec_strides* q_strides, const wmdec_cache* cache,
+                          const wmdec_cache_table* table, const int* lens, const int* counts, void* o,
+                          const wmdec_strides* o_strides, int dtype, float scale, int causal, int n, int tq, int tk,
+                          int heads_q, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Whole decoder:  latent z[N,latent_c,h,w] -> frame [N,out_c,8h,8w]
  * (the I_t <- VAE_Decode(z_t) step of Alg. 1 / Alg. 2).
  * Graph: conv_in 3x3; mid = ResBlock, attention, ResBlock; per level

@@ -300,3 +300,31 @@ def cross_attention(q, k, v, scale, key_lens=None, key_mask=None):
             p /= p.sum(-1, keepdims=True)
             o[i, :, h], a[i, :, h] = p @ vv, p @ np.abs(vv)
     return o, a
+
+
+# ------------------------------------------------------------------ a cache of keys and values in four bits
+CACHE_VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def cache_held(x, dtype):
+    """What the cache holds of x [..., d] that is stored as `dtype`: by blocks of 32 channels (the last may be shorter) the nearest of sixteen values
+    times a power of two, ties to the even place of the list; a block with a value that is not finite is not a number."""
+    x = np.asarray(x, dtype=np.float64)
+    out = np.empty_like(x)
+    for at in range(0, x.shape[-1], 32):
+        part = x[..., at:at + 32]
+        finite = np.isfinite(part).all(-1, keepdims=True)
+        clean = np.where(finite, part, 0.0)
+        m, e = np.frexp(np.abs(clean).max(-1, keepdims=True))            # m in 0.5 .. 1
+        e = np.clip(e - 1 - 2 + (m >= 0.875), -125, 13 if dtype == "f16" else 125)
+        e = np.where(m == 0, -125, e)
+        a = np.ldexp(np.abs(clean), -e)
+        far = np.abs(a[..., None] - CACHE_VALUES)
+        place = np.zeros(a.shape, dtype=int)
+        best = far[..., 0]
+        for i in range(1, 8):
+            better = (far[..., i] < best) | ((far[..., i] == best) & (i % 2 == 0))
+            place, best = np.where(better, i, place), np.minimum(best, far[..., i])
+        held = np.copysign(np.ldexp(CACHE_VALUES[place], e), clean)
+        out[..., at:at + 32] = np.where(finite, held, np.nan)
+    return out

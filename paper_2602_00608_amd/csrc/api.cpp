@@ -991,6 +991,125 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
   return launch_cross_attention(a, dtype, (hipStream_t)stream);
 }
 
+// ---- a cache of keys and values in four bits
+static bool cache_sizes(int page_tokens, int heads, int d) {
+  return in_range(page_tokens, 1, kCacheMaxPageTokens) && in_range(heads, 1, kCacheMaxHeads) && in_range(d, 1, kCacheMaxD) && d % 8 == 0 &&
+         cache_head_bytes(page_tokens, d) * heads < (1UL << 31);
+}
+
+size_t wmdec_cache_page_bytes(int page_tokens, int heads, int d) { return cache_sizes(page_tokens, heads, d) ? cache_head_bytes(page_tokens, d) * heads : 0; }
+
+static int check_cache(const char* who, const wmdec_cache* cache, const wmdec_cache_table* table, int n, CachePages* out) {
+  WMDEC_REQUIRE(cache && table && cache->data && (table->pages || table->count == 0), WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(n > 0 && cache->pages > 0 && cache->page_tokens > 0 && cache->heads > 0 && cache->d > 0 && table->count >= 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
+  WMDEC_REQUIRE(cache_sizes(cache->page_tokens, cache->heads, cache->d), WMDEC_ERR_UNSUPPORTED,
+                "%s: d %d must be a multiple of 8 and at most %d, page_tokens at most %d, heads at most %d, a page less than 2 GiB", who, cache->d, kCacheMaxD, kCacheMaxPageTokens,
+                kCacheMaxHeads);
+  WMDEC_REQUIRE((long)table->count * cache->page_tokens <= (1L << 31) - 2048, WMDEC_ERR_UNSUPPORTED, "%s: a row of the table holds 2^31 - 2048 tokens at most", who);
+  WMDEC_REQUIRE(aligned16(cache->data) && element_aligned(table->pages, 4), WMDEC_ERR_INVALID_ARG, "%s: misaligned pointer", who);
+  WMDEC_REQUIRE((table->stride == 0 || table->stride >= table->count || n == 1) && (double)n * table->stride < 0x1p58, WMDEC_ERR_SHAPE, "%s: rows of the table overlap", who);
+  out->data = (unsigned char*)cache->data;
+  out->table = table->pages; out->table_stride = n == 1 ? 0 : (long)table->stride; out->table_pages = table->count;
+  out->pages = cache->pages; out->page_tokens = (unsigned)cache->page_tokens;
+  out->inv_page_tokens = cache->page_tokens == 1 ? 0xffffffffu : (unsigned)((1UL << 32) / (unsigned)cache->page_tokens);
+  out->head_bytes = (unsigned)cache_head_bytes(cache->page_tokens, cache->d);
+  out->page_bytes = out->head_bytes * (unsigned)cache->heads;
+  out->heads = cache->heads; out->d = cache->d;
+  return WMDEC_OK;
+}
+
+static int check_cache_states(const char* who, const void* p, const wmdec_strides* s, int n, int t, int heads, size_t es) {
+  if (!p) return WMDEC_OK;
+  WMDEC_REQUIRE(s, WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(strides_in_range(*s, n, t, heads), WMDEC_ERR_INVALID_ARG, "%s: a stride is negative or too large", who);
+  WMDEC_REQUIRE(aligned16(p) && s->sample * es % 16 == 0 && s->token * es % 16 == 0 && s->head * es % 16 == 0, WMDEC_ERR_INVALID_ARG,
+                "%s: pointers and strides must be multiples of 16 bytes", who);
+  return WMDEC_OK;
+}
+
+static int check_cache_tokens(const char* who, const wmdec_cache* cache, const wmdec_cache_table* table, const int* first, const int* counts, const void* k,
+                              const wmdec_strides* ks, const void* v, const wmdec_strides* vs, int dtype, int n, int t, CacheTokens* a) {
+  WMDEC_REQUIRE(valid_dtype(dtype), WMDEC_ERR_INVALID_ARG, "%s: bad dtype", who);
+  WMDEC_REQUIRE(k || v, WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(n > 0 && t > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
+  int rc = check_cache(who, cache, table, n, &a->pages);
+  if (rc == WMDEC_OK) rc = check_cache_states(who, k, ks, n, t, cache->heads, dtype_size(dtype));
+  if (rc == WMDEC_OK) rc = check_cache_states(who, v, vs, n, t, cache->heads, dtype_size(dtype));
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(element_aligned(first, 4) && element_aligned(counts, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  WMDEC_REQUIRE(k != cache->data && v != cache->data, WMDEC_ERR_INVALID_ARG, "%s: the cache must not overlap the states", who);
+  WMDEC_REQUIRE(t <= (1 << 30) && cache_tokens_fit(n, t, cache->heads, cache->d), WMDEC_ERR_UNSUPPORTED, "%s: too many tokens", who);
+  a->first = first; a->counts = counts;
+  a->k = const_cast<void*>(k); a->v = const_cast<void*>(v);
+  if (k) a->ks = *ks;
+  if (v) a->vs = *vs;
+  a->n = n; a->t = t;
+  return WMDEC_OK;
+}
+
+int wmdec_cache_write(const wmdec_cache* cache, const wmdec_cache_table* table, const int* first, const int* counts, const void* k, const wmdec_strides* k_strides,
+                      const void* v, const wmdec_strides* v_strides, int dtype, int n, int t, void* stream) {
+  CacheTokens a;
+  const int rc = check_cache_tokens("cache_write", cache, table, first, counts, k, k_strides, v, v_strides, dtype, n, t, &a);
+  return rc != WMDEC_OK ? rc : launch_cache_write(a, dtype, (hipStream_t)stream);
+}
+
+int wmdec_cache_read(const wmdec_cache* cache, const wmdec_cache_table* table, const int* first, const int* counts, void* k, const wmdec_strides* k_strides, void* v,
+                     const wmdec_strides* v_strides, int dtype, int n, int t, void* stream) {
+  const char* who = "cache_read";
+  CacheTokens a;
+  const int rc = check_cache_tokens(who, cache, table, first, counts, k, k_strides, v, v_strides, dtype, n, t, &a);
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(k != v && (!k || distinct(a.ks, n, t, cache->heads)) && (!v || distinct(a.vs, n, t, cache->heads)), WMDEC_ERR_INVALID_ARG,
+                "%s: outputs must not overlap each other or themselves", who);
+  return launch_cache_read(a, dtype, (hipStream_t)stream);
+}
+
+// (rows of a key head and keys are checked before anything is reckoned with them in 32 bits)
+static bool cache_attention_sizes(int dtype, int n, int tq, int tk, int heads_q, int heads, int d) {
+  const long most = (1L << 31) - 2048;
+  return (long)tq * (heads_q / heads) <= most && tk <= most && cache_attention_fits(dtype, n, tq, tk, heads, heads_q / heads, d);
+}
+
+size_t wmdec_cache_attention_workspace_bytes(int dtype, int n, int tq, int tk, int heads_q, int heads_kv, int d) {
+  if (!valid_dtype(dtype) || tk < 0 || n <= 0 || tq <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q % heads_kv || !cache_sizes(1, heads_kv, d) ||
+      !cache_attention_sizes(dtype, n, tq, tk, heads_q, heads_kv, d))
+    return 0;
+  return cache_attention_scratch_bytes(dtype, n, tq, tk, heads_kv, heads_q / heads_kv, d);
+}
+
+int wmdec_cache_attention(const void* q, const wmdec_strides* q_strides, const wmdec_cache* cache, const wmdec_cache_table* table, const int* lens,
+                          const int* counts, void* o, const wmdec_strides* o_strides, int dtype, float scale, int causal, int n, int tq, int tk, int heads_q,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "cache_attention";
+  WMDEC_REQUIRE(valid_dtype(dtype), WMDEC_ERR_INVALID_ARG, "%s: bad dtype", who);
+  WMDEC_REQUIRE(q && o && lens, WMDEC_ERR_INVALID_ARG, "%s: null pointer", who);
+  WMDEC_REQUIRE(n > 0 && tq > 0 && tk >= 0 && heads_q > 0, WMDEC_ERR_INVALID_ARG, "%s: non-positive size", who);
+  CacheAttentionArgs a;
+  int rc = check_cache(who, cache, table, n, &a.pages);
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(heads_q % cache->heads == 0, WMDEC_ERR_SHAPE, "%s: %d query heads are no multiple of %d key heads", who, heads_q, cache->heads);
+  rc = check_cache_states(who, q, q_strides, n, tq, heads_q, dtype_size(dtype));
+  if (rc == WMDEC_OK) rc = check_cache_states(who, o, o_strides, n, tq, heads_q, dtype_size(dtype));
+  if (rc != WMDEC_OK) return rc;
+  WMDEC_REQUIRE(scale > 0.f && scale <= 2e38f, WMDEC_ERR_INVALID_ARG, "%s: scale must be positive and at most 2e38", who);   // (times log2(e) still finite)
+  WMDEC_REQUIRE(o != q && o != cache->data && q != cache->data && distinct(*o_strides, n, tq, heads_q), WMDEC_ERR_INVALID_ARG, "%s: o must not overlap the inputs or itself", who);
+  WMDEC_REQUIRE(element_aligned(lens, 4) && element_aligned(counts, 4), WMDEC_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  WMDEC_REQUIRE(cache_attention_sizes(dtype, n, tq, tk, heads_q, cache->heads, cache->d), WMDEC_ERR_UNSUPPORTED, "%s: too many rows", who);
+  a.group = heads_q / cache->heads;
+  const size_t need = cache_attention_scratch_bytes(dtype, n, tq, tk, cache->heads, a.group, cache->d);
+  WMDEC_REQUIRE(need == 0 || (workspace && aligned16(workspace) && workspace_bytes >= need), WMDEC_ERR_WORKSPACE,
+                "%s: workspace needs %zu 16-byte aligned bytes, got %zu", who, need, workspace ? workspace_bytes : (size_t)0);
+  a.q = q; a.o = o;
+  a.qs = *q_strides; a.os = *o_strides;
+  a.lens = lens; a.counts = counts; a.scale = scale; a.causal = causal ? 1 : 0;
+  a.n = n; a.tq = tq; a.tk = tk;
+  const long held = (long)table->count * cache->page_tokens;
+  a.reach = held < tk ? (int)held : tk;
+  a.scratch = workspace;
+  return launch_cache_attention(a, dtype, (hipStream_t)stream);
+}
+
 // ---- decoder
 void decoder_default_config(wmdec_decoder_config* cfg) {
   if (!cfg) return;

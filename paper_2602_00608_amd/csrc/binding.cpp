@@ -26,6 +26,10 @@ decltype(&wmdec_adaln_fused_projection) g_adaln;
 decltype(&wmdec_residual_norm) g_residual_norm;
 decltype(&wmdec_rope) g_rope;
 decltype(&wmdec_cross_attention) g_cross_attention;
+decltype(&wmdec_cache_page_bytes) g_cache_page_bytes;
+decltype(&wmdec_cache_write) g_cache_write;
+decltype(&wmdec_cache_read) g_cache_read;
+decltype(&wmdec_cache_attention) g_cache_attention;
 
 constexpr Py_ssize_t kBind = 8;   // arguments of bind(): as many as no other function has
 
@@ -379,6 +383,92 @@ PyObject* cross_attention(PyObject*, PyObject* const* a, Py_ssize_t na) {
                                  bytes, stream));
 }
 
+// a Cache (data, page_tokens, heads, d) and its table; fills in what the library takes
+bool cache(StridedReader& r, int at, int at_table, int64_t n, wmdec_cache& c, wmdec_cache_table& t) {
+  if (r.ok && !g_cache_attention) { r.ok = false; PyErr_SetString(PyExc_RuntimeError, "the entry points have not been bound"); }
+  if (!r.ok) return false;
+  PyObject* spec = r.args[at];
+  if (!PyTuple_Check(spec) || PyTuple_GET_SIZE(spec) != 4) { r.fail(PyExc_TypeError, "a Cache is expected", at); return false; }
+  PyObject* const* outer = r.args;
+  r.args = &PyTuple_GET_ITEM(spec, 0);
+  const at::Tensor* data = r.need(0, 2);
+  r.dense(data, 0);
+  c.page_tokens = r.integer(1); c.heads = r.integer(2); c.d = r.integer(3);
+  r.args = outer;
+  if (!r.ok) return false;
+  c.data = r.address_of(data); c.pages = (int)data->size(0);
+  const size_t bytes = g_cache_page_bytes(c.page_tokens, c.heads, c.d);   // (0: the library refuses these sizes, and says why)
+  if (data->scalar_type() != at::kByte || (bytes && (size_t)data->size(1) != bytes)) { r.fail(PyExc_ValueError, "the cache's data are uint8 [pages, cache_page_bytes]", at); return false; }
+  const at::Tensor* table = r.need(at_table, 2);
+  if (!r.ok) return false;
+  if (table->scalar_type() != at::kInt || table->size(0) != n) { r.fail(PyExc_ValueError, "sizes or type do not match", at_table); return false; }
+  t.pages = (const int*)r.address_of(table); t.count = (int)table->size(1); t.stride = n > 1 ? table->stride(0) : 0;
+  return r.ok;
+}
+
+// k, v, cache, table, first, counts, device, stream: of wmdec_cache_write and wmdec_cache_read
+template <typename F> PyObject* cache_tokens(const char* who, F function, PyObject* const* a, Py_ssize_t na) {
+  StridedReader r(who, a, na, 8, 6);
+  const at::Tensor *k = r.ok ? r.get(0, 4) : nullptr, *v = r.ok ? r.get(1, 4) : nullptr, *x = k ? k : v;
+  if (r.ok && !x) r.fail(PyExc_TypeError, "tensor expected", 0);
+  if (!r.ok) return nullptr;
+  const int dt = r.type_of(x, 0);
+  if (k && v) r.same(v, k, 1);
+  const int64_t n = x->size(0);
+  wmdec_cache c{};
+  wmdec_cache_table t{};
+  if (!cache(r, 2, 3, n, c, t)) return nullptr;
+  if (x->size(2) != c.heads || x->size(3) != c.d) r.fail(PyExc_ValueError, "sizes or type do not match", k ? 0 : 1);
+  const int *first = (const int*)r.typed(4, {n}, {at::kInt}), *counts = (const int*)r.typed(5, {n}, {at::kInt});
+  const wmdec_strides ks = r.strides(k), vs = r.strides(v);
+  void *pk = r.address_of(k), *pv = r.address_of(v);
+  void* stream = r.address(7);
+  WMDEC_RETURN(function(&c, &t, first, counts, pk, &ks, pv, &vs, dt, (int)n, (int)x->size(1), stream));
+}
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return cache_tokens("cache_write", [](auto... v) { return g_cache_write(v...); }, a, na);
+}
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return cache_tokens("cache_read", [](auto... v) { return g_cache_read(v...); }, a, na);
+}
+
+// q, cache, table, lens, o, scale, tk, causal, counts, workspace, device, stream
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  StridedReader r("cache_attention", a, na, 12, 10);
+  const at::Tensor *q = r.need(0, 4), *o = r.ok ? r.need(4, 4) : nullptr;
+  if (!r.ok) return nullptr;
+  const int dt = r.type_of(q, 0);
+  r.same(o, q, 4);
+  const int64_t n = q->size(0);
+  wmdec_cache c{};
+  wmdec_cache_table t{};
+  if (!cache(r, 1, 2, n, c, t)) return nullptr;
+  if (q->size(3) != c.d) r.fail(PyExc_ValueError, "sizes or type do not match", 0);
+  if (r.none(3)) r.fail(PyExc_TypeError, "tensor expected", 3);
+  const int* lens = (const int*)r.typed(3, {n}, {at::kInt});
+  const float scale = r.real(5);
+  const int tk = r.integer(6), causal = r.flag(7);
+  const int* counts = (const int*)r.typed(8, {n}, {at::kInt});
+  const at::Tensor* ws = r.get(9, 1);
+  r.dense(ws, 9);
+  const wmdec_strides qs = r.strides(q), os = r.strides(o);
+  void *pq = r.address_of(q), *po = r.address_of(o), *pw = r.address_of(ws);
+  const size_t bytes = r.ok && ws ? (size_t)ws->nbytes() : 0;
+  void* stream = r.address(11);
+  WMDEC_RETURN(g_cache_attention(pq, &qs, &c, &t, lens, counts, po, &os, dt, scale, causal, (int)n, (int)q->size(1), tk, (int)q->size(2), pw, bytes, stream));
+}
+
+// the addresses of these four, in the order of wmdec.py
+PyObject* bind_cache(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  Reader r("bind_cache", a, na, 4);
+  void* f[4];
+  for (int i = 0; i < 4; ++i) f[i] = r.address(i);
+  if (!r.ok) return nullptr;
+  g_cache_page_bytes = (decltype(g_cache_page_bytes))f[0]; g_cache_write = (decltype(g_cache_write))f[1]; g_cache_read = (decltype(g_cache_read))f[2];
+  g_cache_attention = (decltype(g_cache_attention))f[3];
+  Py_RETURN_NONE;
+}
+
 // the addresses of these three, in the order of wmdec.py
 PyObject* bind_block(PyObject*, PyObject* const* a, Py_ssize_t na) {
   Reader r("bind_block", a, na, 3);
@@ -412,7 +502,8 @@ template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyObject* ent
 #define WMDEC_METHOD(name_) {#name_, (PyCFunction)(void (*)())entry<name_>, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {WMDEC_METHOD(gn_stats), WMDEC_METHOD(conv), WMDEC_METHOD(conv_shortcut), WMDEC_METHOD(conv_stats), WMDEC_METHOD(upconv),
                            WMDEC_METHOD(attention), WMDEC_METHOD(adaln), WMDEC_METHOD(residual_norm), WMDEC_METHOD(rope), WMDEC_METHOD(cross_attention),
-                           WMDEC_METHOD(bind), WMDEC_METHOD(bind_block), {nullptr, nullptr, 0, nullptr}};
+                           WMDEC_METHOD(cache_write), WMDEC_METHOD(cache_read), WMDEC_METHOD(cache_attention),
+                           WMDEC_METHOD(bind), WMDEC_METHOD(bind_block), WMDEC_METHOD(bind_cache), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

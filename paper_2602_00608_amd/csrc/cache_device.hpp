@@ -1,0 +1,445 @@
+// The kernels of attention to a cache of keys and values in four bits (kernels_cache.hip).
+//
+// A row is a token of one of the query heads that share a key head.  With a = scale * log2(e) and m the largest of a row's a q.k so far, o = sum_j 2^(a q.k_j - m) v_j
+// and l = sum_j 2^(a q.k_j - m) are formed in one pass over the keys; o / l is what comes out.  Keys and values are widened to 16 bits on their way into the matrix
+// cores, which rounds nothing (cache_pages.hpp); fp32 queries and probabilities go in as the three bf16 numbers that they are the sum of (24 bits: exact, and
+// three products of 16 bits where products of 32 would take eight times as long).
+#pragma once
+#include <algorithm>
+
+#include "cache_pages.hpp"
+
+namespace wmdec {
+
+constexpr int kFewRows = 16, kCacheMaxSplits = 128;
+
+// How the work is divided (kernels_cache.hip decides).  A block is a number of rows of a key head; its keys are a workgroup's each `range` of them.  Blocks that need
+// one range only write the output, the others partial outputs, and a second launch joins these.
+struct CachePlan {
+  int nb = 1;                                        // blocks of 32 channels
+  int rows = 0, row_blocks = 0, range = 0, splits = 1;
+  __host__ __device__ int block_rows() const { return rows < kFewRows ? rows : kFewRows; }   // of partial outputs
+};
+struct CacheLaunch {
+  CacheAttentionArgs a;
+  CachePlan plan;
+  float* part;                                       // [sample][key head][row block][split][block_rows][32 nb] sums of probabilities times values
+  float2* ml;                                        // [sample][key head][row block][split][block_rows] reference and sum of the probabilities
+};
+
+template <typename T> struct CacheOperand { typedef T type; static constexpr int pieces = 1; };   // what the matrix cores get
+template <> struct CacheOperand<float> { typedef bf16_t type; static constexpr int pieces = 3; };
+
+// the sum of the pieces is x (to 24 bits)
+__device__ __forceinline__ void split3(float a, float b, unsigned (&w)[3]) {
+  w[0] = pack2<bf16_t>(a, b);
+  a -= unpack_lo<bf16_t>(w[0]); b -= unpack_hi<bf16_t>(w[0]);
+  w[1] = pack2<bf16_t>(a, b);
+  a -= unpack_lo<bf16_t>(w[1]); b -= unpack_hi<bf16_t>(w[1]);
+  w[2] = pack2<bf16_t>(a, b);
+}
+
+// what is in the cache for a sample, and how far a block of rows sees of it
+struct CacheView {
+  int len, count;                                    // tokens of the sample, rows of tokens among the queries
+  int rows;                                          // rows of a key head
+  int end;                                           // keys that the block's rows see at most
+};
+__device__ __forceinline__ CacheView view_of(const CacheAttentionArgs& a, int n, int first_row, int block_rows) {
+  CacheView v;
+  v.len = min(max(a.lens[n], 0), a.reach);
+  v.count = a.counts ? min(max(a.counts[n], 0), a.tq) : a.tq;
+  v.rows = v.count * a.group;
+  const int last = min(first_row + block_rows, v.rows) - 1;
+  v.end = a.causal ? min(v.len, max(0, v.len - v.count + last / a.group + 1)) : v.len;
+  return v;
+}
+
+__device__ __forceinline__ float cache_weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
+
+template <typename T> __device__ __forceinline__ void store_four(T* row, int at, int d, f32x4 v) {   // (d is a multiple of 8)
+  if (at >= d) return;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(row + at) = v;
+  else *reinterpret_cast<u32x2*>(row + at) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+}
+template <typename T> __device__ __forceinline__ T* output_row(const CacheAttentionArgs& a, int n, int h, int row) {
+  const int tok = row / a.group;
+  return (T*)a.o + n * a.os.sample + tok * a.os.token + (long)(h * a.group + (row - tok * a.group)) * a.os.head;
+}
+
+// 16-byte chunk c of row r of a tile of `chunks` to a row lies at c ^ turn: eight rows of a chunk, and four rows of two, have banks of their own
+template <int CHUNKS> __device__ __forceinline__ int tile_turn(int row) {
+  if constexpr (CHUNKS % 8 == 0) return ((row & 3) << 1) | ((row >> 2) & 1);
+  else return (row & 2) | ((row >> 2) & 1);
+}
+
+constexpr float kCacheSlack = 8.0f;   // log2 of how far a maximum may exceed the reference before that moves
+
+template <int N> struct Words { unsigned w[N]; };
+
+// ---------------------------------------------------------------- few rows
+// A wavefront takes 16 rows and every fourth 32 keys of its workgroup's range by itself: S^T = K Q^T of 16x16x32 products, whose keys come straight from memory (a lane
+// has 1 / 4 of a key's channels; the queries are in the same order), the softmax, and O^T += V^T P^T with the values turned in LDS.  The next 32 keys are on
+// their way meanwhile.
+template <typename T, int NB> constexpr int kFewWaves = sizeof(T) == 4 ? (NB <= 2 ? 3 : NB <= 5 ? 2 : 1) : NB <= 2 ? 4 : NB <= 4 ? 3 : 2;   // a SIMD
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(CacheLaunch launch) {
+  typedef typename CacheOperand<T>::type O;
+  constexpr int PIECES = CacheOperand<T>::pieces, CH = 4 * NB, ROW = 16 * NB, EXP = exponent_bytes(NB), D = 32 * NB, TILES = 2 * NB, RED = D + 4;
+  constexpr int TILE_BYTES = 32 * CH * 16, JOIN_BYTES = 2 * 16 * (RED + 2) * 4, SMEM = 4 * TILE_BYTES > JOIN_BYTES ? 4 * TILE_BYTES : JOIN_BYTES;
+  __shared__ __align__(16) unsigned char smem[SMEM];
+  const CacheAttentionArgs& a = launch.a;
+  const CachePages& cp = a.pages;
+  const CachePlan& p = launch.plan;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // workgroup id -> (sample, key head, range, row block); the ids of one XCD (id % 8) are neighbours within a sample, and row blocks share their keys
+  const int per_sample = cp.heads * p.splits * p.row_blocks, n = blockIdx.x / per_sample;
+  int L;
+  {
+    const int i = blockIdx.x - n * per_sample, per = per_sample / 8, rem = per_sample % 8, x = i % 8, j = i / 8;
+    L = x * per + (x < rem ? x : rem) + j;
+  }
+  const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits);
+  const CacheView view = view_of(a, n, rb * kFewRows, kFewRows);
+  if (rb * kFewRows >= view.rows) return;
+  const int begin = (int)min((long)split * p.range, (long)view.end), end = (int)min((long)begin + p.range, (long)view.end);
+  if (split > 0 && begin >= end) return;
+  const bool whole = view.end <= p.range;            // the block has one range
+
+  // ---- queries: lane (row l16, g) has channels 8 (NB g + s) .. + 7
+  const int row = rb * kFewRows + l16, row_tok = row / a.group;
+  u32x4 q[NB][PIECES];
+  {
+    const int r = min(row, view.rows - 1), tok = r / a.group, hq = h * a.group + (r - tok * a.group);
+    const T* src = (const T*)a.q + n * a.qs.sample + tok * a.qs.token + hq * a.qs.head;
+#pragma unroll
+    for (int s = 0; s < NB; ++s) {
+      const int at = 8 * (NB * g + s);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) q[s][i] = u32x4{0, 0, 0, 0};
+      if (at < cp.d) {
+        if constexpr (sizeof(T) == 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(src + at), y = *reinterpret_cast<const f32x4*>(src + at + 4);
+          unsigned w[4][3];
+          split3(x[0], x[1], w[0]); split3(x[2], x[3], w[1]); split3(y[0], y[1], w[2]); split3(y[2], y[3], w[3]);
+#pragma unroll
+          for (int i = 0; i < 3; ++i) q[s][i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
+        } else {
+          q[s][0] = *reinterpret_cast<const u32x4*>(src + at);
+        }
+      }
+    }
+  }
+
+  // ---- 32 keys: lane (key l16 of either half, g) has words NB g .. NB g + NB - 1 of a key's and a value's codes
+  struct Keys { Words<NB> k[2], v[2]; unsigned long ke[2], ve[2]; unsigned there; };
+  const int* table = cp.table + n * cp.table_stride;
+  auto numbers = [&](int k0, int (&number)[2], int (&slot)[2]) {   // pages of keys k0 + l16 and k0 + 16 + l16; none past the range
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = k0 + 16 * t + l16;
+      number[t] = -1;
+      const int page = div_rem((unsigned)key, cp.page_tokens, cp.inv_page_tokens, slot[t]);
+      if (key < end) number[t] = table[page];
+    }
+  };
+  auto ask = [&](Keys& x, const int (&number)[2], const int (&slot)[2]) {
+    x.there = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const unsigned char* page = head_of_page(cp, number[t], h);
+      x.there |= ((unsigned)__ballot(page != nullptr) & 0xffffu) << (16 * t);
+      x.k[t] = Words<NB>{};
+      x.v[t] = Words<NB>{};
+      x.ke[t] = x.ve[t] = 0;
+      if (page) {
+        const unsigned at = (unsigned)slot[t] * ROW + 4 * NB * g, values = ROW * cp.page_tokens;
+        x.k[t] = *reinterpret_cast<const Words<NB>*>(page + at);
+        x.v[t] = *reinterpret_cast<const Words<NB>*>(page + values + at);
+        const unsigned char* e = page + 2 * values + (unsigned)slot[t] * EXP;
+        typedef typename std::conditional<EXP == 1, unsigned char, typename std::conditional<EXP == 2, unsigned short, typename std::conditional<EXP == 4, unsigned, unsigned long>::type>::type>::type E;
+        x.ke[t] = *reinterpret_cast<const E*>(e);
+        x.ve[t] = *reinterpret_cast<const E*>(e + EXP * cp.page_tokens);
+      }
+    }
+  };
+  auto unit = [&](unsigned long e, int s) {          // the power of two of word NB g + s
+    const int block = NB % 4 == 0 ? NB / 4 * g + s / 4 : NB == 2 ? g / 2 : (NB * g + s) / 4;
+    if constexpr (NB == 1) return unit_of((unsigned)e);
+    const unsigned half = NB <= 4 ? (unsigned)e : block >= 4 ? (unsigned)(e >> 32) : (unsigned)e;
+    return unit_of((half >> (8 * (block & 3))) & 255u);
+  };
+
+  u32x4* tile = reinterpret_cast<u32x4*>(smem + wave * TILE_BYTES);   // [32 keys][CH] chunks of eight channels
+  // lane i of 16 reads four channels of key 4 g + i / 4, and gets channel i of the four keys
+  constexpr int VB = CH % 8 == 0 ? 4 : 2;
+  int vb[VB];
+#pragma unroll
+  for (int i = 0; i < VB; ++i) {
+    const int r = 4 * g + (l16 >> 2), c = 2 * i + ((l16 & 3) >> 1);
+    vb[i] = (r * CH + (c ^ tile_turn<CH>(r))) * 16 + (l16 & 1) * 8;
+  }
+
+  const float c = a.scale * 1.4426950408889634f;
+  // keys that the lane's row sees, and that all rows of the block see
+  const int see = a.causal ? view.len - view.count + row_tok : view.len - 1;
+  const int all_see = a.causal ? view.len - view.count + rb * kFewRows / a.group : view.len - 1;
+  f32x4 o[TILES];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // Where some rows do not see some of the keys: a block of values that is not a number is zero to the products (its codes are), as nothing times it is not
+  // nothing, and reaches the rows that see it here.
+  auto take_out = [&](Keys& x, int k0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bool any = false;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) any = any || ((x.ve[t] >> (8 * b)) & 255u) == 255u;
+      if (!__ballot(any)) continue;
+      for (int i = 0; i < 16; ++i) {
+        const unsigned lo = __builtin_amdgcn_readlane((int)x.ve[t], i), hi = __builtin_amdgcn_readlane((int)(x.ve[t] >> 32), i);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          if ((((b < 4 ? lo : hi) >> (8 * (b & 3))) & 255u) == 255u && k0 + 16 * t + i <= see) o[2 * b] = o[2 * b + 1] = f32x4{NAN, NAN, NAN, NAN};
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        if (((x.ve[t] >> (8 * b)) & 255u) == 255u) x.ve[t] &= ~(255ul << (8 * b));
+    }
+  };
+
+  auto work = [&](Keys& x, int k0) {
+    f32x4 s[2];
+    if (k0 + 31 > all_see) take_out(x, k0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NB; ++w) {
+        const u32x4 k = widen<O>(x.k[t].w[w], unit(x.ke[t], w));
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) s[t] = Mma<O>::m16(k, q[w][i], s[t]);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (the tile has been read)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = 16 * t + l16;
+#pragma unroll
+      for (int w = 0; w < NB; ++w) tile[r * CH + ((NB * g + w) ^ tile_turn<CH>(r))] = widen<O>(x.v[t].w[w], unit(x.ve[t], w));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (x.there != ~0u || k0 + 31 > all_see) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = 16 * t + 4 * g + r;
+          if (!((x.there >> at) & 1u) || k0 + at > see) s[t][r] = -INFINITY;
+        }
+    }
+    {
+      // the products are rounded as the reference is, so that the largest is at most the reference, however large both are
+#pragma clang fp contract(off)
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[t][r] = s[t][r] * c;
+          mx = __builtin_elementwise_maximum(mx, s[t][r]);
+        }
+      if (__ballot(mx > m + kCacheSlack)) {          // all lanes of a row move together
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const bool moves = mx > m + kCacheSlack;
+        const float factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+        m = moves ? mx : m;
+        l = l * factor;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) o[i] = o[i] * factor;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[t][r] = __builtin_amdgcn_exp2f(s[t][r] - ref);
+          l = l + s[t][r];
+        }
+    }
+    u32x4 pr[PIECES];                                // probabilities of keys 4 g .. + 3 of either half
+    if constexpr (PIECES == 3) {
+      unsigned w[4][3];
+      split3(s[0][0], s[0][1], w[0]); split3(s[0][2], s[0][3], w[1]); split3(s[1][0], s[1][1], w[2]); split3(s[1][2], s[1][3], w[3]);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) pr[i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
+    } else {
+      pr[0] = u32x4{pack2<O>(s[0][0], s[0][1]), pack2<O>(s[0][2], s[0][3]), pack2<O>(s[1][0], s[1][1]), pack2<O>(s[1][2], s[1][3])};
+    }
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* tptr_t;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const unsigned char* at = reinterpret_cast<const unsigned char*>(tile) + vb[i % VB] + i / VB * VB * 32;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 16 * CH * 16)));
+#pragma unroll
+      for (int j = 0; j < PIECES; ++j) o[i] = Mma<O>::m16(u32x4{lo.x, lo.y, hi.x, hi.y}, pr[j], o[i]);
+    }
+  };
+
+  {
+    int k0 = begin + 32 * wave;
+    Keys x, y;
+    int number[2], slot[2];
+    if (k0 < end) {
+      numbers(k0, number, slot);
+      ask(x, number, slot);
+      numbers(k0 + 128, number, slot);
+    }
+    while (k0 < end) {
+      ask(y, number, slot);
+      numbers(k0 + 256, number, slot);
+      work(x, k0);
+      k0 += 128;
+      if (k0 >= end) break;
+      ask(x, number, slot);
+      numbers(k0 + 256, number, slot);
+      work(y, k0);
+      k0 += 128;
+    }
+  }
+
+  // ---- the wavefronts' sums are joined: 2 and 3 to 0 and 1, then 1 to 0.  A lane has channels 16 i + 4 g .. + 3 of its row
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  float* s_o = reinterpret_cast<float*>(smem);                       // [2][16][RED]
+  float2* s_ml = reinterpret_cast<float2*>(s_o + 2 * 16 * RED);      // [2][16]
+#pragma unroll
+  for (int step = 2; step >= 1; step /= 2) {
+    __syncthreads();
+    if (wave >= step && wave < 2 * step) {
+      const int w = wave - step;
+      if (g == 0) s_ml[w * 16 + l16] = make_float2(m, l);
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) *reinterpret_cast<f32x4*>(s_o + (w * 16 + l16) * RED + 16 * i + 4 * g) = o[i];
+    }
+    __syncthreads();
+    if (wave < step) {
+      const float2 e = s_ml[wave * 16 + l16];
+      const float top = fmaxf(m, e.x), own = cache_weight(m, top), other = cache_weight(e.x, top);
+      m = top;
+      l = l * own + e.y * other;
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) o[i] = o[i] * own + *reinterpret_cast<const f32x4*>(s_o + (wave * 16 + l16) * RED + 16 * i + 4 * g) * other;
+    }
+  }
+  if (wave > 0 || row >= view.rows) return;
+  if (whole) {
+    T* dst = output_row<T>(a, n, h, row);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) store_four<T>(dst, 16 * i + 4 * g, cp.d, o[i] * inv);
+  } else {
+    const int br = p.block_rows();
+    const long at = ((((long)n * cp.heads + h) * p.row_blocks + rb) * p.splits + split) * br + l16;
+    if (g == 0) launch.ml[at] = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) *reinterpret_cast<f32x4*>(launch.part + at * D + 16 * i + 4 * g) = o[i];
+  }
+}
+
+// o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) for the rows whose keys were several ranges (`total` of all key heads, `bq` a block).  A thread takes four
+// channels of a row and every groups-th range, eight at a time; the groups of a row are joined in order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheLaunch launch, int bq, int groups, unsigned total) {
+  constexpr int QUADS = D / 4, UNITS = 256 / QUADS, B = 8;
+  __shared__ f32x4 s_num[UNITS][QUADS];
+  __shared__ float2 s_ml[UNITS];
+  const CacheAttentionArgs& a = launch.a;
+  const CachePlan& p = launch.plan;
+  const int unit = threadIdx.x / QUADS, quad = threadIdx.x % QUADS, g = unit % groups, in_block = UNITS / groups, br = p.block_rows();
+  for (unsigned r0 = blockIdx.x * in_block; r0 < total; r0 += gridDim.x * in_block) {
+    const unsigned r = min(r0 + unit / groups, total - 1), nh = r / p.rows;           // row among those of all key heads, its sample and key head
+    const int row = (int)(r - nh * p.rows), n = nh / a.pages.heads, h = nh - n * a.pages.heads, rb = row / bq, in = row - rb * bq;
+    const CacheView view = view_of(a, n, rb * bq, bq);
+    const int ranges = row < view.rows && view.end > p.range ? (view.end + p.range - 1) / p.range : 0;
+    const long pb = ((long)nh * p.row_blocks + rb) * p.splits;
+    const bool there = unit < in_block * groups && r0 + unit / groups < total && ranges > 0;
+    float top = -INFINITY, den = 0.f;
+    f32x4 num{0.f, 0.f, 0.f, 0.f};
+    auto join = [&](float m, float l, f32x4 v) {
+      const float now = fmaxf(top, m), keep = cache_weight(top, now), f = cache_weight(m, now);
+      den = den * keep + l * f;
+      num = num * keep + v * f;
+      top = now;
+    };
+    if (there && quad * 4 < a.pages.d) {
+      for (int s0 = g; s0 < ranges; s0 += B * groups) {
+        float2 e[B];
+        f32x4 v[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          const long at = (pb + min(s0 + b * groups, ranges - 1)) * br + in;
+          e[b] = launch.ml[at];
+          v[b] = *reinterpret_cast<const f32x4*>(launch.part + at * D + quad * 4);
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+          if (s0 + b * groups < ranges) join(e[b].x, e[b].y, v[b]);
+      }
+    }
+    if (groups > 1) {
+      if (unit < UNITS) {
+        s_num[unit][quad] = num;
+        if (quad == 0) s_ml[unit] = make_float2(top, den);
+      }
+      __syncthreads();
+      if (g == 0 && there)
+        for (int i = 1; i < groups; ++i) join(s_ml[unit + i].x, s_ml[unit + i].y, s_num[unit + i][quad]);
+      __syncthreads();   // (read before the next rows' are written)
+    }
+    if (g == 0 && there) store_four<T>(output_row<T>(a, n, h, row), quad * 4, a.pages.d, num * (den == 0.f ? 0.f : 1.f / den));
+  }
+}
+
+template <typename T, int NB>
+int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
+  const CachePlan& p = l.plan;
+  const int heads = l.a.pages.heads;
+  hipLaunchKernelGGL((cache_few_kernel<T, NB>), dim3((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits)), dim3(256), 0, s, l);
+  WMDEC_HIP(hipGetLastError());
+  if (p.splits > 1) {
+    constexpr int units = 256 / (8 * NB);
+    int groups = 1;
+    while (groups * 2 <= units && groups * 8 < p.splits) groups *= 2;
+    const long total = (long)l.a.n * heads * p.rows, in_block = units / groups, most = 8192;   // rows (below 2^26: cache_attention_fits); rows and most workgroups of a launch
+    hipLaunchKernelGGL((cache_join_kernel<T, 32 * NB>), dim3((unsigned)std::min(most, (total + in_block - 1) / in_block)), dim3(256), 0, s, l, kFewRows, groups, (unsigned)total);
+    WMDEC_HIP(hipGetLastError());
+  }
+  return WMDEC_OK;
+}
+
+template <typename T>
+int cache_attention_launch(const CacheLaunch& l, hipStream_t s) {
+  switch (l.plan.nb) {
+    case 1: return cache_attention_width<T, 1>(l, s);
+    case 2: return cache_attention_width<T, 2>(l, s);
+    case 3: return cache_attention_width<T, 3>(l, s);
+    case 4: return cache_attention_width<T, 4>(l, s);
+    case 5: return cache_attention_width<T, 5>(l, s);
+    case 6: return cache_attention_width<T, 6>(l, s);
+    case 7: return cache_attention_width<T, 7>(l, s);
+    default: return cache_attention_width<T, 8>(l, s);
+  }
+}
+extern template int cache_attention_launch<f16_t>(const CacheLaunch&, hipStream_t);
+extern template int cache_attention_launch<bf16_t>(const CacheLaunch&, hipStream_t);
+extern template int cache_attention_launch<float>(const CacheLaunch&, hipStream_t);
+
+}  // namespace wmdec

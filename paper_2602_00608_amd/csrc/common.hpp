@@ -236,6 +236,41 @@ bool cross_attention_fits(int dtype, int n, int tq, int tk, int heads, int group
 size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d);
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s);
 
+// kernels_cache.hip: keys and values in four bits, in pages (the layout is described in cache_device.hpp)
+struct CachePages {
+  unsigned char* data = nullptr;
+  const int* table = nullptr; long table_stride = 0;   // page numbers, a row a sample
+  int table_pages = 0, pages = 0;                      // pages of a row, of the pool
+  unsigned page_tokens = 1, inv_page_tokens = 0;       // (see div_rem)
+  unsigned page_bytes = 0, head_bytes = 0;
+  int heads = 0, d = 0;
+};
+struct CacheTokens {   // the tokens first .. first + count - 1 of every sample, beside dense keys and values (either may be missing)
+  CachePages pages;
+  const int* first = nullptr; const int* counts = nullptr;
+  void* k = nullptr; void* v = nullptr;
+  wmdec_strides ks{0, 0, 0}, vs{0, 0, 0};
+  int n = 0, t = 0;
+};
+struct CacheAttentionArgs {
+  CachePages pages;
+  const void* q = nullptr; void* o = nullptr;
+  wmdec_strides qs{0, 0, 0}, os{0, 0, 0};
+  const int* lens = nullptr; const int* counts = nullptr;
+  float scale = 1.f;
+  int causal = 0, n = 0, tq = 0, tk = 0, group = 1;
+  int reach = 0;                                       // keys that a sample has at most: tk, or what its row of the table holds
+  void* scratch = nullptr;
+};
+constexpr int kCacheMaxD = 256, kCacheMaxPageTokens = 65536, kCacheMaxHeads = 16384;
+size_t cache_head_bytes(int page_tokens, int d);
+bool cache_tokens_fit(int n, int t, int heads, int d);   // into a launch of less than 2^32 threads
+int launch_cache_write(const CacheTokens& a, int dtype, hipStream_t s);
+int launch_cache_read(const CacheTokens& a, int dtype, hipStream_t s);
+bool cache_attention_fits(int dtype, int n, int tq, int tk, int heads, int group, int d);
+size_t cache_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d);
+int launch_cache_attention(const CacheAttentionArgs& a, int dtype, hipStream_t s);
+
 // kernels_attn.hip: attention over the t tokens of a sample, head dimension 512 (q, k, v in the fragment order described there)
 size_t attention_fragment_bytes(int n, int t);
 size_t flash_attention_scratch_bytes(int n, int t);   // partial outputs of the key ranges (none where one range holds all keys)

@@ -1,0 +1,231 @@
+// A cache of keys and values in four bits: states are rounded to it as they are written, and read back.  (Attention to it: cache_device.hpp.)
+//
+// Bound by HBM: 16-bit states are 3.8 times what is held of them, so the dense side counts.  A wavefront takes tokens of one head: its reads of the
+// states are whole rows of a head, what it writes of a page lies together, and neighbouring wavefronts have the next heads of the same tokens.  A lane has eight
+// channels (16 bytes of 16-bit states, four of codes); the four lanes of a block find its largest magnitude among themselves.
+#include <algorithm>
+
+#include "cache_device.hpp"
+
+namespace wmdec {
+
+template int cache_attention_launch<f16_t>(const CacheLaunch&, hipStream_t);
+
+namespace {
+
+constexpr int kSteps = 4;   // tokens of a lane, on their way together
+
+struct TokenParams { CacheTokens a; int chunks; long units; };   // units: (sample, chunk of tokens, head), a wavefront each
+
+// tokens of a wavefront at a time
+__host__ __device__ constexpr int tokens_abreast(int nb) { return 16 / nb; }
+
+template <typename T> struct alignas(16) Eight { T v[8]; };
+
+// Calls f(step, row of the dense tensors, head's part of the page or null, slot) for the lane's tokens.
+template <int NB, typename F>
+__device__ __forceinline__ void for_tokens(const TokenParams& p, F f) {
+  constexpr int LANES = 4 * NB, ABREAST = tokens_abreast(NB);
+  const CachePages& c = p.a.pages;
+  const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= p.units) return;
+  const int lane = threadIdx.x & 63, h = (int)(unit % c.heads), chunk = (int)(unit / c.heads % p.chunks), n = (int)(unit / c.heads / p.chunks);
+  const int count = p.a.counts ? min(p.a.counts[n], p.a.t) : p.a.t;
+  const long first = p.a.first ? p.a.first[n] : 0, most = (long)c.table_pages * c.page_tokens;
+  const int own = lane / LANES;
+  int token[kSteps], number[kSteps], slot[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    token[i] = (chunk * kSteps + i) * ABREAST + own;
+    if (own >= ABREAST || token[i] >= count) token[i] = -1;
+    const long at = first + token[i];
+    number[i] = -1;
+    slot[i] = 0;
+    if (token[i] >= 0 && at >= 0 && at < most) number[i] = c.table[n * c.table_stride + div_rem((unsigned)at, c.page_tokens, c.inv_page_tokens, slot[i])];
+  }
+  f(n, h, lane % LANES, token, number, slot);
+}
+
+// 16-bit sources have no exponent above that of their type's largest value rounded down to it; f16 reads back what it wrote
+template <typename T> constexpr int kTopExponent = 125 + 127;
+template <> constexpr int kTopExponent<f16_t> = 13 + 127;
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void cache_write_kernel(TokenParams p) {
+  for_tokens<NB>(p, [&](int n, int h, int c, const int (&token)[kSteps], const int (&number)[kSteps], const int (&slot)[kSteps]) {
+    const CachePages& cp = p.a.pages;
+    Eight<T> x[2][kSteps];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const T* src = (const T*)(which ? p.a.v : p.a.k);
+      const wmdec_strides& st = which ? p.a.vs : p.a.ks;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        x[which][i] = Eight<T>{};
+        if (src && number[i] >= 0 && 8 * c < cp.d) x[which][i] = *reinterpret_cast<const Eight<T>*>(src + n * st.sample + token[i] * st.token + h * st.head + 8 * c);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      unsigned char* page = head_of_page(cp, number[i], h);
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        if (!(which ? p.a.v : p.a.k)) continue;
+        float v[8];
+        unsigned top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] = to_float(x[which][i].v[e]);
+          top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+        }
+        top = max(top, (unsigned)__shfl_xor((int)top, 1));
+        top = max(top, (unsigned)__shfl_xor((int)top, 2));
+        // the exponent of the largest value as three bits of it round, which is one more from 1.75 on
+        const int held = min(max((int)((top + 0x200000u) >> 23) - 2, 2), kTopExponent<T>);
+        const bool finite = top < 0x7f800000u;
+        const unsigned codes = finite ? narrow(v, unit_of(held)) : 0;
+        if (page) {
+          constexpr int ROW = 16 * NB, EXP = exponent_bytes(NB);
+          unsigned char* at = page + which * ROW * cp.page_tokens;
+          *reinterpret_cast<unsigned*>(at + (unsigned)slot[i] * ROW + 4 * c) = codes;
+          if (c % 4 == 0) page[(2 * ROW + which * EXP) * cp.page_tokens + slot[i] * EXP + c / 4] = (unsigned char)(finite ? held : 255);
+        }
+      }
+    }
+  });
+}
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void cache_read_kernel(TokenParams p) {
+  for_tokens<NB>(p, [&](int n, int h, int c, const int (&token)[kSteps], const int (&number)[kSteps], const int (&slot)[kSteps]) {
+    const CachePages& cp = p.a.pages;
+    if (8 * c >= cp.d) return;
+    constexpr int ROW = 16 * NB, EXP = exponent_bytes(NB);
+    unsigned codes[2][kSteps], held[2][kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const unsigned char* page = head_of_page(cp, number[i], h);
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        codes[which][i] = held[which][i] = 0;   // no page: zeros
+        if (page && (which ? p.a.v : p.a.k)) {
+          codes[which][i] = *reinterpret_cast<const unsigned*>(page + which * ROW * cp.page_tokens + (unsigned)slot[i] * ROW + 4 * c);
+          held[which][i] = page[(2 * ROW + which * EXP) * cp.page_tokens + slot[i] * EXP + c / 4];
+        }
+      }
+    }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      T* dst = (T*)(which ? p.a.v : p.a.k);
+      if (!dst) continue;
+      const wmdec_strides& st = which ? p.a.vs : p.a.ks;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        if (token[i] < 0) continue;
+        T* to = dst + n * st.sample + token[i] * st.token + h * st.head + 8 * c;
+        const float unit = unit_of(held[which][i]);
+        if constexpr (sizeof(T) == 4) {
+          const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 1),
+                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 3)};
+          *reinterpret_cast<f32x4*>(to) = f32x4{v[0].x, v[0].y, v[1].x, v[1].y};
+          *reinterpret_cast<f32x4*>(to + 4) = f32x4{v[2].x, v[2].y, v[3].x, v[3].y};
+        } else {
+          *reinterpret_cast<u32x4*>(to) = widen<T>(codes[which][i], unit);
+        }
+      }
+    }
+  });
+}
+
+int blocks_of(int d) { return (d + 31) / 32; }
+int chunks_of(int t, int d) { const int per = kSteps * tokens_abreast(blocks_of(d)); return (int)(((long)t + per - 1) / per); }
+
+template <typename T, bool WRITE, int NB>
+int launch_tokens(const TokenParams& p, hipStream_t s) {
+  const dim3 grid((unsigned)((p.units + 3) / 4));
+  if constexpr (WRITE) hipLaunchKernelGGL((cache_write_kernel<T, NB>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((cache_read_kernel<T, NB>), grid, dim3(256), 0, s, p);
+  WMDEC_HIP(hipGetLastError());
+  return WMDEC_OK;
+}
+
+template <typename T, bool WRITE>
+int launch_width(const TokenParams& p, hipStream_t s) {
+  switch (blocks_of(p.a.pages.d)) {
+    case 1: return launch_tokens<T, WRITE, 1>(p, s);
+    case 2: return launch_tokens<T, WRITE, 2>(p, s);
+    case 3: return launch_tokens<T, WRITE, 3>(p, s);
+    case 4: return launch_tokens<T, WRITE, 4>(p, s);
+    case 5: return launch_tokens<T, WRITE, 5>(p, s);
+    case 6: return launch_tokens<T, WRITE, 6>(p, s);
+    case 7: return launch_tokens<T, WRITE, 7>(p, s);
+    default: return launch_tokens<T, WRITE, 8>(p, s);
+  }
+}
+
+template <bool WRITE>
+int launch_type(const CacheTokens& a, int dtype, hipStream_t s) {
+  TokenParams p;
+  p.a = a;
+  p.chunks = chunks_of(a.t, a.pages.d);
+  p.units = (long)a.n * p.chunks * a.pages.heads;
+  if (dtype == WMDEC_F32) return launch_width<float, WRITE>(p, s);
+  return dtype == WMDEC_BF16 ? launch_width<bf16_t, WRITE>(p, s) : launch_width<f16_t, WRITE>(p, s);
+}
+
+}  // namespace
+
+size_t cache_head_bytes(int page_tokens, int d) {
+  const int nb = blocks_of(d);
+  return ((size_t)page_tokens * 2 * (16 * nb + exponent_bytes(nb)) + 15) / 16 * 16;
+}
+
+bool cache_tokens_fit(int n, int t, int heads, int d) { return (double)n * chunks_of(t, d) * heads < 0x1p26; }   // (64 threads each)
+
+int launch_cache_write(const CacheTokens& a, int dtype, hipStream_t s) { return launch_type<true>(a, dtype, s); }
+int launch_cache_read(const CacheTokens& a, int dtype, hipStream_t s) { return launch_type<false>(a, dtype, s); }
+
+// ---------------------------------------------------------------- attention: what is decided on sizes alone
+namespace {
+
+// Nothing here looks at the number of samples, so that the bits of a sample do not depend on what it is batched with.
+CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
+  CachePlan p;
+  p.nb = blocks_of(d);
+  p.rows = tq * group;
+  p.row_blocks = (p.rows + kFewRows - 1) / kFewRows;
+  const long blocks = (long)heads * p.row_blocks;
+  const long range = 512;                               // fewest keys of a range
+  const long wanted = std::max(1L, std::min({1024 / blocks, tk / range, (long)kCacheMaxSplits}));
+  p.range = (int)(((long)tk + wanted - 1) / wanted + 127) / 128 * 128;
+  if (p.range == 0) p.range = 128;
+  p.splits = std::max(1, (int)(((long)tk + p.range - 1) / p.range));
+  return p;
+}
+
+size_t part_rows(const CachePlan& p, int n, int heads) { return p.splits == 1 ? 0 : (size_t)n * heads * p.row_blocks * p.splits * p.block_rows(); }
+
+}  // namespace
+
+bool cache_attention_fits(int dtype, int n, int tq, int tk, int heads, int group, int d) {
+  const CachePlan p = plan_of(dtype, tq, tk, heads, group, d);
+  const double blocks = (double)n * heads * p.row_blocks;
+  return blocks * p.splits < 0x1p24 && (p.splits == 1 || (double)n * heads * p.rows < 0x1p26);
+}
+
+size_t cache_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d) {
+  const CachePlan p = plan_of(dtype, tq, tk, heads, group, d);
+  return part_rows(p, n, heads) * (32 * p.nb + 2) * sizeof(float);
+}
+
+int launch_cache_attention(const CacheAttentionArgs& a, int dtype, hipStream_t s) {
+  CacheLaunch l;
+  l.a = a;
+  l.plan = plan_of(dtype, a.tq, a.tk, a.pages.heads, a.group, a.pages.d);
+  l.part = (float*)a.scratch;
+  l.ml = (float2*)(l.part + part_rows(l.plan, a.n, a.pages.heads) * 32 * l.plan.nb);
+  if (dtype == WMDEC_F32) return cache_attention_launch<float>(l, s);
+  return dtype == WMDEC_BF16 ? cache_attention_launch<bf16_t>(l, s) : cache_attention_launch<f16_t>(l, s);
+}
+
+}  // namespace wmdec

@@ -56,7 +56,15 @@ class _CStrides(ctypes.Structure):
     _fields_ = [("sample", ctypes.c_longlong), ("token", ctypes.c_longlong), ("head", ctypes.c_longlong)]
 
 
-_nm, _st = ctypes.POINTER(_CNorm), ctypes.POINTER(_CStrides)
+class _CCache(ctypes.Structure):
+    _fields_ = [("data", _vp), ("pages", _i), ("page_tokens", _i), ("heads", _i), ("d", _i)]
+
+
+class _CCacheTable(ctypes.Structure):
+    _fields_ = [("pages", _vp), ("stride", ctypes.c_longlong), ("count", _i)]
+
+
+_nm, _st, _ca, _ct = (ctypes.POINTER(c) for c in (_CNorm, _CStrides, _CCache, _CCacheTable))
 
 # name -> (restype, argtypes): every symbol include/wmdec.h and include/wmdec_measure.h declare
 SIGNATURES = {
@@ -89,6 +97,11 @@ SIGNATURES = {
     "wmdec_rope": (_i, [_vp, _st, _vp, _st, _i, _vp, _st, _vp, _st, _i, _i, _vp, ctypes.c_longlong, _vp, ctypes.POINTER(_CRopeLayout), _i, _i, _i, _vp]),
     "wmdec_cross_attention_workspace_bytes": (_sz, [_i] * 7),
     "wmdec_cross_attention": (_i, [_vp, _st, _vp, _st, _vp, _st, _vp, _st, _i, _f, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
+    "wmdec_cache_page_bytes": (_sz, [_i] * 3),
+    "wmdec_cache_write": (_i, [_ca, _ct, _vp, _vp, _vp, _st, _vp, _st, _i, _i, _i, _vp]),
+    "wmdec_cache_read": (_i, [_ca, _ct, _vp, _vp, _vp, _st, _vp, _st, _i, _i, _i, _vp]),
+    "wmdec_cache_attention_workspace_bytes": (_sz, [_i] * 7),
+    "wmdec_cache_attention": (_i, [_vp, _st, _ca, _ct, _vp, _vp, _vp, _st, _i, _f, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
     "decoder_default_config": (None, [ctypes.POINTER(DecoderConfig)]),
     "decoder_create": (_i, [ctypes.POINTER(DecoderConfig), ctypes.POINTER(_vp)]),
     "decoder_destroy": (_i, [_vp]),
@@ -123,6 +136,7 @@ _native = None   # the native module, bound to the loaded library
 _BOUND = ("wmdec_gn_stats", "wmdec_gn_silu_conv3x3", "wmdec_gn_conv1x1", "wmdec_gn_silu_conv3x3_shortcut",
           "wmdec_gn_silu_conv3x3_stats", "wmdec_upsample2x_conv3x3", "wmdec_attention", "wmdec_adaln_fused_projection")
 _BOUND_BLOCK = ("wmdec_residual_norm", "wmdec_rope", "wmdec_cross_attention")   # ... and of its bind_block()
+_BOUND_CACHE = ("wmdec_cache_page_bytes", "wmdec_cache_write", "wmdec_cache_read", "wmdec_cache_attention")   # ... and of its bind_cache()
 
 
 def lib():
@@ -144,6 +158,7 @@ def lib():
                                "`python -m paper_2602_00608_amd.build`; there is no fallback path" % e) from e
         _binding.bind(*(ctypes.cast(getattr(l, name), _vp).value for name in _BOUND))
         _binding.bind_block(*(ctypes.cast(getattr(l, name), _vp).value for name in _BOUND_BLOCK))
+        _binding.bind_cache(*(ctypes.cast(getattr(l, name), _vp).value for name in _BOUND_CACHE))
         _native = _binding   # (before _lib: another thread takes a set _lib for both)
         _lib = l
     return _lib
@@ -344,6 +359,38 @@ def cross_attention(q, k, v, o, scale, key_lens=None, key_mask=None, workspace=N
     """o = softmax(scale * q k^T) v over the keys below key_lens[n] (int32 [n]) whose key_mask [n,tk] (bool or uint8) is set.
     q, o [n,tq,heads_q,d]; k, v [n,tk,heads_kv,d]; strides are free but for the channels'."""
     _check(_ops().cross_attention(q, k, v, o, scale, key_lens, key_mask, workspace, _device(), _stream()))
+
+
+# ------------------------------------------------------------------ a cache of keys and values in four bits
+Cache = collections.namedtuple("Cache", "data page_tokens heads d")
+Cache.__doc__ = """Pages of keys and values in four bits: data uint8 [pages, cache_page_bytes(page_tokens, heads, d)], contiguous, on the GPU."""
+
+
+def cache_page_bytes(page_tokens, heads, d):
+    """Bytes of a page of page_tokens tokens; 0 for sizes that are refused."""
+    return lib().wmdec_cache_page_bytes(page_tokens, heads, d)
+
+
+def cache_write(k, v, cache, table, first=None, counts=None):
+    """Stores k and v [n,t,heads,d] (one of them may be None) as tokens first[n] .. of every sample, counts[n] of them (int32 [n]; None: 0, t).
+    table: int32 [n, pages of a sample], page numbers of the cache (its rows may be expanded); strides are free but for the channels'."""
+    _check(_ops().cache_write(k, v, cache, table, first, counts, _device(), _stream()))
+
+
+def cache_read(cache, table, k_out, v_out, first=None, counts=None):
+    """The way back: tokens first[n] .. into k_out and v_out [n,t,heads,d] (one of them may be None); rows from counts[n] on stay as they are."""
+    _check(_ops().cache_read(k_out, v_out, cache, table, first, counts, _device(), _stream()))
+
+
+def cache_attention_workspace_bytes(q, cache, tk):
+    n, tq, hq, d = q.shape
+    return lib().wmdec_cache_attention_workspace_bytes(dtype_enum(q), n, tq, tk, hq, cache.heads, d)
+
+
+def cache_attention(q, cache, table, lens, o, scale, tk, causal=False, counts=None, workspace=None):
+    """o = softmax(scale * q k^T) v over the first lens[n] tokens of every sample in the cache (int32 [n], at most tk).
+    q, o [n,tq,heads_q,d]; causal: the queries are the last counts[n] (None: tq) tokens; rows of o from counts[n] on stay as they are."""
+    _check(_ops().cache_attention(q, cache, table, lens, o, scale, tk, causal, counts, workspace, _device(), _stream()))
 
 
 # ------------------------------------------------------------------ decoder

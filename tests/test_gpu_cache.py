@@ -1,0 +1,470 @@
+"""The cache of keys and values in four bits on the GPU, against the oracle in 64 bits.
+
+What is held is defined to the bit, so writing and reading back are compared for equality.  The tolerance of attention is a bound, element by element:
+half a step of the stored type for every rounding to it, and for fp32 arithmetic 2^-24 of the magnitudes that go into an element times the roundings on its way."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ref
+from paper_2602_00608_amd import synth, wmdec
+from tests import gpu_util as G
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {"f32": U, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}          # half a step, relative to the value
+TINY = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -25}   # half a step of the smallest numbers
+MARK = 7.0                                                        # what lies where nothing is to be written
+
+
+def rng(seed):
+    return np.random.default_rng(synth.SEED_BASE + 9000 + seed)
+
+
+def dev(a, dtype):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(G.TORCH[dtype]).cuda()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def ints(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+def new_cache(pages, page, hk, d, fill=255):
+    """A cache inside a larger allocation; what it holds at first is of no consequence.  (256 bytes on both sides are checked by the second result.)"""
+    size = pages * wmdec.cache_page_bytes(page, hk, d)
+    big = torch.full((size + 512,), fill, dtype=torch.uint8, device="cuda")
+    big[:256] = 77
+    big[256 + size:] = 77
+
+    def check():
+        assert bool((big[:256] == 77).all()) and bool((big[256 + size:] == 77).all()), "out-of-bounds write"
+    return wmdec.Cache(big[256:256 + size].view(pages, -1), page, hk, d), check
+
+
+def tables(r, n, per, spare=2):
+    """Pages of n samples, no two alike, in no order."""
+    return r.permutation(n * per + spare)[:n * per].reshape(n, per), n * per + spare
+
+
+def same_values(got, want):
+    """Equal values, sign of zero included; not a number where it is wanted."""
+    got, want = np.asarray(got), np.asarray(want)
+    bad = ~((got == want) & (np.signbit(got) == np.signbit(want)) | (np.isnan(got) & np.isnan(want)))
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
+
+
+# ------------------------------------------------------------------ writing and reading back
+def run_store(dtype, n, t, hk, d, page, first=None, counts=None, place=lambda s: s, seed=0, values=None, out_dtype=None, spoil=0):
+    """Writes, reads back and compares with the oracle; `spoil` table entries are no pages."""
+    r = rng(seed)
+    k, v = (G.stored(r.standard_normal((n, t, hk, d)) * np.exp2(r.integers(-6, 6, (n, t, hk, 1))), dtype) if values is None else G.stored(values, dtype) for _ in range(2))
+    f = np.zeros(n, int) if first is None else np.asarray(first)
+    c = np.full(n, t) if counts is None else np.asarray(counts)
+    per = max(1, -(-int((f + t).max()) // page))
+    table, pages = tables(r, n, per)
+    for _ in range(spoil):
+        table[r.integers(n), r.integers(per)] = r.choice([-1, pages, 2 ** 31 - 1, -2 ** 31])
+    cache, check = new_cache(pages, page, hk, d)
+    before = cache.data.clone()
+    ft, ct = None if first is None else ints(first), None if counts is None else ints(counts)
+    wmdec.cache_write(place(dev(k, dtype)), place(dev(v, dtype)), cache, ints(table), ft, ct)
+    used = np.zeros(pages, bool)
+    for b in range(n):
+        for i in range(min(max(c[b], 0), t)):
+            p = f[b] + i
+            if 0 <= p < per * page and 0 <= table[b, p // page] < pages:
+                used[table[b, p // page]] = True
+    assert torch.equal(cache.data[torch.from_numpy(~used).cuda()], before[torch.from_numpy(~used).cuda()])     # pages that no token lies in
+    out = out_dtype or dtype
+    ko, vo = (torch.full((n, t, hk, d), MARK, dtype=G.TORCH[out], device="cuda") for _ in range(2))
+    kp, vp = place(ko), place(vo)
+    wmdec.cache_read(cache, ints(table), kp, vp, ft, ct)
+    torch.cuda.synchronize()
+    check()
+    for x, o in ((k, kp), (v, vp)):
+        want = ref.cache_held(x, dtype)
+        for b in range(n):
+            for i in range(t):
+                p = f[b] + i
+                if i >= c[b]:
+                    want[b, i] = MARK
+                elif not (0 <= p < per * page and 0 <= table[b, p // page] < pages):
+                    want[b, i] = 0.0
+        with np.errstate(over="ignore"):
+            same_values(host(o), want if out == dtype else torch.from_numpy(want).to(G.TORCH[out]).double().numpy())
+    return cache, table, k, v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [8, 16, 32, 40, 64, 72, 96, 104, 128, 136, 160, 192, 200, 224, 232, 256])
+def test_store_head_sizes(dtype, d):
+    run_store(dtype, 2, 37, 3, d, 16, seed=d)
+    run_store(dtype, 1, 1, 1, d, 1, seed=d)
+
+
+@pytest.mark.parametrize("page", [1, 2, 7, 16, 33, 64, 100, 256, 5400, 65536])
+@pytest.mark.parametrize("t", [1, 5, 130])
+def test_store_pages(page, t):
+    run_store("bf16", 2, t, 2, 64, page, seed=page)
+    run_store("f32", 2, t, 1, 72, page, first=[3, 5407], seed=page + 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_store_ragged(dtype):
+    run_store(dtype, 4, 50, 2, 96, 16, first=[0, 17, 300, 1], counts=[50, 0, 31, 1], seed=1)
+    run_store(dtype, 4, 50, 2, 40, 16, first=[5, 0, 2, 9], counts=[60, -3, 50, 49], seed=2)         # counts past both ends
+    run_store(dtype, 3, 40, 2, 64, 8, first=[-5, -40, -2 ** 31], seed=3)                          # positions below zero are dropped
+    run_store(dtype, 3, 70, 2, 64, 8, spoil=6, seed=4)                                            # entries that are no pages
+
+
+def test_store_past_the_table():
+    """Positions from the row's end on, up to those past 31 bits, are dropped, and read as zeros."""
+    for first in (60, 64, 1000, 2 ** 31 - 1):
+        cache, check = new_cache(3, 32, 2, 64)
+        k = torch.randn((1, 8, 2, 64), device="cuda").bfloat16()
+        before = cache.data.clone()
+        table = ints([[0, 2]])
+        wmdec.cache_write(k, k, cache, table, ints([first]))
+        out = torch.full_like(k, MARK)
+        wmdec.cache_read(cache, table, out, None, ints([first]))
+        inside = max(0, min(8, 64 - first))
+        same_values(host(out[:, :inside]), ref.cache_held(host(k[:, :inside]), "bf16"))
+        assert not out[:, inside:].any()
+        assert torch.equal(cache.data[1], before[1]) and (inside or torch.equal(cache.data, before))
+        check()
+    none, check = new_cache(1, 16, 1, 32)
+    x = torch.randn((2, 3, 1, 32), device="cuda")
+    wmdec.cache_write(x, x, none, torch.empty((2, 0), dtype=torch.int32, device="cuda"))     # rows without pages
+    assert bool((none.data == 255).all())
+    wmdec.cache_read(none, torch.empty((2, 0), dtype=torch.int32, device="cuda"), x, None)
+    assert not x.any()
+
+
+def every(dtype):
+    """Numbers whose rounding is next to a border, and those at the ends of the type."""
+    steps = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 0.5, 1, 1.5, 2, 3, 4, 6])
+    eps = {"f32": 2.0 ** -23, "bf16": 2.0 ** -7, "f16": 2.0 ** -10}[dtype]
+    near = np.concatenate([steps, steps * (1 + eps), steps * (1 - eps / 2), [0.0, 2.0 ** -12, 3 * 2.0 ** -9]])
+    tops = np.array([4.0, 6.0, 7.0 * (1 - eps / 2), 7.0, 7.0 * (1 + eps), 8.0 * (1 - eps / 2)])
+    big = {"f32": 127, "bf16": 127, "f16": 15}[dtype]
+    small = {"f32": -140, "bf16": -130, "f16": -24}[dtype]
+    rows = []
+    for e in list(range(small, small + 12)) + [-8, 0, 5] + list(range(big - 6, big - 1)):
+        for top in tops:
+            for at in range(0, near.size, 31):
+                part = near[at:at + 31]
+                rows.append(np.ldexp(np.concatenate([[top], part, np.zeros(31 - part.size)]), e))
+    x = np.array(rows)
+    x = np.clip(x, 0, {"f32": 3.4028234e38, "bf16": 3.3895e38, "f16": 65504.0}[dtype])
+    return x * np.where(np.arange(x.size).reshape(x.shape) % 2, 1.0, -1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_store_rounds_as_defined(dtype):
+    x = every(dtype)
+    run_store(dtype, 1, x.shape[0], 1, 32, 64, values=x[None, :, None])
+    assert np.isfinite(ref.cache_held(G.stored(x, dtype), dtype)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_store_not_finite_stays_in_its_block(dtype):
+    x = rng(5).standard_normal((1, 6, 2, 72))
+    x[0, 1, 0, 3], x[0, 2, 1, 40], x[0, 3, 0, 71], x[0, 4, 1, 0] = np.nan, np.inf, -np.inf, np.nan
+    run_store(dtype, 1, 6, 2, 72, 4, values=x)
+
+
+def test_read_in_another_type():
+    """What bf16 and fp32 wrote, rounded to f16 (past its range: infinite), and what any wrote in the wider types."""
+    x = rng(6).standard_normal((1, 40, 2, 64)) * np.exp2(rng(7).integers(-30, 22, (1, 40, 2, 1)))
+    for dtype, out in (("bf16", "f16"), ("f32", "f16"), ("f16", "f32"), ("f32", "bf16"), ("f16", "bf16"), ("bf16", "f32")):
+        run_store(dtype, 1, 40, 2, 64, 16, values=x, out_dtype=out)
+
+
+def test_store_strided():
+    def in_qkv(s):
+        n, t, h, d = s.shape
+        big = torch.full((n, t, 3, h + 1, d), MARK, dtype=s.dtype, device="cuda")
+        big[:, :, 1, :h].copy_(s)
+        return big[:, :, 1, :h]
+
+    def heads_first(s):
+        return s.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    for place in (in_qkv, heads_first):
+        for dtype in ("bf16", "f32"):
+            run_store(dtype, 3, 21, 5, 64, 16, counts=[21, 4, 0], place=place, seed=8)
+            run_store(dtype, 3, 21, 5, 40, 16, counts=[21, 4, 0], place=place, seed=8)
+
+
+def test_store_one_of_both_and_pages_shared():
+    r = rng(9)
+    k, v = (dev(r.standard_normal((1, 20, 2, 64)), "bf16") for _ in range(2))
+    cache, check = new_cache(3, 8, 2, 64)
+    table = ints([[2, 0, 1]])
+    wmdec.cache_write(k, v, cache, table)
+    both = cache.data.clone()
+    wmdec.cache_write(None, v, cache, table)
+    wmdec.cache_write(k, None, cache, table)
+    assert torch.equal(cache.data, both)
+    out = torch.empty((3, 20, 2, 64), dtype=torch.bfloat16, device="cuda")
+    wmdec.cache_read(cache, table.expand(3, 3), None, out)                     # the same pages for three samples
+    same_values(host(out), np.repeat(ref.cache_held(host(v), "bf16"), 3, 0))
+    moved = wmdec.Cache(cache.data[[1, 2, 0]].contiguous(), 8, 2, 64)          # pages are moved as a whole
+    again = torch.empty_like(k)
+    wmdec.cache_read(moved, ints([[1, 2, 0]]), again, None)
+    same_values(host(again), ref.cache_held(host(k), "bf16"))
+    check()
+
+
+def test_store_is_stable():
+    """What is held is held as itself: storing what was read back changes nothing."""
+    cache, table, k, v = run_store("bf16", 2, 33, 2, 72, 16, seed=10)
+    ko, vo = (torch.empty((2, 33, 2, 72), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    wmdec.cache_read(cache, ints(table), ko, vo)
+    kk = ko.clone()
+    wmdec.cache_write(ko, vo, cache, ints(table))
+    wmdec.cache_read(cache, ints(table), ko, None)
+    assert torch.equal(ko, kk)
+
+
+def test_store_past_32_bit_offsets():
+    page, hk, d = 65536, 8, 256                                       # 136 MiB a page: 40 of them are 5.7 GB
+    cache = wmdec.Cache(torch.empty((40, wmdec.cache_page_bytes(page, hk, d)), dtype=torch.uint8, device="cuda"), page, hk, d)
+    assert cache.data.numel() > 1 << 32
+    k, v = (torch.randn((1, 700, hk, d), device="cuda").bfloat16() for _ in range(2))
+    table, first = ints([[0, 39]]), ints([65536 - 300])
+    wmdec.cache_write(k, v, cache, table, first)
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    wmdec.cache_read(cache, table, ko, vo, first)
+    same_values(host(ko), ref.cache_held(host(k), "bf16"))
+    same_values(host(vo), ref.cache_held(host(v), "bf16"))
+
+
+# ------------------------------------------------------------------ attention
+def tolerance(dtype, q, k, want, weighted, scale, tk, v):
+    """weighted: the softmax weights times |v|.  Half a step for the output; half a step for every probability in 16 bits (and half of the smallest f16
+    number, beside a largest probability of at least one); fp32 scores that are off by 3 d + 8 roundings of |q| |k| at most (three products a channel in fp32),
+    which moves every weight by twice that; a sum of tk probabilities and exponentials good to a few steps.  And a probability below 2^-126, beside a
+    largest one of at least one, may be taken as zero, as may its products with a value: an element loses at most 2^-126 times the sum of |v| for either."""
+    d = q.shape[-1]
+    size = float(np.sqrt((q ** 2).sum(-1)).max() * np.sqrt((k ** 2).sum(-1)).max()) * scale if k.size else 0.0
+    fp32 = 2 * ((3 if dtype == "f32" else 1) * d + 8) * U * size + (math.sqrt(tk) + 64) * 2 * U
+    tol = HALF[dtype] * np.abs(want) + TINY[dtype] + fp32 * weighted
+    if dtype != "f32":
+        tol = tol + HALF[dtype] * weighted * 1.01
+    tol = tol + 2 * 2.0 ** -126 * float(np.abs(v).sum(1).max() if v.size else 0.0)
+    if dtype == "f16":
+        tol = tol + TINY["f16"] * float(np.abs(v).sum(1).max() if v.size else 0.0)
+    return tol
+
+
+def run_attend(dtype, n, tq, tk, hq, hk, d, page, lens=None, counts=None, causal=False, place=lambda s: s, std=1.5, seed=0, spoil=0, source=None, bound=None, scale=None):
+    """tk: tokens in the cache; bound: what the call is told."""
+    r = rng(500 + seed)
+    source = source or dtype
+    lens = [tk] * n if lens is None else lens
+    q = G.stored(r.standard_normal((n, tq, hq, d)) * std, dtype)
+    k, v = (G.stored(r.standard_normal((n, tk, hk, d)), source) for _ in range(2))
+    scale = float(np.float32(1 / math.sqrt(d) if scale is None else scale))
+    per = max(1, -(-tk // page))
+    table, pages = tables(r, n, per)
+    for _ in range(spoil):
+        table[r.integers(n), r.integers(per)] = r.choice([-1, pages, 2 ** 31 - 1, -2 ** 31])
+    cache, ccheck = new_cache(pages, page, hk, d)
+    if tk:
+        wmdec.cache_write(dev(k, source), dev(v, source), cache, ints(table), None, ints(np.clip(lens, 0, tk)))
+    there = np.arange(tk)[None] < np.clip(lens, 0, tk)[:, None]
+    there &= np.array([[0 <= table[b, j // page] < pages for j in range(tk)] for b in range(n)], bool).reshape(n, tk)
+    kh, vh = (np.where(there[..., None, None], ref.cache_held(x, source), 0.0) for x in (k, v))
+    big = torch.full((n, tq, hq, d), MARK, dtype=G.TORCH[dtype], device="cuda")
+    o, qd, told = place(big), place(dev(q, dtype)), tk if bound is None else bound
+    need = wmdec.cache_attention_workspace_bytes(qd, cache, told)
+    ws, wcheck = G.canaried((max(need // 4, 1),), torch.float32)
+    wmdec.cache_attention(qd, cache, ints(table), ints(lens), o, scale, told, causal=causal, counts=None if counts is None else ints(counts), workspace=ws if need else None)
+    torch.cuda.synchronize()
+    ccheck()
+    wcheck()
+    got = host(o)
+    c = np.full(n, tq) if counts is None else np.clip(counts, 0, tq)
+    for b in range(n):
+        length = int(np.clip(lens[b], 0, tk))
+        assert (got[b, c[b]:] == MARK).all()
+        groups = [(slice(0, c[b]), there[b:b + 1])]
+        if causal:
+            groups = [(slice(j, j + 1), there[b:b + 1] & (np.arange(tk) <= length - c[b] + j)[None]) for j in range(c[b])]
+        for rows, keep in groups:
+            if rows.stop == rows.start:
+                continue
+            want, weighted = ref.cross_attention(q[b:b + 1, rows], np.where(keep[..., None, None], kh[b:b + 1], 0), np.where(keep[..., None, None], vh[b:b + 1], 0), scale, None, keep)
+            tol = tolerance(dtype, q[b:b + 1], kh[b:b + 1], want, weighted, scale, tk, vh[b:b + 1])
+            bad = ~(np.abs(got[b:b + 1, rows] - want) <= tol)
+            assert not bad.any(), (b, rows, int(bad.sum()), np.argwhere(bad)[:4].tolist(), float(np.abs(got[b:b + 1, rows] - want)[bad].max()), float(np.broadcast_to(tol, want.shape)[bad].max()))
+    return o
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [8, 24, 32, 40, 64, 72, 96, 104, 128, 136, 160, 192, 200, 224, 256])
+def test_attend_head_sizes(dtype, d):
+    run_attend(dtype, 2, 3, 301, 4, 2, d, 64, lens=[301, 130], seed=d)
+    run_attend(dtype, 2, 150, 77, 2, 1, d, 16, lens=[77, 70], seed=d + 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tq", [1, 2, 15, 17, 33, 65, 129, 257])
+@pytest.mark.parametrize("tk", [1, 31, 33, 64, 127, 129, 257, 1000])
+def test_attend_lengths(dtype, tq, tk):
+    run_attend(dtype, 1, tq, tk, 2, 2, 64, 48, seed=tq + tk)
+
+
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 7, 8, 16, 33])
+def test_attend_groups(group):
+    for tq in (1, 2, 40):
+        run_attend("bf16", 2, tq, 200, 2 * group, 2, 64, 32, lens=[200, 37], seed=group)
+
+
+@pytest.mark.parametrize("page", [1, 3, 16, 31, 32, 50, 64, 100, 128, 1000, 5400])
+def test_attend_pages(page):
+    """Pages that end inside a tile, and entries that are no pages."""
+    for tq in (1, 70):
+        run_attend("bf16", 2, tq, 900, 4, 2, 64, page, lens=[900, 333], seed=page)
+        run_attend("f32", 2, tq, 300, 4, 2, 72, page, spoil=3, seed=page + 1)
+        run_attend("f16", 1, tq, 2500, 4, 2, 128, page, spoil=4, causal=tq > 1, seed=page + 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attend_causal(dtype):
+    for tq, tk in ((1, 50), (5, 5), (16, 100), (33, 33), (70, 300), (130, 130), (200, 1500)):
+        run_attend(dtype, 1, tq, tk, 4, 2, 64, 32, causal=True, seed=tq)
+    run_attend(dtype, 4, 60, 400, 6, 2, 96, 32, lens=[400, 60, 17, 0], counts=[60, 60, 17, 0], causal=True, seed=1)
+    run_attend(dtype, 3, 40, 100, 3, 3, 40, 8, lens=[10, 39, 100], causal=True, seed=2)               # more queries than tokens: the first see none
+    run_attend(dtype, 3, 140, 100, 3, 1, 64, 8, lens=[10, 0, 100], causal=True, seed=3)
+    run_attend(dtype, 3, 3, 5000, 4, 1, 128, 64, lens=[5000, 700, 2], counts=[3, 1, 2], causal=True, seed=4)
+
+
+def test_attend_nothing_to_see():
+    for tq in (1, 40, 200):
+        for causal in (False, True):
+            o = run_attend("bf16", 3, tq, 700, 2, 1, 64, 32, lens=[0, 700, -5], causal=causal, seed=3)
+            assert not o[0].any() and not o[2].any()
+    o = run_attend("f32", 2, 2, 0, 2, 2, 64, 32, lens=[0, 4], seed=4)
+    assert not o.any()
+    run_attend("f16", 2, 3, 40, 2, 2, 64, 32, lens=[1000, 2 ** 31 - 1], seed=5)                        # clamped to what is there
+
+
+def test_attend_counts_of_a_padded_batch():
+    for tq in (4, 33, 150):
+        run_attend("bf16", 4, tq, 600, 4, 2, 64, 32, lens=[600, 40, 599, 1], counts=[0, tq, 2, tq - 1], seed=6)
+        run_attend("bf16", 4, tq, 600, 4, 2, 64, 32, lens=[600, 40, 599, 1], counts=[-1, tq + 5, 2, 1], seed=7)
+
+
+def test_attend_long():
+    run_attend("bf16", 1, 1, 20000, 4, 1, 128, 256, seed=8)
+    run_attend("f32", 2, 2, 9000, 4, 2, 64, 100, lens=[9000, 4097], seed=9)
+    run_attend("f16", 1, 100, 6000, 2, 1, 64, 100, seed=10)
+    run_attend("bf16", 1, 1, 700, 4, 2, 64, 16, lens=[700], bound=100000, seed=11)                     # a bound far above, past the table
+    run_attend("bf16", 1, 150, 700, 4, 2, 64, 16, lens=[700], bound=60000, causal=True, seed=12)
+
+
+def test_attend_strided():
+    def in_qkv(s):
+        n, t, h, d = s.shape
+        big = torch.full((n, t, h + 2, d), MARK, dtype=s.dtype, device="cuda")
+        big[:, :, 1:h + 1].copy_(s)
+        return big[:, :, 1:h + 1]
+
+    def heads_first(s):
+        return s.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    for place in (in_qkv, heads_first):
+        for tq in (2, 140):
+            run_attend("bf16", 2, tq, 300, 6, 2, 72, 32, counts=[tq, tq - 1], place=place, seed=13)
+            run_attend("f32", 2, tq, 900, 6, 2, 64, 32, lens=[900, 3], place=place, seed=13)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attend_large_scores(dtype):
+    """Scores of some thousands: one key has all the weight."""
+    for tq in (2, 100):
+        run_attend(dtype, 1, tq, 200, 2, 2, 64, 32, std=300.0, seed=14)
+
+
+def test_attend_largest_probability_is_one():
+    """Scores past 2^24 of the reference's steps: the key that wins gets its value to the bit."""
+    r = rng(15)
+    for dtype in ("bf16", "f32"):
+        for tq in (1, 140):
+            k = np.zeros((1, 64, 1, 64))
+            k[0, :, 0, 0] = np.arange(64) % 2 * 4.0 + 2.0
+            k[0, 37, 0, 0] = 6144.0
+            v = np.zeros((1, 64, 1, 64))
+            v[0, :, 0, 5] = r.permutation(64) % 7
+            cache, check = new_cache(4, 16, 1, 64)
+            wmdec.cache_write(dev(k, dtype), dev(v, dtype), cache, ints([[3, 1, 0, 2]]))
+            q = torch.zeros((1, tq, 1, 64), dtype=G.TORCH[dtype], device="cuda")
+            q[..., 0] = 23000.0
+            o = torch.empty_like(q)
+            wmdec.cache_attention(q, cache, ints([[3, 1, 0, 2]]), ints([64]), o, 1.37, 64)
+            assert bool((o[..., 5] == float(ref.cache_held(v, dtype)[0, 37, 0, 5])).all())
+
+
+def test_attend_not_finite_stays_where_it_is_seen():
+    """A block that is not a number reaches the rows that see it, and no others; what lies past a sample's tokens does not matter."""
+    for tq in (4, 150):
+        k, v = (torch.randn((2, 200, 2, 64), device="cuda") for _ in range(2))
+        v[0, 190, 1, 40] = float("inf")
+        k[1, 199, 0, 3] = float("nan")
+        cache, check = new_cache(26, 16, 2, 64)
+        table = ints(np.arange(26).reshape(2, 13))
+        wmdec.cache_write(k.bfloat16(), v.bfloat16(), cache, table)
+        q = torch.randn((2, tq, 4, 64), device="cuda").bfloat16()
+        o = torch.empty_like(q)
+        wmdec.cache_attention(q, cache, table, ints([191, 199]), o, 0.125, 200, causal=True)
+        bad = torch.isnan(o)
+        want = torch.zeros_like(bad)
+        want[0, -1, 2:, 32:] = True                      # the last query alone sees token 190
+        assert torch.equal(bad, want)
+
+
+def test_attend_bits_do_not_depend_on_the_batch():
+    r = rng(16)
+    for dtype, tq, tk, hq, hk, d in (("bf16", 1, 3000, 8, 2, 128), ("f32", 3, 2000, 4, 2, 64), ("f16", 150, 2500, 4, 2, 64), ("bf16", 20, 900, 4, 1, 96)):
+        k, v, q = (dev(r.standard_normal((3, t, h, d)), dtype) for t, h in ((tk, hk), (tk, hk), (tq, hq)))
+        per = -(-tk // 64)
+        cache, _ = new_cache(3 * per, 64, hk, d)
+        table = ints(r.permutation(3 * per).reshape(3, per))
+        wmdec.cache_write(k, v, cache, table)
+        outs = []
+        for samples in ([0, 1, 2], [1], [2, 1]):
+            lens = ints([tk, tk - 411, 77])[samples]
+            qs, o = q[samples].contiguous(), torch.empty((len(samples), tq, hq, d), dtype=q.dtype, device="cuda")
+            ws = torch.empty(max(16, wmdec.cache_attention_workspace_bytes(qs, cache, tk)), dtype=torch.uint8, device="cuda")
+            wmdec.cache_attention(qs, cache, table[samples].contiguous(), lens, o, 0.1, tk, workspace=ws)
+            outs.append(o[samples.index(1)])
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_attend_equals_attention_to_what_is_read_back():
+    """The same softmax over the states that cache_read gives, in f16 from a cache that bf16 wrote too."""
+    for dtype, source in (("bf16", "bf16"), ("f16", "bf16"), ("f16", "f16"), ("f32", "bf16")):
+        for tq in (3, 140):
+            run_attend(dtype, 2, tq, 260, 4, 2, 64, 32, lens=[260, 100], source=source, seed=17)
+
+
+def test_attend_past_32_bit_offsets():
+    page, hk, d = 65536, 8, 256
+    cache = wmdec.Cache(torch.empty((40, wmdec.cache_page_bytes(page, hk, d)), dtype=torch.uint8, device="cuda"), page, hk, d)
+    k, v = (torch.randn((1, 300, hk, d), device="cuda").bfloat16() for _ in range(2))
+    table = ints([[39]])
+    wmdec.cache_write(k, v, cache, table)
+    for tq in (1, 130):
+        q = torch.randn((1, tq, hk, d), device="cuda").bfloat16()
+        o = torch.empty_like(q)
+        wmdec.cache_attention(q, cache, table, ints([300]), o, 0.0625, 300)
+        kh, vh = (ref.cache_held(host(x), "bf16") for x in (k, v))
+        want, weighted = ref.cross_attention(host(q), kh, vh, 0.0625)
+        assert (np.abs(host(o) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.0625, 300, vh)).all()
