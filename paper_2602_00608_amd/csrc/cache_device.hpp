@@ -11,14 +11,16 @@
 
 namespace wmdec {
 
-constexpr int kFewRows = 16, kCacheMaxSplits = 128;
+constexpr int kFewRows = 16, kManyRows = 128, kCacheMaxSplits = 128;
 
 // How the work is divided (kernels_cache.hip decides).  A block is a number of rows of a key head; its keys are a workgroup's each `range` of them.  Blocks that need
 // one range only write the output, the others partial outputs, and a second launch joins these.
 struct CachePlan {
   int nb = 1;                                        // blocks of 32 channels
+  bool few = true;                                   // blocks of kFewRows rows, else of kManyRows
   int rows = 0, row_blocks = 0, range = 0, splits = 1;
-  __host__ __device__ int block_rows() const { return rows < kFewRows ? rows : kFewRows; }   // of partial outputs
+  __host__ __device__ int bq() const { return few ? kFewRows : kManyRows; }
+  __host__ __device__ int block_rows() const { return rows < bq() ? rows : bq(); }   // of partial outputs
 };
 struct CacheLaunch {
   CacheAttentionArgs a;
@@ -354,6 +356,318 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
   }
 }
 
+// ---------------------------------------------------------------- many rows
+// The four wavefronts of a workgroup take 32 rows each of the same tiles of KT keys and values, which the workgroup widens into LDS while it works on the tile
+// before; the codes of the tile after that are on their way meanwhile.  Per 32 keys a wavefront forms S^T = K Q^T of 32x32x16 products (keys along the accumulator's
+// registers, one row a lane), the softmax, and O^T += V^T P^T with the probabilities as they are in their registers: an accumulator's keys of lane half lk
+// are 8 (r / 4) + 4 lk + r % 4, so V^T is read from LDS in that order of keys, transposed on the way.
+template <typename T, int NB> constexpr bool kHasMany = sizeof(T) == 2 || NB < 8;   // (the queries of 256 channels in three pieces and the outputs leave no registers)
+
+template <typename T, int NB>
+struct ManyForm {
+  static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = sizeof(T) == 4 ? (NB <= 3 ? 2 : 1) : NB <= 1 ? 4 : NB == 2 ? 3 : NB <= 5 ? 2 : 1;   // (TILE: chunks of a tile)
+  static constexpr int ITEMS = (2 * KT * NB + 255) / 256;   // blocks of 32 channels that a thread widens
+};
+
+// every LDS access of this wavefront is done, and so for the others: codes on their way are not waited for
+__device__ __forceinline__ void sync_tiles_of_cache() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kernel(CacheLaunch launch) {
+  typedef typename CacheOperand<T>::type O;
+  typedef ManyForm<T, NB> F;
+  constexpr int PIECES = CacheOperand<T>::pieces, CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ITEMS = F::ITEMS, ROW = 16 * NB, EXP = exponent_bytes(NB);
+  constexpr int GP = CH % 8 == 0 ? 8 : 4;            // chunks that are exchanged among each other
+  __shared__ __align__(16) u32x4 s_k[2 * TILE], s_v[2 * TILE];
+  __shared__ unsigned s_bad[3][2 * NB + 2];          // by tile: values that are not a number, bits of the keys of every block, and whether there are any
+  const CacheAttentionArgs& a = launch.a;
+  const CachePages& cp = a.pages;
+  const CachePlan& p = launch.plan;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lk = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // workgroup id -> (sample, key head, range, row block), as for few rows
+  const int per_sample = cp.heads * p.splits * p.row_blocks, n = blockIdx.x / per_sample;
+  int L;
+  {
+    const int i = blockIdx.x - n * per_sample, per = per_sample / 8, rem = per_sample % 8, x = i % 8, j = i / 8;
+    L = x * per + (x < rem ? x : rem) + j;
+  }
+  const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits), row0 = rb * kManyRows;
+  const CacheView view = view_of(a, n, row0, kManyRows);
+  if (row0 >= view.rows) return;
+  const int begin = (int)min((long)split * p.range, (long)view.end), end = (int)min((long)begin + p.range, (long)view.end);
+  if (split > 0 && begin >= end) return;
+  const bool whole = view.end <= p.range;
+  const int tiles = (end - begin + KT - 1) / KT;
+
+  // ---- queries: chunk 2 s + lk of the lane's row
+  const int row = row0 + wave * 32 + l32, first_row = row0 + wave * 32;
+  const bool idle = first_row >= view.rows;          // a wavefront past the last row only widens
+  u32x4 q[QS][PIECES];
+  {
+    const int r = min(row, view.rows - 1), tok = r / a.group, hq = h * a.group + (r - tok * a.group);
+    const T* src = (const T*)a.q + n * a.qs.sample + tok * a.qs.token + hq * a.qs.head;
+#pragma unroll
+    for (int s = 0; s < QS; ++s) {
+      const int at = 8 * (2 * s + lk);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) q[s][i] = u32x4{0, 0, 0, 0};
+      if (at < cp.d) {
+        if constexpr (sizeof(T) == 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(src + at), y = *reinterpret_cast<const f32x4*>(src + at + 4);
+          unsigned w[4][3];
+          split3(x[0], x[1], w[0]); split3(x[2], x[3], w[1]); split3(y[0], y[1], w[2]); split3(y[2], y[3], w[3]);
+#pragma unroll
+          for (int i = 0; i < 3; ++i) q[s][i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
+        } else {
+          q[s][0] = *reinterpret_cast<const u32x4*>(src + at);
+        }
+      }
+    }
+  }
+  // keys up to which the lane's row, all rows of the wavefront, and its last row see
+  const int behind = view.len - view.count;
+  const int see = a.causal ? behind + row / a.group : view.len - 1, all_see = a.causal ? behind + first_row / a.group : view.len - 1;
+  const int last_see = a.causal ? behind + min(first_row + 31, view.rows - 1) / a.group : view.len - 1;
+
+  // ---- tiles.  A thread widens blocks i 256 + tid of a tile: keys' blocks first, then values'
+  const int* table = cp.table + n * cp.table_stride;
+  struct Item { int number, slot; };
+  Item where[ITEMS];
+  u32x4 codes[ITEMS];
+  unsigned held[ITEMS];
+  auto item_of = [&](int i, bool& values, int& key, int& block) {
+    const int it = i * 256 + tid, rest = it < KT * NB ? it : it - KT * NB;
+    values = it >= KT * NB;
+    key = rest / NB;
+    block = rest - key * NB;
+    return it < 2 * KT * NB;
+  };
+  auto look_up = [&](int j) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      bool values;
+      int key, block;
+      const bool live = item_of(i, values, key, block);
+      const int at = begin + j * KT + key, page = div_rem((unsigned)at, cp.page_tokens, cp.inv_page_tokens, where[i].slot);
+      where[i].number = -1;
+      if (live && at < end) where[i].number = table[page];
+    }
+  };
+  auto ask = [&]() {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      bool values;
+      int key, block;
+      item_of(i, values, key, block);
+      const unsigned char* page = head_of_page(cp, where[i].number, h);
+      codes[i] = u32x4{0, 0, 0, 0};
+      held[i] = 0;
+      if (page) {
+        codes[i] = *reinterpret_cast<const u32x4*>(page + (unsigned)where[i].slot * ROW + 16 * block + (values ? ROW * cp.page_tokens : 0u));
+        held[i] = page[2 * ROW * cp.page_tokens + (unsigned)where[i].slot * EXP + block + (values ? EXP * cp.page_tokens : 0u)];
+      }
+    }
+  };
+  auto fill = [&](int j) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      bool values;
+      int key, block;
+      if (!item_of(i, values, key, block)) continue;
+      u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + key * CH;
+      const bool bad = a.causal && values && held[i] == 255u;   // (as take_out does for few rows)
+      if (bad) {
+        atomicOr(&s_bad[j % 3][2 * block + (key >> 5)], 1u << (key & 31));
+        atomicOr(&s_bad[j % 3][2 * NB], 1u);
+      }
+      const float unit = unit_of(bad ? 0u : held[i]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(key)] = widen<O>(codes[i][c], unit);
+    }
+  };
+  // valid keys of a tile, by the wavefront for itself
+  unsigned long there = 0;
+  int next_number = -1;
+  auto look_there = [&](int j) {
+    const int at = begin + j * KT + (KT == 64 ? lane : l32);
+    int slot;
+    const int page = div_rem((unsigned)at, cp.page_tokens, cp.inv_page_tokens, slot);
+    next_number = -1;
+    if (at < end) next_number = table[page];
+  };
+
+  // ---- where a lane reads its operands (chunks, and bytes, of a tile)
+  int kb[GP / 2];
+#pragma unroll
+  for (int s = 0; s < GP / 2; ++s) kb[s] = l32 * CH + ((2 * s + lk) ^ tile_turn<CH>(l32));
+  int vb[GP / 4];
+#pragma unroll
+  for (int i = 0; i < GP / 4; ++i) {   // channels 16 (l32 / 16) + 4 (lane % 4) .. + 3 of key 4 lk + lane / 4 % 4, of which the lane gets channel l32 of four keys
+    const int r = 4 * lk + ((lane >> 2) & 3), c = 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    vb[i] = (r * CH + (c ^ tile_turn<CH>(r))) * 16 + (lane & 1) * 8;
+  }
+
+  f32x16 o[NB], s[NS];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < NB; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+  const float c = a.scale * 1.4426950408889634f;
+
+  auto scores = [&](const u32x4* tk, int k0) {
+#pragma unroll
+    for (int ns = 0; ns < NS; ++ns) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[ns][r] = 0.f;
+#pragma unroll
+      for (int st = 0; st < QS; ++st) {
+        const u32x4 kf = tk[kb[st % (GP / 2)] + st / (GP / 2) * GP + ns * 32 * CH];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) s[ns] = Mma<O>::m32(kf, q[st][i], s[ns]);
+      }
+    }
+#pragma unroll
+    for (int ns = 0; ns < NS; ++ns) {
+      const int at = k0 + 32 * ns;
+      const unsigned is_there = (unsigned)(there >> (32 * ns));
+      if (is_there != ~0u || at + 31 > all_see) {
+        const int seen = see - at + 1;
+        const unsigned b = (is_there & (seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1)) >> (4 * lk);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {   // -inf where the bit is not set, in two instructions: the bit spread over the word, and a choice by it
+          const unsigned is = (unsigned)((int)(b << (31 - 8 * (r / 4) - r % 4)) >> 31);
+          s[ns][r] = __uint_as_float((is & __float_as_uint(s[ns][r])) | (~is & 0xff800000u));
+        }
+      }
+    }
+  };
+  // The reference is a rounded product.  From 2^24 on a fused multiply-add would find the largest score half a step of the reference away from it, 1 and more: there
+  // the products are rounded like the reference, and then subtracted.
+  bool far = false;   // (of any of the wavefront's rows)
+  auto round_and_subtract = [&](float ref) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = s[ns][r] * c;
+        s[ns][r] = x - ref;
+      }
+  };
+  auto maximum = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
+  auto softmax = [&]() {
+    float mx = maximum(maximum(s[0][0], s[0][1]), s[0][2]);
+#pragma unroll
+    for (int i = 3; i + 1 < 16 * NS; i += 2) mx = maximum(maximum(mx, s[i / 16][i % 16]), s[(i + 1) / 16][(i + 1) % 16]);
+    mx = maximum(mx, s[NS - 1][15]);
+    mx = half_max(mx) * c;
+    const bool moves = mx > m + kCacheSlack;
+    if (__ballot(moves)) {
+      const float to = moves ? mx : m, factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+      m = to;
+      far = __ballot(fabsf(m) >= 0x1p24f && m != -INFINITY) != 0;
+      l *= factor;
+#pragma unroll
+      for (int dt = 0; dt < NB; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= factor;
+    }
+    float ref = m == -INFINITY ? 0.f : m, by = c;
+    if (far) {
+      round_and_subtract(ref);
+      by = 1.f;
+      ref = 0.f;
+    }
+#pragma unroll
+    for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[ns][r] = __builtin_amdgcn_exp2f(fmaf(s[ns][r], by, -ref));
+        l += s[ns][r];
+      }
+  };
+  auto values = [&](const unsigned char* tv) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* tptr_t;
+#pragma unroll
+    for (int i = 0; i < 2 * NS; ++i) {               // 16 keys
+      unsigned w[4][PIECES];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = s[i / 2][8 * (i % 2) + 2 * e], y = s[i / 2][8 * (i % 2) + 2 * e + 1];
+        if constexpr (PIECES == 3) split3(x, y, w[e]);
+        else w[e][0] = pack2<O>(x, y);
+      }
+#pragma unroll
+      for (int dt = 0; dt < NB; ++dt) {
+        const unsigned char* at = tv + vb[dt % (GP / 4)] + dt / (GP / 4) * GP * 16 + i * 16 * CH * 16;
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 8 * CH * 16)));
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) o[dt] = Mma<O>::m32(u32x4{lo.x, lo.y, hi.x, hi.y}, u32x4{w[0][j], w[1][j], w[2][j], w[3][j]}, o[dt]);
+      }
+    }
+  };
+
+  if (tid < 3 * (2 * NB + 2)) s_bad[0][tid] = 0;
+  if (tiles > 0) {
+    look_up(0);
+    ask();
+    look_up(1);
+    look_there(0);
+    sync_tiles_of_cache();                           // (s_bad is clear)
+    fill(0);
+    ask();
+    look_up(2);
+  }
+  for (int j = 0; j < tiles; ++j) {
+    sync_tiles_of_cache();                           // the tile is there, and every wavefront is done with the other buffer
+    there = __ballot((unsigned)next_number < (unsigned)cp.pages);
+    if (j + 1 < tiles) {
+      fill(j + 1);
+      ask();
+      look_up(j + 3);
+      look_there(j + 1);
+    }
+    if (a.causal && tid < 2 * NB + 2) s_bad[(j + 2) % 3][tid] = 0;
+    const int k0 = begin + j * KT;
+    if (idle || k0 > last_see) continue;
+    if (a.causal && __builtin_amdgcn_readfirstlane((int)s_bad[j % 3][2 * NB])) {
+#pragma unroll
+      for (int dt = 0; dt < NB; ++dt)
+        for (int i = 0; i < KT; ++i)
+          if (((s_bad[j % 3][2 * dt + (i >> 5)] >> (i & 31)) & 1u) && k0 + i <= see)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] = NAN;
+    }
+    scores(s_k + (j & 1) * TILE, k0);
+    softmax();
+    values(reinterpret_cast<const unsigned char*>(s_v + (j & 1) * TILE));
+  }
+
+  // ---- output.  A lane holds channels 32 dt + 8 g + 4 lk .. + 3 of its row
+  l += __shfl_xor(l, 32);
+  if (row >= view.rows) return;
+  if (whole) {
+    T* dst = output_row<T>(a, n, h, row);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int dt = 0; dt < NB; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) store_four<T>(dst, 32 * dt + 8 * g + 4 * lk, cp.d, f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]} * inv);
+  } else {
+    const long at = ((((long)n * cp.heads + h) * p.row_blocks + rb) * p.splits + split) * p.block_rows() + wave * 32 + l32;
+    if (lk == 0) launch.ml[at] = make_float2(m, l);
+    float* dst = launch.part + at * D + 4 * lk;
+#pragma unroll
+    for (int dt = 0; dt < NB; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * g) = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+  }
+}
+
 // o = sum_s part_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) for the rows whose keys were several ranges (`total` of all key heads, `bq` a block).  A thread takes four
 // channels of a row and every groups-th range, eight at a time; the groups of a row are joined in order.
 template <typename T, int D>
@@ -412,14 +726,20 @@ template <typename T, int NB>
 int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const CachePlan& p = l.plan;
   const int heads = l.a.pages.heads;
-  hipLaunchKernelGGL((cache_few_kernel<T, NB>), dim3((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits)), dim3(256), 0, s, l);
+  const dim3 grid((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits));
+  if constexpr (kHasMany<T, NB>) {
+    if (p.few) hipLaunchKernelGGL((cache_few_kernel<T, NB>), grid, dim3(256), 0, s, l);
+    else hipLaunchKernelGGL((cache_many_kernel<T, NB>), grid, dim3(256), 0, s, l);
+  } else {
+    hipLaunchKernelGGL((cache_few_kernel<T, NB>), grid, dim3(256), 0, s, l);
+  }
   WMDEC_HIP(hipGetLastError());
   if (p.splits > 1) {
     constexpr int units = 256 / (8 * NB);
     int groups = 1;
     while (groups * 2 <= units && groups * 8 < p.splits) groups *= 2;
     const long total = (long)l.a.n * heads * p.rows, in_block = units / groups, most = 8192;   // rows (below 2^26: cache_attention_fits); rows and most workgroups of a launch
-    hipLaunchKernelGGL((cache_join_kernel<T, 32 * NB>), dim3((unsigned)std::min(most, (total + in_block - 1) / in_block)), dim3(256), 0, s, l, kFewRows, groups, (unsigned)total);
+    hipLaunchKernelGGL((cache_join_kernel<T, 32 * NB>), dim3((unsigned)std::min(most, (total + in_block - 1) / in_block)), dim3(256), 0, s, l, p.bq(), groups, (unsigned)total);
     WMDEC_HIP(hipGetLastError());
   }
   return WMDEC_OK;

@@ -193,10 +193,11 @@ CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   CachePlan p;
   p.nb = blocks_of(d);
   p.rows = tq * group;
-  p.row_blocks = (p.rows + kFewRows - 1) / kFewRows;
+  p.few = p.rows <= 64 || (dtype == WMDEC_F32 && !kHasMany<float, 8> && p.nb == 8);
+  p.row_blocks = (p.rows + p.bq() - 1) / p.bq();
   const long blocks = (long)heads * p.row_blocks;
   const long range = 512;                               // fewest keys of a range
-  const long wanted = std::max(1L, std::min({1024 / blocks, tk / range, (long)kCacheMaxSplits}));
+  const long wanted = std::max(1L, std::min({(p.few ? 1024 : 512) / blocks, tk / range, (long)kCacheMaxSplits}));
   p.range = (int)(((long)tk + wanted - 1) / wanted + 127) / 128 * 128;
   if (p.range == 0) p.range = 128;
   p.splits = std::max(1, (int)(((long)tk + p.range - 1) / p.range));
