@@ -1106,6 +1106,7 @@ int wmdec_cache_attention(const void* q, const wmdec_strides* q_strides, const w
   a.n = n; a.tq = tq; a.tk = tk;
   const long held = (long)table->count * cache->page_tokens;
   a.reach = held < tk ? (int)held : tk;
+  if (held == 0) { a.pages.table = lens; a.pages.table_stride = 0; a.pages.table_pages = 1; }   // (a number that may be read, and stands for no key)
   a.scratch = workspace;
   return launch_cache_attention(a, dtype, (hipStream_t)stream);
 }

@@ -11,7 +11,7 @@
 
 namespace wmdec {
 
-constexpr int kFewRows = 16, kManyRows = 128, kCacheMaxSplits = 128;
+constexpr int kFewRows = 16, kManyRows = 128, kCacheMaxSplits = 64;
 
 // How the work is divided (kernels_cache.hip decides).  A block is a number of rows of a key head; its keys are a workgroup's each `range` of them.  Blocks that need
 // one range only write the output, the others partial outputs, and a second launch joins these.
@@ -83,9 +83,10 @@ template <int N> struct Words { unsigned w[N]; };
 // A wavefront takes 16 rows and every fourth 32 keys of its workgroup's range by itself: S^T = K Q^T of 16x16x32 products, whose keys come straight from memory (a lane
 // has 1 / 4 of a key's channels; the queries are in the same order), the softmax, and O^T += V^T P^T with the values turned in LDS.  The next 32 keys are on
 // their way meanwhile.
-template <typename T, int NB> constexpr int kFewWaves = sizeof(T) == 4 ? (NB <= 2 ? 3 : NB <= 5 ? 2 : 1) : NB <= 2 ? 4 : NB <= 4 ? 3 : 2;   // a SIMD
+template <typename T, int NB> constexpr int kFewWaves = sizeof(T) == 4 ? (NB <= 2 ? 3 : NB <= 5 ? 2 : 1) : NB <= 4 ? 4 : 2;   // a SIMD
 
-template <typename T, int NB>
+// EVEN: pages hold a multiple of 32 tokens, so that 32 keys lie together in one of them: its number and address are the wavefront's, not a lane's.
+template <typename T, int NB, bool EVEN>
 __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(CacheLaunch launch) {
   typedef typename CacheOperand<T>::type O;
   constexpr int PIECES = CacheOperand<T>::pieces, CH = 4 * NB, ROW = 16 * NB, EXP = exponent_bytes(NB), D = 32 * NB, TILES = 2 * NB, RED = D + 4;
@@ -104,6 +105,19 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
     L = x * per + (x < rem ? x : rem) + j;
   }
   const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits);
+  // pages of 32 keys; where they are the wavefront's, the first are asked for before the sample's length is known
+  struct Place { int number[EVEN ? 1 : 2], slot[EVEN ? 1 : 2]; };   // of keys k0, or k0 + l16 and k0 + 16 + l16; no page past the range
+  const int* table = cp.table + n * cp.table_stride;
+  auto find_even = [&](int k0) {
+    typedef const __attribute__((address_space(4))) int* uniform_t;
+    Place w;
+    const int page = div_rem((unsigned)k0, cp.page_tokens, cp.inv_page_tokens, w.slot[0]);
+    w.number[0] = ((uniform_t)(uintptr_t)table)[min(page, cp.table_pages - 1)];   // (past the range: not used)
+    return w;
+  };
+  Place next;
+  if constexpr (EVEN) next = find_even(split * p.range + 32 * wave);
+
   const CacheView view = view_of(a, n, rb * kFewRows, kFewRows);
   if (rb * kFewRows >= view.rows) return;
   const int begin = (int)min((long)split * p.range, (long)view.end), end = (int)min((long)begin + p.range, (long)view.end);
@@ -136,41 +150,68 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
   }
 
   // ---- 32 keys: lane (key l16 of either half, g) has words NB g .. NB g + NB - 1 of a key's and a value's codes
-  struct Keys { Words<NB> k[2], v[2]; unsigned long ke[2], ve[2]; unsigned there; };
-  const int* table = cp.table + n * cp.table_stride;
-  auto numbers = [&](int k0, int (&number)[2], int (&slot)[2]) {   // pages of keys k0 + l16 and k0 + 16 + l16; none past the range
+  typedef typename std::conditional<EXP == 1, unsigned char, typename std::conditional<EXP == 2, unsigned short, typename std::conditional<EXP == 4, unsigned, unsigned long>::type>::type>::type E;
+  typedef typename std::conditional<EXP == 8, unsigned long, unsigned>::type EW;
+  struct Half { Words<NB> w[2]; EW e[2]; };          // keys, or values
+  Half xk, xv;
+  unsigned there = 0;                                // which of the 32 are keys
+  const unsigned values_at = ROW * cp.page_tokens, exps_at = 2 * values_at;
+  auto find = [&](int k0) {
+    Place w;
+    if constexpr (EVEN) {
+      w = find_even(k0);
+    } else {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int key = k0 + 16 * t + l16;
-      number[t] = -1;
-      const int page = div_rem((unsigned)key, cp.page_tokens, cp.inv_page_tokens, slot[t]);
-      if (key < end) number[t] = table[page];
+      for (int t = 0; t < 2; ++t) {
+        const int key = k0 + 16 * t + l16, page = div_rem((unsigned)key, cp.page_tokens, cp.inv_page_tokens, w.slot[t]);
+        w.number[t] = -1;
+        if (key < end) w.number[t] = table[page];
+      }
     }
+    return w;
   };
-  auto ask = [&](Keys& x, const int (&number)[2], const int (&slot)[2]) {
-    x.there = 0;
+  auto ask = [&](Half& x, bool values, const Place& w) {
+    const unsigned codes_at = values ? values_at : 0, to_exps = exps_at + (values ? EXP * cp.page_tokens : 0);
+    if constexpr (EVEN) {
+      // (no page: none of them is a key, and what page 0 has instead is taken for zeros)
+      const unsigned char* page = head_of_page(cp, (unsigned)w.number[0] < (unsigned)cp.pages ? w.number[0] : 0, h);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const unsigned char* page = head_of_page(cp, number[t], h);
-      x.there |= ((unsigned)__ballot(page != nullptr) & 0xffffu) << (16 * t);
-      x.k[t] = Words<NB>{};
-      x.v[t] = Words<NB>{};
-      x.ke[t] = x.ve[t] = 0;
-      if (page) {
-        const unsigned at = (unsigned)slot[t] * ROW + 4 * NB * g, values = ROW * cp.page_tokens;
-        x.k[t] = *reinterpret_cast<const Words<NB>*>(page + at);
-        x.v[t] = *reinterpret_cast<const Words<NB>*>(page + values + at);
-        const unsigned char* e = page + 2 * values + (unsigned)slot[t] * EXP;
-        typedef typename std::conditional<EXP == 1, unsigned char, typename std::conditional<EXP == 2, unsigned short, typename std::conditional<EXP == 4, unsigned, unsigned long>::type>::type>::type E;
-        x.ke[t] = *reinterpret_cast<const E*>(e);
-        x.ve[t] = *reinterpret_cast<const E*>(e + EXP * cp.page_tokens);
+      for (int t = 0; t < 2; ++t) {
+        const unsigned row = 16 * t + l16;
+        x.w[t] = *reinterpret_cast<const Words<NB>*>(page + (codes_at + (unsigned)w.slot[0] * ROW + (row * ROW + 4 * NB * g)));
+        x.e[t] = *reinterpret_cast<const E*>(page + (to_exps + (unsigned)w.slot[0] * EXP + row * EXP));
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const unsigned char* page = head_of_page(cp, w.number[t], h);
+        x.w[t] = Words<NB>{};
+        x.e[t] = 0;
+        if (page) {
+          x.w[t] = *reinterpret_cast<const Words<NB>*>(page + (codes_at + (unsigned)w.slot[t] * ROW + 4 * NB * g));
+          x.e[t] = *reinterpret_cast<const E*>(page + (to_exps + (unsigned)w.slot[t] * EXP));
+        }
       }
     }
   };
-  auto unit = [&](unsigned long e, int s) {          // the power of two of word NB g + s
+  auto keys_of = [&](const Place& w, int k0) {
+    if constexpr (EVEN) return (unsigned)w.number[0] >= (unsigned)cp.pages ? 0u : end - k0 >= 32 ? ~0u : (1u << (end - k0)) - 1;
+    else return ((unsigned)__ballot((unsigned)w.number[0] < (unsigned)cp.pages) & 0xffffu) | (unsigned)__ballot((unsigned)w.number[1] < (unsigned)cp.pages) << 16;
+  };
+  // what is no key: zeros (its exponents may be anything)
+  auto cut = [&](Half& x) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if (!((there >> (16 * t + l16)) & 1u)) {
+        x.w[t] = Words<NB>{};
+        x.e[t] = 0;
+      }
+  };
+  auto unit = [&](EW e, int s) {                     // the power of two of word NB g + s
     const int block = NB % 4 == 0 ? NB / 4 * g + s / 4 : NB == 2 ? g / 2 : (NB * g + s) / 4;
     if constexpr (NB == 1) return unit_of((unsigned)e);
-    const unsigned half = NB <= 4 ? (unsigned)e : block >= 4 ? (unsigned)(e >> 32) : (unsigned)e;
+    unsigned half = (unsigned)e;
+    if constexpr (NB > 4) half = block >= 4 ? (unsigned)(e >> 32) : half;
     return unit_of((half >> (8 * (block & 3))) & 255u);
   };
 
@@ -195,53 +236,60 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
 
   // Where some rows do not see some of the keys: a block of values that is not a number is zero to the products (its codes are), as nothing times it is not
   // nothing, and reaches the rows that see it here.
-  auto take_out = [&](Keys& x, int k0) {
+  auto take_out = [&](int k0) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       bool any = false;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) any = any || ((x.ve[t] >> (8 * b)) & 255u) == 255u;
+      for (int b = 0; b < NB; ++b) any = any || ((xv.e[t] >> (8 * b)) & 255u) == 255u;
       if (!__ballot(any)) continue;
+#pragma unroll 1
       for (int i = 0; i < 16; ++i) {
-        const unsigned lo = __builtin_amdgcn_readlane((int)x.ve[t], i), hi = __builtin_amdgcn_readlane((int)(x.ve[t] >> 32), i);
+        const unsigned lo = __builtin_amdgcn_readlane((int)xv.e[t], i), hi = __builtin_amdgcn_readlane((int)((unsigned long)xv.e[t] >> 32), i);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
           if ((((b < 4 ? lo : hi) >> (8 * (b & 3))) & 255u) == 255u && k0 + 16 * t + i <= see) o[2 * b] = o[2 * b + 1] = f32x4{NAN, NAN, NAN, NAN};
       }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        if (((x.ve[t] >> (8 * b)) & 255u) == 255u) x.ve[t] &= ~(255ul << (8 * b));
+        if (((xv.e[t] >> (8 * b)) & 255u) == 255u) xv.e[t] &= ~((EW)255 << (8 * b));
     }
   };
 
-  auto work = [&](Keys& x, int k0) {
+  auto work = [&](int k0) {                          // and asks for the wavefront's next keys as soon as there is room for them
+    const bool more = k0 + 128 < end;
     f32x4 s[2];
-    if (k0 + 31 > all_see) take_out(x, k0);
+    if constexpr (EVEN) {
+      if (there != ~0u) { cut(xk); cut(xv); }
+    }
+    if (k0 + 31 > all_see) take_out(k0);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < NB; ++w) {
-        const u32x4 k = widen<O>(x.k[t].w[w], unit(x.ke[t], w));
+        const u32x4 k = widen<O>(xk.w[t].w[w], unit(xk.e[t], w));
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) s[t] = Mma<O>::m16(k, q[w][i], s[t]);
       }
     }
+    if (more) ask(xk, false, next);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (the tile has been read)
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int r = 16 * t + l16;
 #pragma unroll
-      for (int w = 0; w < NB; ++w) tile[r * CH + ((NB * g + w) ^ tile_turn<CH>(r))] = widen<O>(x.v[t].w[w], unit(x.ve[t], w));
+      for (int w = 0; w < NB; ++w) tile[r * CH + ((NB * g + w) ^ tile_turn<CH>(r))] = widen<O>(xv.w[t].w[w], unit(xv.e[t], w));
     }
+    if (more) ask(xv, true, next);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (x.there != ~0u || k0 + 31 > all_see) {
+    if (there != ~0u || k0 + 31 > all_see) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int at = 16 * t + 4 * g + r;
-          if (!((x.there >> at) & 1u) || k0 + at > see) s[t][r] = -INFINITY;
+          if (!((there >> at) & 1u) || k0 + at > see) s[t][r] = -INFINITY;
         }
     }
     {
@@ -295,26 +343,17 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
     }
   };
 
-  {
-    int k0 = begin + 32 * wave;
-    Keys x, y;
-    int number[2], slot[2];
-    if (k0 < end) {
-      numbers(k0, number, slot);
-      ask(x, number, slot);
-      numbers(k0 + 128, number, slot);
-    }
-    while (k0 < end) {
-      ask(y, number, slot);
-      numbers(k0 + 256, number, slot);
-      work(x, k0);
-      k0 += 128;
-      if (k0 >= end) break;
-      ask(x, number, slot);
-      numbers(k0 + 256, number, slot);
-      work(y, k0);
-      k0 += 128;
-    }
+  int k0 = begin + 32 * wave;
+  if (k0 < end) {
+    if (!EVEN) next = find(k0);
+    ask(xk, false, next);
+    ask(xv, true, next);
+  }
+  while (k0 < end) {
+    there = keys_of(next, k0);
+    next = find(k0 + 128);
+    work(k0);
+    k0 += 128;
   }
 
   // ---- the wavefronts' sums are joined: 2 and 3 to 0 and 1, then 1 to 0.  A lane has channels 16 i + 4 g .. + 3 of its row
@@ -727,11 +766,13 @@ int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const CachePlan& p = l.plan;
   const int heads = l.a.pages.heads;
   const dim3 grid((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits));
-  if constexpr (kHasMany<T, NB>) {
-    if (p.few) hipLaunchKernelGGL((cache_few_kernel<T, NB>), grid, dim3(256), 0, s, l);
-    else hipLaunchKernelGGL((cache_many_kernel<T, NB>), grid, dim3(256), 0, s, l);
+  const bool even = l.a.pages.page_tokens % 32 == 0;
+  if (!p.few) {
+    if constexpr (kHasMany<T, NB>) hipLaunchKernelGGL((cache_many_kernel<T, NB>), grid, dim3(256), 0, s, l);
+  } else if (even) {
+    hipLaunchKernelGGL((cache_few_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
   } else {
-    hipLaunchKernelGGL((cache_few_kernel<T, NB>), grid, dim3(256), 0, s, l);
+    hipLaunchKernelGGL((cache_few_kernel<T, NB, false>), grid, dim3(256), 0, s, l);
   }
   WMDEC_HIP(hipGetLastError());
   if (p.splits > 1) {
