@@ -31,10 +31,12 @@ template <> __device__ __forceinline__ u32x4 widen<f16_t>(unsigned codes, float 
 }
 __device__ __forceinline__ float unit_of(unsigned exponent) { return __uint_as_float(exponent << 23); }   // (255 is infinite here and not a number to the conversions)
 
-// eight floats -> a word of codes: times 1 / unit, to the nearest value, ties to the even code, 6 for what is above
+// floats -> their codes, in order from the low bits: times 1 / unit, to the nearest value, ties to the even code, 6 for what is above
+__device__ __forceinline__ unsigned narrow(const float (&x)[4], float unit) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], unit, 0), x[2], x[3], unit, 1);
+}
 __device__ __forceinline__ unsigned narrow(const float (&x)[8], float unit) {
-  unsigned w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+  unsigned w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], unit, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);

@@ -14,19 +14,19 @@ template int cache_attention_launch<f16_t>(const CacheLaunch&, hipStream_t);
 
 namespace {
 
-constexpr int kSteps = 4;   // tokens of a lane, on their way together
+constexpr int kSteps = 2;   // tokens of a lane, on their way together
 
 struct TokenParams { CacheTokens a; int chunks; long units; };   // units: (sample, chunk of tokens, head), a wavefront each
 
-// tokens of a wavefront at a time
-__host__ __device__ constexpr int tokens_abreast(int nb) { return 16 / nb; }
+// A lane has 16 bytes of a state; lanes of a token, tokens of a wavefront at a time.
+template <typename T> constexpr int kLaneChannels = 16 / (int)sizeof(T);
+__host__ __device__ constexpr int lanes_of(int nb, int channels) { return 32 / channels * nb; }
+__host__ __device__ constexpr int tokens_abreast(int nb, int channels) { return 64 / lanes_of(nb, channels); }
 
-template <typename T> struct alignas(16) Eight { T v[8]; };
-
-// Calls f(step, row of the dense tensors, head's part of the page or null, slot) for the lane's tokens.
-template <int NB, typename F>
+// Calls f(sample, head, lane's place in the row, tokens, page numbers, places in the pages) for the lane's tokens.
+template <typename T, int NB, typename F>
 __device__ __forceinline__ void for_tokens(const TokenParams& p, F f) {
-  constexpr int LANES = 4 * NB, ABREAST = tokens_abreast(NB);
+  constexpr int LANES = lanes_of(NB, kLaneChannels<T>), ABREAST = tokens_abreast(NB, kLaneChannels<T>);
   const CachePages& c = p.a.pages;
   const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= p.units) return;
@@ -47,23 +47,34 @@ __device__ __forceinline__ void for_tokens(const TokenParams& p, F f) {
   f(n, h, lane % LANES, token, number, slot);
 }
 
-// 16-bit sources have no exponent above that of their type's largest value rounded down to it; f16 reads back what it wrote
+// f16 reads back what it wrote
 template <typename T> constexpr int kTopExponent = 125 + 127;
 template <> constexpr int kTopExponent<f16_t> = 13 + 127;
 
-template <typename T, int NB>
+// (by the caches or not at compile time: the compiler makes an ordinary access of two branches)
+template <bool STREAM> __device__ __forceinline__ u32x4 load_state(const void* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load((const u32x4*)p);
+  else return *(const u32x4*)p;
+}
+template <bool STREAM> __device__ __forceinline__ void store_state(void* p, u32x4 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, (u32x4*)p);
+  else *(u32x4*)p = v;
+}
+
+template <typename T, int NB, bool STREAM>
 __global__ __launch_bounds__(256) void cache_write_kernel(TokenParams p) {
-  for_tokens<NB>(p, [&](int n, int h, int c, const int (&token)[kSteps], const int (&number)[kSteps], const int (&slot)[kSteps]) {
+  for_tokens<T, NB>(p, [&](int n, int h, int c, const int (&token)[kSteps], const int (&number)[kSteps], const int (&slot)[kSteps]) {
+    constexpr int E = kLaneChannels<T>, PER = 32 / E, ROW = 16 * NB, EXP = exponent_bytes(NB);   // PER: lanes of a block
     const CachePages& cp = p.a.pages;
-    Eight<T> x[2][kSteps];
+    u32x4 x[2][kSteps];
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       const T* src = (const T*)(which ? p.a.v : p.a.k);
       const wmdec_strides& st = which ? p.a.vs : p.a.ks;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        x[which][i] = Eight<T>{};
-        if (src && number[i] >= 0 && 8 * c < cp.d) x[which][i] = *reinterpret_cast<const Eight<T>*>(src + n * st.sample + token[i] * st.token + h * st.head + 8 * c);
+        x[which][i] = u32x4{0, 0, 0, 0};
+        if (src && number[i] >= 0 && E * c < cp.d) x[which][i] = load_state<STREAM>(src + n * st.sample + token[i] * st.token + h * st.head + E * c);
       }
     }
 #pragma unroll
@@ -72,36 +83,38 @@ __global__ __launch_bounds__(256) void cache_write_kernel(TokenParams p) {
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
         if (!(which ? p.a.v : p.a.k)) continue;
-        float v[8];
+        float v[E];
         unsigned top = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] = to_float(x[which][i].v[e]);
+        for (int e = 0; e < E; ++e) {
+          if constexpr (E == 4) v[e] = __uint_as_float(x[which][i][e]);
+          else v[e] = e % 2 ? unpack_hi<T>(x[which][i][e / 2]) : unpack_lo<T>(x[which][i][e / 2]);
           top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
         }
-        top = max(top, (unsigned)__shfl_xor((int)top, 1));
-        top = max(top, (unsigned)__shfl_xor((int)top, 2));
+#pragma unroll
+        for (int step = 1; step < PER; step *= 2) top = max(top, (unsigned)__shfl_xor((int)top, step));
         // the exponent of the largest value as three bits of it round, which is one more from 1.75 on
         const int held = min(max((int)((top + 0x200000u) >> 23) - 2, 2), kTopExponent<T>);
         const bool finite = top < 0x7f800000u;
         const unsigned codes = finite ? narrow(v, unit_of(held)) : 0;
         if (page) {
-          constexpr int ROW = 16 * NB, EXP = exponent_bytes(NB);
-          unsigned char* at = page + which * ROW * cp.page_tokens;
-          *reinterpret_cast<unsigned*>(at + (unsigned)slot[i] * ROW + 4 * c) = codes;
-          if (c % 4 == 0) page[(2 * ROW + which * EXP) * cp.page_tokens + slot[i] * EXP + c / 4] = (unsigned char)(finite ? held : 255);
+          unsigned char* at = page + which * ROW * cp.page_tokens + (unsigned)slot[i] * ROW + E / 2 * c;
+          if constexpr (E == 4) *reinterpret_cast<unsigned short*>(at) = (unsigned short)codes;
+          else *reinterpret_cast<unsigned*>(at) = codes;
+          if (c % PER == 0) page[(2 * ROW + which * EXP) * cp.page_tokens + slot[i] * EXP + c / PER] = (unsigned char)(finite ? held : 255);
         }
       }
     }
   });
 }
 
-template <typename T, int NB>
+template <typename T, int NB, bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(TokenParams p) {
-  for_tokens<NB>(p, [&](int n, int h, int c, const int (&token)[kSteps], const int (&number)[kSteps], const int (&slot)[kSteps]) {
+  for_tokens<T, NB>(p, [&](int n, int h, int c, const int (&token)[kSteps], const int (&number)[kSteps], const int (&slot)[kSteps]) {
+    constexpr int E = kLaneChannels<T>, PER = 32 / E, ROW = 16 * NB, EXP = exponent_bytes(NB);
+    typedef typename std::conditional<E == 4, unsigned short, unsigned>::type Codes;
     const CachePages& cp = p.a.pages;
-    if (8 * c >= cp.d) return;
-    constexpr int ROW = 16 * NB, EXP = exponent_bytes(NB);
+    if (E * c >= cp.d) return;
     unsigned codes[2][kSteps], held[2][kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
@@ -110,8 +123,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(TokenParams p) {
       for (int which = 0; which < 2; ++which) {
         codes[which][i] = held[which][i] = 0;   // no page: zeros
         if (page && (which ? p.a.v : p.a.k)) {
-          codes[which][i] = *reinterpret_cast<const unsigned*>(page + which * ROW * cp.page_tokens + (unsigned)slot[i] * ROW + 4 * c);
-          held[which][i] = page[(2 * ROW + which * EXP) * cp.page_tokens + slot[i] * EXP + c / 4];
+          codes[which][i] = *reinterpret_cast<const Codes*>(page + which * ROW * cp.page_tokens + (unsigned)slot[i] * ROW + E / 2 * c);
+          held[which][i] = page[(2 * ROW + which * EXP) * cp.page_tokens + slot[i] * EXP + c / PER];
         }
       }
     }
@@ -123,44 +136,48 @@ __global__ __launch_bounds__(256) void cache_read_kernel(TokenParams p) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         if (token[i] < 0) continue;
-        T* to = dst + n * st.sample + token[i] * st.token + h * st.head + 8 * c;
         const float unit = unit_of(held[which][i]);
-        if constexpr (sizeof(T) == 4) {
-          const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 1),
-                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 3)};
-          *reinterpret_cast<f32x4*>(to) = f32x4{v[0].x, v[0].y, v[1].x, v[1].y};
-          *reinterpret_cast<f32x4*>(to + 4) = f32x4{v[2].x, v[2].y, v[3].x, v[3].y};
+        u32x4 v;
+        if constexpr (E == 4) {
+          const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[which][i], unit, 1);
+          v = __builtin_bit_cast(u32x4, f32x4{lo.x, lo.y, hi.x, hi.y});
         } else {
-          *reinterpret_cast<u32x4*>(to) = widen<T>(codes[which][i], unit);
+          v = widen<T>(codes[which][i], unit);
         }
+        store_state<STREAM>(dst + n * st.sample + token[i] * st.token + h * st.head + E * c, v);
       }
     }
   });
 }
 
 int blocks_of(int d) { return (d + 31) / 32; }
-int chunks_of(int t, int d) { const int per = kSteps * tokens_abreast(blocks_of(d)); return (int)(((long)t + per - 1) / per); }
+int chunks_of(int t, int d, int channels) { const int per = kSteps * tokens_abreast(blocks_of(d), channels); return (int)(((long)t + per - 1) / per); }
+
+// States that are whole 64-byte pieces of memory pass by the caches.
+bool pieces(const void* p, const wmdec_strides& s, int d, size_t es) {
+  return !p || ((uintptr_t)p % 64 == 0 && d * es % 64 == 0 && s.sample * es % 64 == 0 && s.token * es % 64 == 0 && s.head * es % 64 == 0);
+}
 
 template <typename T, bool WRITE, int NB>
-int launch_tokens(const TokenParams& p, hipStream_t s) {
+int launch_tokens(const TokenParams& p, bool stream, hipStream_t s) {
   const dim3 grid((unsigned)((p.units + 3) / 4));
-  if constexpr (WRITE) hipLaunchKernelGGL((cache_write_kernel<T, NB>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((cache_read_kernel<T, NB>), grid, dim3(256), 0, s, p);
+  auto kern = WRITE ? (stream ? cache_write_kernel<T, NB, true> : cache_write_kernel<T, NB, false>) : (stream ? cache_read_kernel<T, NB, true> : cache_read_kernel<T, NB, false>);
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, p);
   WMDEC_HIP(hipGetLastError());
   return WMDEC_OK;
 }
 
 template <typename T, bool WRITE>
-int launch_width(const TokenParams& p, hipStream_t s) {
+int launch_width(const TokenParams& p, bool stream, hipStream_t s) {
   switch (blocks_of(p.a.pages.d)) {
-    case 1: return launch_tokens<T, WRITE, 1>(p, s);
-    case 2: return launch_tokens<T, WRITE, 2>(p, s);
-    case 3: return launch_tokens<T, WRITE, 3>(p, s);
-    case 4: return launch_tokens<T, WRITE, 4>(p, s);
-    case 5: return launch_tokens<T, WRITE, 5>(p, s);
-    case 6: return launch_tokens<T, WRITE, 6>(p, s);
-    case 7: return launch_tokens<T, WRITE, 7>(p, s);
-    default: return launch_tokens<T, WRITE, 8>(p, s);
+    case 1: return launch_tokens<T, WRITE, 1>(p, stream, s);
+    case 2: return launch_tokens<T, WRITE, 2>(p, stream, s);
+    case 3: return launch_tokens<T, WRITE, 3>(p, stream, s);
+    case 4: return launch_tokens<T, WRITE, 4>(p, stream, s);
+    case 5: return launch_tokens<T, WRITE, 5>(p, stream, s);
+    case 6: return launch_tokens<T, WRITE, 6>(p, stream, s);
+    case 7: return launch_tokens<T, WRITE, 7>(p, stream, s);
+    default: return launch_tokens<T, WRITE, 8>(p, stream, s);
   }
 }
 
@@ -168,10 +185,12 @@ template <bool WRITE>
 int launch_type(const CacheTokens& a, int dtype, hipStream_t s) {
   TokenParams p;
   p.a = a;
-  p.chunks = chunks_of(a.t, a.pages.d);
+  const size_t es = dtype_size(dtype);
+  p.chunks = chunks_of(a.t, a.pages.d, 16 / (int)es);
+  const bool stream = pieces(a.k, a.ks, a.pages.d, es) && pieces(a.v, a.vs, a.pages.d, es) && (!WRITE || a.pages.d * es >= 128);
   p.units = (long)a.n * p.chunks * a.pages.heads;
-  if (dtype == WMDEC_F32) return launch_width<float, WRITE>(p, s);
-  return dtype == WMDEC_BF16 ? launch_width<bf16_t, WRITE>(p, s) : launch_width<f16_t, WRITE>(p, s);
+  if (dtype == WMDEC_F32) return launch_width<float, WRITE>(p, stream, s);
+  return dtype == WMDEC_BF16 ? launch_width<bf16_t, WRITE>(p, stream, s) : launch_width<f16_t, WRITE>(p, stream, s);
 }
 
 }  // namespace
@@ -181,7 +200,7 @@ size_t cache_head_bytes(int page_tokens, int d) {
   return ((size_t)page_tokens * 2 * (16 * nb + exponent_bytes(nb)) + 15) / 16 * 16;
 }
 
-bool cache_tokens_fit(int n, int t, int heads, int d) { return (double)n * chunks_of(t, d) * heads < 0x1p26; }   // (64 threads each)
+bool cache_tokens_fit(int n, int t, int heads, int d) { return (double)n * chunks_of(t, d, 4) * heads < 0x1p26; }   // (64 threads each)
 
 int launch_cache_write(const CacheTokens& a, int dtype, hipStream_t s) { return launch_type<true>(a, dtype, s); }
 int launch_cache_read(const CacheTokens& a, int dtype, hipStream_t s) { return launch_type<false>(a, dtype, s); }
