@@ -400,25 +400,28 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
 // before; the codes of the tile after that are on their way meanwhile.  Per 32 keys a wavefront forms S^T = K Q^T of 32x32x16 products (keys along the accumulator's
 // registers, one row a lane), the softmax, and O^T += V^T P^T with the probabilities as they are in their registers: an accumulator's keys of lane half lk
 // are 8 (r / 4) + 4 lk + r % 4, so V^T is read from LDS in that order of keys, transposed on the way.
-template <typename T, int NB> constexpr bool kHasMany = sizeof(T) == 2 || NB < 8;   // (the queries of 256 channels in three pieces and the outputs leave no registers)
+template <typename T, int NB> constexpr bool kHasMany = sizeof(T) == 2 || NB < 7;   // (the queries of more channels in three pieces and the outputs leave no registers)
 
 template <typename T, int NB>
 struct ManyForm {
-  static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = sizeof(T) == 4 ? (NB <= 3 ? 2 : 1) : NB <= 1 ? 4 : NB == 2 ? 3 : NB <= 5 ? 2 : 1;   // (TILE: chunks of a tile)
-  static constexpr int ITEMS = (2 * KT * NB + 255) / 256;   // blocks of 32 channels that a thread widens
+  static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = sizeof(T) == 4 ? (NB <= 3 ? 2 : 1) : NB <= 1 ? 4 : NB == 2 ? 3 : 2;   // (TILE: chunks of a tile)
+  static constexpr bool PAIR = NB >= 3;              // a thread widens a block of 32 channels of a key and of its value, else of one of them
 };
 
 // every LDS access of this wavefront is done, and so for the others: codes on their way are not waited for
 __device__ __forceinline__ void sync_tiles_of_cache() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
-template <typename T, int NB>
+// SMALL: for pages of any size; else they hold a tile or more.
+template <typename T, int NB, bool SMALL>
 __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kernel(CacheLaunch launch) {
   typedef typename CacheOperand<T>::type O;
   typedef ManyForm<T, NB> F;
-  constexpr int PIECES = CacheOperand<T>::pieces, CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ITEMS = F::ITEMS, ROW = 16 * NB, EXP = exponent_bytes(NB);
+  constexpr int PIECES = CacheOperand<T>::pieces, CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ROW = 16 * NB, EXP = exponent_bytes(NB);
   constexpr int GP = CH % 8 == 0 ? 8 : 4;            // chunks that are exchanged among each other
   __shared__ __align__(16) u32x4 s_k[2 * TILE], s_v[2 * TILE];
-  __shared__ unsigned s_bad[3][2 * NB + 2];          // by tile: values that are not a number, bits of the keys of every block, and whether there are any
+  // what is out of the ordinary in a tile: bits of the keys whose values are not a number, by block; whether there are any (1), or keys without a page (2); those
+  constexpr int FLAGS = 2 * NB, GONE = FLAGS + 1, BAD = FLAGS + 3;
+  __shared__ unsigned s_bad[3][BAD];
   const CacheAttentionArgs& a = launch.a;
   const CachePages& cp = a.pages;
   const CachePlan& p = launch.plan;
@@ -469,72 +472,86 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   const int see = a.causal ? behind + row / a.group : view.len - 1, all_see = a.causal ? behind + first_row / a.group : view.len - 1;
   const int last_see = a.causal ? behind + min(first_row + 31, view.rows - 1) / a.group : view.len - 1;
 
-  // ---- tiles.  A thread widens blocks i 256 + tid of a tile: keys' blocks first, then values'
+  // ---- tiles.  A thread widens a block of 32 channels of a key, of a value, or of both.  Its place goes from tile to tile: page numbers are asked for a tile before
+  // they are needed, and with large pages only where the last one ends.
+  constexpr int ITEMS = F::PAIR ? 2 : 1;
+  constexpr unsigned kGone = 256;                    // instead of an exponent: there is no page
+  const int mine = F::PAIR || tid < KT * NB ? tid : tid - KT * NB, key = mine / NB, block = mine - key * NB;
+  const bool live = mine < KT * NB, of_values = !F::PAIR && tid >= KT * NB;
   const int* table = cp.table + n * cp.table_stride;
-  struct Item { int number, slot; };
-  Item where[ITEMS];
+  const unsigned char* page = nullptr;
+  int slot = 0, page_index = 0, next_number = -1, next_slot = 0;
   u32x4 codes[ITEMS];
   unsigned held[ITEMS];
-  auto item_of = [&](int i, bool& values, int& key, int& block) {
-    const int it = i * 256 + tid, rest = it < KT * NB ? it : it - KT * NB;
-    values = it >= KT * NB;
-    key = rest / NB;
-    block = rest - key * NB;
-    return it < 2 * KT * NB;
+  auto number_at = [&](int index) { return index < cp.table_pages ? table[index] : -1; };
+  auto first_place = [&]() {
+    page_index = div_rem((unsigned)(begin + key), cp.page_tokens, cp.inv_page_tokens, slot);
+    page = head_of_page(cp, number_at(page_index), h);
+    if constexpr (SMALL) next_number = number_at(div_rem((unsigned)(begin + KT + key), cp.page_tokens, cp.inv_page_tokens, next_slot));
+    else next_number = number_at(page_index + 1);
   };
-  auto look_up = [&](int j) {
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      bool values;
-      int key, block;
-      const bool live = item_of(i, values, key, block);
-      const int at = begin + j * KT + key, page = div_rem((unsigned)at, cp.page_tokens, cp.inv_page_tokens, where[i].slot);
-      where[i].number = -1;
-      if (live && at < end) where[i].number = table[page];
+  auto next_place = [&](int j) {                     // from tile j - 1 to tile j
+    if constexpr (SMALL) {
+      page = head_of_page(cp, next_number, h);
+      slot = next_slot;
+      next_number = number_at(div_rem((unsigned)(begin + (j + 1) * KT + key), cp.page_tokens, cp.inv_page_tokens, next_slot));
+    } else {
+      slot += KT;
+      if (slot >= (int)cp.page_tokens) {
+        slot -= (int)cp.page_tokens;
+        ++page_index;
+        page = head_of_page(cp, next_number, h);
+        next_number = number_at(page_index + 1);
+      }
     }
   };
+  const unsigned values_at = ROW * cp.page_tokens, exps_at = 2 * values_at, value_exps_at = EXP * cp.page_tokens;
   auto ask = [&]() {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      bool values;
-      int key, block;
-      item_of(i, values, key, block);
-      const unsigned char* page = head_of_page(cp, where[i].number, h);
       codes[i] = u32x4{0, 0, 0, 0};
-      held[i] = 0;
-      if (page) {
-        codes[i] = *reinterpret_cast<const u32x4*>(page + (unsigned)where[i].slot * ROW + 16 * block + (values ? ROW * cp.page_tokens : 0u));
-        held[i] = page[2 * ROW * cp.page_tokens + (unsigned)where[i].slot * EXP + block + (values ? EXP * cp.page_tokens : 0u)];
+      held[i] = kGone;
+    }
+    if (live && page) {
+      const unsigned char *c = page + (16 * block + (unsigned)slot * ROW), *e = page + (exps_at + block + (unsigned)slot * EXP);
+      if constexpr (F::PAIR) {
+        codes[0] = *reinterpret_cast<const u32x4*>(c);
+        codes[ITEMS - 1] = *reinterpret_cast<const u32x4*>(c + values_at);
+        held[0] = *e;
+        held[ITEMS - 1] = e[value_exps_at];
+      } else {
+        codes[0] = *reinterpret_cast<const u32x4*>(c + (of_values ? values_at : 0u));
+        held[0] = e[of_values ? value_exps_at : 0u];
       }
     }
   };
   auto fill = [&](int j) {
+    const int left = end - begin - j * KT;           // keys of the tile
+    if (!live) return;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      bool values;
-      int key, block;
-      if (!item_of(i, values, key, block)) continue;
-      u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + key * CH;
-      const bool bad = a.causal && values && held[i] == 255u;   // (as take_out does for few rows)
-      if (bad) {
-        atomicOr(&s_bad[j % 3][2 * block + (key >> 5)], 1u << (key & 31));
-        atomicOr(&s_bad[j % 3][2 * NB], 1u);
+      const bool values = F::PAIR ? i == 1 : of_values;
+      if (left < KT && key >= left) {                // (a page has room for keys that are not there; their exponents may be anything)
+        codes[i] = u32x4{0, 0, 0, 0};
+        held[i] = 0;
       }
-      const float unit = unit_of(bad ? 0u : held[i]);
+      if (held[i] >= 255u) {
+        const bool gone = held[i] == kGone, bad = !gone && a.causal && values;   // (as take_out does for few rows)
+        if (gone ? !values && block == 0 : bad) {
+          atomicOr(&s_bad[j % 3][(gone ? GONE : 2 * block) + (key >> 5)], 1u << (key & 31));
+          atomicOr(&s_bad[j % 3][FLAGS], gone ? 2u : 1u);
+        }
+        if (gone || bad) held[i] = 0;
+      }
+      int at = key;
+      if constexpr (NB >= 7) asm volatile("" : "+v"(at));   // (worked out again for every tile: outputs and queries leave no registers to keep it)
+      u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + at * CH;
+      const float unit = unit_of(held[i]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(key)] = widen<O>(codes[i][c], unit);
+      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(at)] = widen<O>(codes[i][c], unit);
     }
   };
-  // valid keys of a tile, by the wavefront for itself
-  unsigned long there = 0;
-  int next_number = -1;
-  auto look_there = [&](int j) {
-    const int at = begin + j * KT + (KT == 64 ? lane : l32);
-    int slot;
-    const int page = div_rem((unsigned)at, cp.page_tokens, cp.inv_page_tokens, slot);
-    next_number = -1;
-    if (at < end) next_number = table[page];
-  };
+  unsigned long there = 0;                           // which of a tile's keys are there
 
   // ---- where a lane reads its operands (chunks, and bytes, of a tile)
   int kb[GP / 2];
@@ -650,37 +667,39 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
     }
   };
 
-  if (tid < 3 * (2 * NB + 2)) s_bad[0][tid] = 0;
+  if (tid < 3 * BAD) s_bad[0][tid] = 0;
   if (tiles > 0) {
-    look_up(0);
+    first_place();
     ask();
-    look_up(1);
-    look_there(0);
     sync_tiles_of_cache();                           // (s_bad is clear)
     fill(0);
+    next_place(1);
     ask();
-    look_up(2);
   }
   for (int j = 0; j < tiles; ++j) {
     sync_tiles_of_cache();                           // the tile is there, and every wavefront is done with the other buffer
-    there = __ballot((unsigned)next_number < (unsigned)cp.pages);
     if (j + 1 < tiles) {
       fill(j + 1);
+      next_place(j + 2);
       ask();
-      look_up(j + 3);
-      look_there(j + 1);
     }
-    if (a.causal && tid < 2 * NB + 2) s_bad[(j + 2) % 3][tid] = 0;
-    const int k0 = begin + j * KT;
+    if (tid < BAD) s_bad[(j + 2) % 3][tid] = 0;
+    const int k0 = begin + j * KT, left = end - k0;
     if (idle || k0 > last_see) continue;
-    if (a.causal && __builtin_amdgcn_readfirstlane((int)s_bad[j % 3][2 * NB])) {
+    there = left >= 64 ? ~0ul : (1ul << left) - 1;
+    const unsigned* bad = s_bad[j % 3];
+    const unsigned flags = __builtin_amdgcn_readfirstlane((int)bad[FLAGS]);
+    if (flags & 2u) there &= ~((unsigned)__builtin_amdgcn_readfirstlane((int)bad[GONE]) | (unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)bad[GONE + 1]) << 32);
+    if (flags & 1u) {
 #pragma unroll
       for (int dt = 0; dt < NB; ++dt)
+#pragma unroll 1
         for (int i = 0; i < KT; ++i)
-          if (((s_bad[j % 3][2 * dt + (i >> 5)] >> (i & 31)) & 1u) && k0 + i <= see)
+          if (((bad[2 * dt + (i >> 5)] >> (i & 31)) & 1u) && k0 + i <= see)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[dt][r] = NAN;
     }
+    __builtin_amdgcn_sched_barrier(0);
     scores(s_k + (j & 1) * TILE, k0);
     softmax();
     values(reinterpret_cast<const unsigned char*>(s_v + (j & 1) * TILE));
@@ -768,7 +787,11 @@ int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const dim3 grid((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits));
   const bool even = l.a.pages.page_tokens % 32 == 0;
   if (!p.few) {
-    if constexpr (kHasMany<T, NB>) hipLaunchKernelGGL((cache_many_kernel<T, NB>), grid, dim3(256), 0, s, l);
+    if constexpr (kHasMany<T, NB>) {
+      constexpr bool ANY = NB == 8;                  // (two registers short of the other)
+      if (ANY || l.a.pages.page_tokens < ManyForm<T, NB>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
+      else hipLaunchKernelGGL((cache_many_kernel<T, NB, ANY>), grid, dim3(256), 0, s, l);
+    }
   } else if (even) {
     hipLaunchKernelGGL((cache_few_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
   } else {

@@ -215,7 +215,7 @@ CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   p.rows = tq * group;
   // us, few / many rows a workgroup: bf16, causal, 32 / 8 heads of 128, 64 rows a key head against 2048 keys 11.2 / 16.0, 16384 21.4 / 31.1, 16 x 4096 80 / 72; 128 rows against
   // 2048 13.3 / 18.1, 16 x 4096 137 / 90; 100 of 30 heads of 64 against 2000 15.0 / 18.7, 16 x 1000 62 / 31.
-  p.few = p.rows <= 64 || (dtype == WMDEC_F32 && !kHasMany<float, 8> && p.nb == 8);
+  p.few = p.rows <= 64 || (dtype == WMDEC_F32 && !kHasMany<float, 7> && p.nb >= 7);
   p.row_blocks = (p.rows + p.bq() - 1) / p.bq();
   const long blocks = (long)heads * p.row_blocks;
   long ranges;
