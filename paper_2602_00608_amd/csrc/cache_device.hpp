@@ -405,6 +405,7 @@ template <typename T, int NB> constexpr bool kHasMany = sizeof(T) == 2 || NB < 7
 template <typename T, int NB>
 struct ManyForm {
   static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = sizeof(T) == 4 ? (NB <= 3 ? 2 : 1) : NB <= 1 ? 4 : NB == 2 ? 3 : 2;   // (TILE: chunks of a tile)
+  static constexpr bool TIGHT = NB >= 7;   // queries and outputs leave few registers
   static constexpr bool PAIR = NB >= 3;              // a thread widens a block of 32 channels of a key and of its value, else of one of them
 };
 
@@ -418,6 +419,7 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   typedef ManyForm<T, NB> F;
   constexpr int PIECES = CacheOperand<T>::pieces, CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ROW = 16 * NB, EXP = exponent_bytes(NB);
   constexpr int GP = CH % 8 == 0 ? 8 : 4;            // chunks that are exchanged among each other
+  constexpr bool TIGHT = F::TIGHT;
   __shared__ __align__(16) u32x4 s_k[2 * TILE], s_v[2 * TILE];
   // what is out of the ordinary in a tile: bits of the keys whose values are not a number, by block; whether there are any (1), or keys without a page (2); those
   constexpr int FLAGS = 2 * NB, GONE = FLAGS + 1, BAD = FLAGS + 3;
@@ -476,8 +478,14 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   // they are needed, and with large pages only where the last one ends.
   constexpr int ITEMS = F::PAIR ? 2 : 1;
   constexpr unsigned kGone = 256;                    // instead of an exponent: there is no page
-  const int mine = F::PAIR || tid < KT * NB ? tid : tid - KT * NB, key = mine / NB, block = mine - key * NB;
-  const bool live = mine < KT * NB, of_values = !F::PAIR && tid >= KT * NB;
+  struct Mine { int key, block; bool live, values; };
+  auto mine_of = [&]() {
+    int t = tid;
+    if constexpr (TIGHT) asm volatile("" : "+v"(t));   // (worked out again wherever it is needed: there are no registers to keep it)
+    const bool second = !F::PAIR && t >= KT * NB;
+    if (second) t -= KT * NB;
+    return Mine{t / NB, t % NB, t < KT * NB, second};
+  };
   const int* table = cp.table + n * cp.table_stride;
   const unsigned char* page = nullptr;
   int slot = 0, page_index = 0, next_number = -1, next_slot = 0;
@@ -485,6 +493,7 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   unsigned held[ITEMS];
   auto number_at = [&](int index) { return index < cp.table_pages ? table[index] : -1; };
   auto first_place = [&]() {
+    const int key = mine_of().key;
     page_index = div_rem((unsigned)(begin + key), cp.page_tokens, cp.inv_page_tokens, slot);
     page = head_of_page(cp, number_at(page_index), h);
     if constexpr (SMALL) next_number = number_at(div_rem((unsigned)(begin + KT + key), cp.page_tokens, cp.inv_page_tokens, next_slot));
@@ -492,6 +501,7 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   };
   auto next_place = [&](int j) {                     // from tile j - 1 to tile j
     if constexpr (SMALL) {
+      const int key = mine_of().key;
       page = head_of_page(cp, next_number, h);
       slot = next_slot;
       next_number = number_at(div_rem((unsigned)(begin + (j + 1) * KT + key), cp.page_tokens, cp.inv_page_tokens, next_slot));
@@ -512,25 +522,28 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
       codes[i] = u32x4{0, 0, 0, 0};
       held[i] = kGone;
     }
-    if (live && page) {
-      const unsigned char *c = page + (16 * block + (unsigned)slot * ROW), *e = page + (exps_at + block + (unsigned)slot * EXP);
+    const Mine x = mine_of();
+    if (x.live && page) {
+      const unsigned char *c = page + (16 * x.block + (unsigned)slot * ROW), *e = page + (exps_at + x.block + (unsigned)slot * EXP);
       if constexpr (F::PAIR) {
         codes[0] = *reinterpret_cast<const u32x4*>(c);
         codes[ITEMS - 1] = *reinterpret_cast<const u32x4*>(c + values_at);
         held[0] = *e;
         held[ITEMS - 1] = e[value_exps_at];
       } else {
-        codes[0] = *reinterpret_cast<const u32x4*>(c + (of_values ? values_at : 0u));
-        held[0] = e[of_values ? value_exps_at : 0u];
+        codes[0] = *reinterpret_cast<const u32x4*>(c + (x.values ? values_at : 0u));
+        held[0] = e[x.values ? value_exps_at : 0u];
       }
     }
   };
   auto fill = [&](int j) {
     const int left = end - begin - j * KT;           // keys of the tile
-    if (!live) return;
+    const Mine x = mine_of();
+    const int key = x.key, block = x.block;
+    if (!x.live) return;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const bool values = F::PAIR ? i == 1 : of_values;
+      const bool values = F::PAIR ? i == 1 : x.values;
       if (left < KT && key >= left) {                // (a page has room for keys that are not there; their exponents may be anything)
         codes[i] = u32x4{0, 0, 0, 0};
         held[i] = 0;
@@ -543,12 +556,10 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
         }
         if (gone || bad) held[i] = 0;
       }
-      int at = key;
-      if constexpr (NB >= 7) asm volatile("" : "+v"(at));   // (worked out again for every tile: outputs and queries leave no registers to keep it)
-      u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + at * CH;
+      u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + key * CH;
       const float unit = unit_of(held[i]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(at)] = widen<O>(codes[i][c], unit);
+      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(key)] = widen<O>(codes[i][c], unit);
     }
   };
   unsigned long there = 0;                           // which of a tile's keys are there
@@ -573,13 +584,18 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   const float c = a.scale * 1.4426950408889634f;
 
   auto scores = [&](const u32x4* tk, int k0) {
+    int k_at[GP / 2];
+    k_at[0] = kb[0];
+    if constexpr (TIGHT) asm volatile("" : "+v"(k_at[0]));
+#pragma unroll
+    for (int i = 1; i < GP / 2; ++i) k_at[i] = GP == 8 ? k_at[0] ^ 2 * i : kb[i];   // (eight chunks are exchanged by their three bits)
 #pragma unroll
     for (int ns = 0; ns < NS; ++ns) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[ns][r] = 0.f;
 #pragma unroll
       for (int st = 0; st < QS; ++st) {
-        const u32x4 kf = tk[kb[st % (GP / 2)] + st / (GP / 2) * GP + ns * 32 * CH];
+        const u32x4 kf = tk[k_at[st % (GP / 2)] + st / (GP / 2) * GP + ns * 32 * CH];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) s[ns] = Mma<O>::m32(kf, q[st][i], s[ns]);
       }
@@ -647,6 +663,11 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   auto values = [&](const unsigned char* tv) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* tptr_t;
+    int v_at[GP / 4];
+    v_at[0] = vb[0];
+    if constexpr (TIGHT) asm volatile("" : "+v"(v_at[0]));
+#pragma unroll
+    for (int i = 1; i < GP / 4; ++i) v_at[i] = GP == 8 ? v_at[0] ^ 64 * i : vb[i];
 #pragma unroll
     for (int i = 0; i < 2 * NS; ++i) {               // 16 keys
       unsigned w[4][PIECES];
@@ -658,7 +679,7 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
       }
 #pragma unroll
       for (int dt = 0; dt < NB; ++dt) {
-        const unsigned char* at = tv + vb[dt % (GP / 4)] + dt / (GP / 4) * GP * 16 + i * 16 * CH * 16;
+        const unsigned char* at = tv + v_at[dt % (GP / 4)] + dt / (GP / 4) * GP * 16 + i * 16 * CH * 16;
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 8 * CH * 16)));
 #pragma unroll
@@ -788,9 +809,8 @@ int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const bool even = l.a.pages.page_tokens % 32 == 0;
   if (!p.few) {
     if constexpr (kHasMany<T, NB>) {
-      constexpr bool ANY = NB == 8;                  // (two registers short of the other)
-      if (ANY || l.a.pages.page_tokens < ManyForm<T, NB>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
-      else hipLaunchKernelGGL((cache_many_kernel<T, NB, ANY>), grid, dim3(256), 0, s, l);
+      if (l.a.pages.page_tokens < ManyForm<T, NB>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
+      else hipLaunchKernelGGL((cache_many_kernel<T, NB, false>), grid, dim3(256), 0, s, l);
     }
   } else if (even) {
     hipLaunchKernelGGL((cache_few_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
