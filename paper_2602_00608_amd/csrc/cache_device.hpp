@@ -400,11 +400,9 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
 // before; the codes of the tile after that are on their way meanwhile.  Per 32 keys a wavefront forms S^T = K Q^T of 32x32x16 products (keys along the accumulator's
 // registers, one row a lane), the softmax, and O^T += V^T P^T with the probabilities as they are in their registers: an accumulator's keys of lane half lk
 // are 8 (r / 4) + 4 lk + r % 4, so V^T is read from LDS in that order of keys, transposed on the way.
-template <typename T, int NB> constexpr bool kHasMany = sizeof(T) == 2 || NB < 7;   // (the queries of more channels in three pieces and the outputs leave no registers)
-
-template <typename T, int NB>
+template <int NB>
 struct ManyForm {
-  static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = sizeof(T) == 4 ? (NB <= 3 ? 2 : 1) : NB <= 1 ? 4 : NB == 2 ? 3 : 2;   // (TILE: chunks of a tile)
+  static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = NB <= 1 ? 4 : NB == 2 ? 3 : 2;   // (TILE: chunks of a tile)
   static constexpr bool TIGHT = NB >= 7;   // queries and outputs leave few registers
   static constexpr bool PAIR = NB >= 3;              // a thread widens a block of 32 channels of a key and of its value, else of one of them
 };
@@ -414,10 +412,9 @@ __device__ __forceinline__ void sync_tiles_of_cache() { asm volatile("s_waitcnt 
 
 // SMALL: for pages of any size; else they hold a tile or more.
 template <typename T, int NB, bool SMALL>
-__global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kernel(CacheLaunch launch) {
-  typedef typename CacheOperand<T>::type O;
-  typedef ManyForm<T, NB> F;
-  constexpr int PIECES = CacheOperand<T>::pieces, CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ROW = 16 * NB, EXP = exponent_bytes(NB);
+__global__ __launch_bounds__(256, (ManyForm<NB>::WAVES)) void cache_many_kernel(CacheLaunch launch) {
+  typedef ManyForm<NB> F;
+  constexpr int CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ROW = 16 * NB, EXP = exponent_bytes(NB);
   constexpr int GP = CH % 8 == 0 ? 8 : 4;            // chunks that are exchanged among each other
   constexpr bool TIGHT = F::TIGHT;
   __shared__ __align__(16) u32x4 s_k[2 * TILE], s_v[2 * TILE];
@@ -447,26 +444,15 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
   // ---- queries: chunk 2 s + lk of the lane's row
   const int row = row0 + wave * 32 + l32, first_row = row0 + wave * 32;
   const bool idle = first_row >= view.rows;          // a wavefront past the last row only widens
-  u32x4 q[QS][PIECES];
+  u32x4 q[QS];
   {
     const int r = min(row, view.rows - 1), tok = r / a.group, hq = h * a.group + (r - tok * a.group);
     const T* src = (const T*)a.q + n * a.qs.sample + tok * a.qs.token + hq * a.qs.head;
 #pragma unroll
     for (int s = 0; s < QS; ++s) {
       const int at = 8 * (2 * s + lk);
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) q[s][i] = u32x4{0, 0, 0, 0};
-      if (at < cp.d) {
-        if constexpr (sizeof(T) == 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(src + at), y = *reinterpret_cast<const f32x4*>(src + at + 4);
-          unsigned w[4][3];
-          split3(x[0], x[1], w[0]); split3(x[2], x[3], w[1]); split3(y[0], y[1], w[2]); split3(y[2], y[3], w[3]);
-#pragma unroll
-          for (int i = 0; i < 3; ++i) q[s][i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
-        } else {
-          q[s][0] = *reinterpret_cast<const u32x4*>(src + at);
-        }
-      }
+      q[s] = u32x4{0, 0, 0, 0};
+      if (at < cp.d) q[s] = *reinterpret_cast<const u32x4*>(src + at);
     }
   }
   // keys up to which the lane's row, all rows of the wavefront, and its last row see
@@ -559,7 +545,7 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
       u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + key * CH;
       const float unit = unit_of(held[i]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(key)] = widen<O>(codes[i][c], unit);
+      for (int c = 0; c < 4; ++c) to[(4 * block + c) ^ tile_turn<CH>(key)] = widen<T>(codes[i][c], unit);
     }
   };
   unsigned long there = 0;                           // which of a tile's keys are there
@@ -595,9 +581,7 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
       for (int r = 0; r < 16; ++r) s[ns][r] = 0.f;
 #pragma unroll
       for (int st = 0; st < QS; ++st) {
-        const u32x4 kf = tk[k_at[st % (GP / 2)] + st / (GP / 2) * GP + ns * 32 * CH];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) s[ns] = Mma<O>::m32(kf, q[st][i], s[ns]);
+        s[ns] = Mma<T>::m32(tk[k_at[st % (GP / 2)] + st / (GP / 2) * GP + ns * 32 * CH], q[st], s[ns]);
       }
     }
 #pragma unroll
@@ -670,20 +654,15 @@ __global__ __launch_bounds__(256, (ManyForm<T, NB>::WAVES)) void cache_many_kern
     for (int i = 1; i < GP / 4; ++i) v_at[i] = GP == 8 ? v_at[0] ^ 64 * i : vb[i];
 #pragma unroll
     for (int i = 0; i < 2 * NS; ++i) {               // 16 keys
-      unsigned w[4][PIECES];
+      u32x4 pr;                                      // the one rounding inside the operator: probabilities as operands of T
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = s[i / 2][8 * (i % 2) + 2 * e], y = s[i / 2][8 * (i % 2) + 2 * e + 1];
-        if constexpr (PIECES == 3) split3(x, y, w[e]);
-        else w[e][0] = pack2<O>(x, y);
-      }
+      for (int e = 0; e < 4; ++e) pr[e] = pack2<T>(s[i / 2][8 * (i % 2) + 2 * e], s[i / 2][8 * (i % 2) + 2 * e + 1]);
 #pragma unroll
       for (int dt = 0; dt < NB; ++dt) {
         const unsigned char* at = tv + v_at[dt % (GP / 4)] + dt / (GP / 4) * GP * 16 + i * 16 * CH * 16;
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 8 * CH * 16)));
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) o[dt] = Mma<O>::m32(u32x4{lo.x, lo.y, hi.x, hi.y}, u32x4{w[0][j], w[1][j], w[2][j], w[3][j]}, o[dt]);
+        o[dt] = Mma<T>::m32(u32x4{lo.x, lo.y, hi.x, hi.y}, pr, o[dt]);
       }
     }
   };
@@ -808,8 +787,8 @@ int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const dim3 grid((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits));
   const bool even = l.a.pages.page_tokens % 32 == 0;
   if (!p.few) {
-    if constexpr (kHasMany<T, NB>) {
-      if (l.a.pages.page_tokens < ManyForm<T, NB>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
+    if constexpr (sizeof(T) == 2) {
+      if (l.a.pages.page_tokens < ManyForm<NB>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
       else hipLaunchKernelGGL((cache_many_kernel<T, NB, false>), grid, dim3(256), 0, s, l);
     }
   } else if (even) {

@@ -213,19 +213,20 @@ CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   CachePlan p;
   p.nb = blocks_of(d);
   p.rows = tq * group;
-  // us, few / many rows a workgroup: bf16, causal, 32 / 8 heads of 128, 64 rows a key head against 2048 keys 11.2 / 16.0, 16384 21.4 / 31.1, 16 x 4096 80 / 72; 128 rows against
-  // 2048 13.3 / 18.1, 16 x 4096 137 / 90; 100 of 30 heads of 64 against 2000 15.0 / 18.7, 16 x 1000 62 / 31.
-  p.few = p.rows <= 64 || (dtype == WMDEC_F32 && !kHasMany<float, 7> && p.nb >= 7);
+  // us, blocks of 16 rows / of 128: bf16, causal, 32 / 8 heads of 128, 64 rows a key head against 2048 keys 11.2 / 16.0, 16384 21.4 / 31.1, 16 x 4096 80 / 72; 128 rows against
+  // 2048 13.3 / 18.1, 16 x 4096 137 / 90; 100 of 30 heads of 64 against 2000 15.0 / 18.7, 16 x 1000 62 / 31.  In fp32, where products weigh more than what is widened for
+  // them, all: 1000x1000 of 12 of 64 19 / 30, four of 1000x3000 of 8 of 128 161 / 221, 2000x2000 of 16 of 160 138 / 205, of 192 247 / 226.
+  p.few = p.rows <= 64 || dtype == WMDEC_F32;
   p.row_blocks = (p.rows + p.bq() - 1) / p.bq();
   const long blocks = (long)heads * p.row_blocks;
   long ranges;
   if (p.few) {
-    // Up to sixteen ranges of 256 keys or more, then of 512 or more, at most 64 (us, 256 or 512 keys a range: one token of 32 / 8 heads of 128 against 2048 10.6 / 12.1, 16384
-    // 17.0 / 15.8; 512 or 1024: against 65536 22.8 / 20.5), as long as there are no more than four workgroups a compute unit.
-    ranges = std::min({1024 / blocks, std::max(std::min(16L, tk / 256L), tk / 512L), (long)kCacheMaxSplits});
+    // Up to eight ranges of 256 keys or more, then of 512 or more, at most 64 (us, 256 or 512 keys a range: one token of 32 / 8 heads of 128 against 2048 10.6 / 12.1, 16384
+    // 17.0 / 15.8, 16 x 4096 23.1 / 20.3; 512 or 1024: against 65536 22.8 / 20.5), as long as there are no more than four workgroups a compute unit.
+    ranges = std::min({1024 / blocks, std::max(std::min(8L, tk / 256L), tk / 512L), (long)kCacheMaxSplits});
   } else {
     // Partial outputs of 128 rows weigh: s ranges take a / s for their keys, b * s for writing and reading what they leave, and the second launch.
-    const double a = (dtype == WMDEC_F32 ? 5e-4 : 1.8e-4) * tk * 32 * p.nb, b = 1.2e-6 * 512 * 32 * p.nb * blocks;   // us
+    const double a = 1.8e-4 * tk * 32 * p.nb, b = 1.2e-6 * 512 * 32 * p.nb * blocks;   // us
     ranges = std::min({512 / blocks, tk / 256L, (long)kCacheMaxSplits, (long)std::sqrt(a / b)});
     if (ranges < 2 || a - a / ranges < 5 + b * ranges) ranges = 1;
   }
