@@ -76,6 +76,13 @@ struct Reader {
     if (v == (unsigned long)-1 && PyErr_Occurred()) ok = false;
     return (int)v;
   }
+  int whole(int i) {   // an index that 32 bits hold
+    if (!ok) return 0;
+    const long long v = PyLong_AsLongLong(args[i]);
+    if (v == -1 && PyErr_Occurred()) ok = false;
+    else if (v != (int)v) { ok = false; PyErr_Format(PyExc_ValueError, "argument %d: %lld is out of range", i, v); }
+    return (int)v;
+  }
   int flag(int i) {   // int() of the argument: None and texts that are no number are refused, 0.5 is 0
     if (!ok) return 0;
     PyObject* whole = PyNumber_Long(args[i]);
@@ -393,7 +400,7 @@ bool cache(StridedReader& r, int at, int at_table, int64_t n, wmdec_cache& c, wm
   r.args = &PyTuple_GET_ITEM(spec, 0);
   const at::Tensor* data = r.need(0, 2);
   r.dense(data, 0);
-  c.page_tokens = r.integer(1); c.heads = r.integer(2); c.d = r.integer(3);
+  c.page_tokens = r.whole(1); c.heads = r.whole(2); c.d = r.whole(3);
   r.args = outer;
   if (!r.ok) return false;
   c.data = r.address_of(data); c.pages = (int)data->size(0);
@@ -447,7 +454,7 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t na) {
   if (r.none(3)) r.fail(PyExc_TypeError, "tensor expected", 3);
   const int* lens = (const int*)r.typed(3, {n}, {at::kInt});
   const float scale = r.real(5);
-  const int tk = r.integer(6), causal = r.flag(7);
+  const int tk = r.whole(6), causal = r.flag(7);
   const int* counts = (const int*)r.typed(8, {n}, {at::kInt});
   const at::Tensor* ws = r.get(9, 1);
   r.dense(ws, 9);

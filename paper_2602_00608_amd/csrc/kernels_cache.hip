@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kSteps = 2;   // tokens of a lane, on their way together
 
-struct TokenParams { CacheTokens a; int chunks; long units; };   // units: (sample, chunk of tokens, head), a wavefront each
+struct TokenParams { CacheTokens a; int chunks; unsigned units; };   // units: (sample, chunk of tokens, head), a wavefront each
 
 // A lane has 16 bytes of a state; lanes of a token, tokens of a wavefront at a time.
 template <typename T> constexpr int kLaneChannels = 16 / (int)sizeof(T);
@@ -28,9 +28,10 @@ template <typename T, int NB, typename F>
 __device__ __forceinline__ void for_tokens(const TokenParams& p, F f) {
   constexpr int LANES = lanes_of(NB, kLaneChannels<T>), ABREAST = tokens_abreast(NB, kLaneChannels<T>);
   const CachePages& c = p.a.pages;
-  const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // (below 2^26: cache_tokens_fit)
   if (unit >= p.units) return;
-  const int lane = threadIdx.x & 63, h = (int)(unit % c.heads), chunk = (int)(unit / c.heads % p.chunks), n = (int)(unit / c.heads / p.chunks);
+  const unsigned above = unit / (unsigned)c.heads;
+  const int lane = threadIdx.x & 63, h = (int)(unit - above * (unsigned)c.heads), n = (int)(above / (unsigned)p.chunks), chunk = (int)(above - (unsigned)n * (unsigned)p.chunks);
   const int count = p.a.counts ? min(p.a.counts[n], p.a.t) : p.a.t;
   const long first = p.a.first ? p.a.first[n] : 0, most = (long)c.table_pages * c.page_tokens;
   const int own = lane / LANES;
@@ -188,7 +189,7 @@ int launch_type(const CacheTokens& a, int dtype, hipStream_t s) {
   const size_t es = dtype_size(dtype);
   p.chunks = chunks_of(a.t, a.pages.d, 16 / (int)es);
   const bool stream = pieces(a.k, a.ks, a.pages.d, es) && pieces(a.v, a.vs, a.pages.d, es) && (!WRITE || a.pages.d * es >= 128);
-  p.units = (long)a.n * p.chunks * a.pages.heads;
+  p.units = (unsigned)((long)a.n * p.chunks * a.pages.heads);
   if (dtype == WMDEC_F32) return launch_width<float, WRITE>(p, stream, s);
   return dtype == WMDEC_BF16 ? launch_width<bf16_t, WRITE>(p, stream, s) : launch_width<f16_t, WRITE>(p, stream, s);
 }

@@ -468,3 +468,178 @@ def test_attend_past_32_bit_offsets():
         kh, vh = (ref.cache_held(host(x), "bf16") for x in (k, v))
         want, weighted = ref.cross_attention(host(q), kh, vh, 0.0625)
         assert (np.abs(host(o) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.0625, 300, vh)).all()
+
+
+# ------------------------------------------------------------------ together, as they are used
+def test_a_stream_of_frames():
+    """A block's part of a stream that is made frame by frame: rotary positions, the frame's keys and values into the page of the oldest frame, attention to
+    the frames that are there.  The order of a table's pages does not matter to attention, so the oldest page is simply written over."""
+    r = rng(30)
+    tokens, hq, hk, d, window, n = 45, 6, 2, 64, 3, 2
+    freq = torch.empty(32, dtype=torch.float64, device="cuda")
+    wmdec.rope_frequencies((16, 24, 24), freq)
+    f = ref.rope_frequencies((16, 24, 24))
+    cache, check = new_cache(n * window, tokens, hk, d)
+    table = ints(r.permutation(n * window).reshape(n, window))
+    seen = []
+    for frame in range(6):
+        place = np.stack([np.full(tokens, frame), np.arange(tokens) // 9, np.arange(tokens) % 9], -1)
+        x = G.stored(r.standard_normal((n, tokens, hq + 2 * hk, d)), "bf16")
+        xd = dev(x, "bf16")
+        q, k, v = xd[:, :, :hq], xd[:, :, hq:hq + hk], xd[:, :, hq + hk:]
+        wmdec.rope(q, k, ints(place), freq, (16, 24, 24), q, k)
+        first = ints([frame % window * tokens] * n)
+        wmdec.cache_write(k, v, cache, table, first)
+        lens = min(frame + 1, window) * tokens
+        o = torch.empty((n, tokens, hq, d), dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(max(16, wmdec.cache_attention_workspace_bytes(q, cache, window * tokens)), dtype=torch.uint8, device="cuda")
+        wmdec.cache_attention(q, cache, table, ints([lens] * n), o, 0.125, window * tokens, workspace=ws)
+        turned = ref.rope(x[:, :, hq:hq + hk], place[None].repeat(n, 0), f, (16, 24, 24))
+        assert (np.abs(host(k) - turned) <= HALF["bf16"] * np.abs(turned) + 2.0 ** -18).all()
+        seen = (seen + [(host(k), x[:, :, hq + hk:])])[-window:]
+        kh, vh = (ref.cache_held(np.concatenate([s[i] for s in seen], 1), "bf16") for i in (0, 1))
+        want, weighted = ref.cross_attention(host(q), kh, vh, 0.125)
+        assert (np.abs(host(o) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.125, lens, vh)).all()
+        # the same states, read back and attended to as dense ones
+        ko, vo = (torch.empty((n, lens, hk, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        wmdec.cache_read(cache, table, ko, vo)
+        dense = torch.empty_like(o)
+        ws = torch.empty(max(16, wmdec.cross_attention_workspace_bytes(q, ko)), dtype=torch.uint8, device="cuda")
+        wmdec.cross_attention(q, ko, vo, dense, 0.125, workspace=ws)
+        assert (np.abs(host(dense) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.125, lens, vh)).all()
+    check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_a_prompt_and_then_token_by_token(dtype):
+    """A padded batch of prompts in two stretches, and then a token of every sequence at a time."""
+    r = rng(31)
+    n, hq, hk, d, page = 3, 4, 2, 96, 24
+    lengths = np.array([130, 64, 7])
+    total = lengths + 5
+    q, k, v = (G.stored(r.standard_normal((n, 135, h, d)), dtype) for h in (hq, hk, hk))
+    per = -(-135 // page)
+    cache, check = new_cache(n * per + 1, page, hk, d)
+    table = ints(r.permutation(n * per + 1)[:n * per].reshape(n, per))
+    kh, vh = ref.cache_held(k, dtype), ref.cache_held(v, dtype)
+    steps = [(np.zeros(n, int), np.minimum(lengths, 60)), (np.minimum(lengths, 60), lengths - np.minimum(lengths, 60))] + [(lengths + i, np.ones(n, int)) for i in range(5)]
+    for first, count in steps:
+        t = int(count.max())
+        part = [torch.full((n, t, h, d), float("nan"), device="cuda").to(G.TORCH[dtype]) for h in (hq, hk, hk)]     # what pads the batch does not matter
+        for b in range(n):
+            for x, y in zip(part, (q, k, v)):
+                x[b, :count[b]] = dev(y[b, first[b]:first[b] + count[b]], dtype)
+        wmdec.cache_write(part[1], part[2], cache, table, ints(first), ints(count))
+        o = torch.full((n, t, hq, d), MARK, device="cuda").to(G.TORCH[dtype])
+        ws = torch.empty(max(16, wmdec.cache_attention_workspace_bytes(part[0], cache, 135)), dtype=torch.uint8, device="cuda")
+        wmdec.cache_attention(part[0], cache, table, ints(first + count), o, 0.1, 135, causal=True, counts=ints(count), workspace=ws)
+        got = host(o)
+        for b in range(n):
+            assert (got[b, count[b]:] == MARK).all()
+            for i in range(count[b]):
+                see = first[b] + i + 1
+                at = slice(first[b] + i, first[b] + i + 1)
+                want, weighted = ref.cross_attention(q[b:b + 1, at], kh[b:b + 1, :see], vh[b:b + 1, :see], float(np.float32(0.1)))
+                assert (np.abs(got[b:b + 1, i:i + 1] - want) <= tolerance(dtype, q[b:b + 1, at], kh[b:b + 1, :see], want, weighted, 0.1, see, vh[b:b + 1, :see])).all(), (b, i)
+    assert (first + count == total).all()
+    check()
+
+
+def test_graphs_are_replayed():
+    """A token's step captured: what it reads and writes is on the device, positions and lengths among it.  Two graphs share a workspace; every replay is compared with
+    an eager step on a cache of its own, with eager work and synchronisation in between."""
+    r = rng(32)
+    n, hq, hk, d, page, most = 2, 8, 2, 128, 64, 3000
+    per = -(-most // page)
+    table = ints(r.permutation(n * per).reshape(n, per))
+    start = [dev(r.standard_normal((n, 2500, hk, d)), "bf16") for _ in range(2)]
+    caches = [new_cache(n * per, page, hk, d)[0] for _ in range(2)]
+    for c in caches:
+        wmdec.cache_write(*start, c, table)
+    q, k, v = (torch.zeros((n, 1, h, d), dtype=torch.bfloat16, device="cuda") for h in (hq, hk, hk))
+    first, lens = ints([2500, 1300]), ints([2501, 1301])
+    o, wide, qw, ow = torch.empty_like(q), [torch.empty((n, 1, hk, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)], torch.zeros((n, 90, hq, d), dtype=torch.bfloat16, device="cuda"), None
+    ow = torch.empty_like(qw)
+    ws = torch.empty(max(wmdec.cache_attention_workspace_bytes(x, caches[0], most) for x in (q, qw)), dtype=torch.uint8, device="cuda")
+    assert min(wmdec.cache_attention_workspace_bytes(x, caches[0], most) for x in (q, qw)) > 0
+
+    def token(c, out, back):
+        wmdec.cache_write(k, v, c, table, first)
+        wmdec.cache_attention(q, c, table, lens, out, 0.09, most, workspace=ws)
+        wmdec.cache_read(c, table, back[0], back[1], first)
+
+    def many(c, out):
+        wmdec.cache_attention(qw, c, table, lens, out, 0.09, most, causal=True, workspace=ws)
+    token(caches[0], o, wide)
+    many(caches[0], ow)
+    torch.cuda.synchronize()
+    one, two = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(one):
+        token(caches[0], o, wide)
+    with torch.cuda.graph(two):
+        many(caches[0], ow)
+    for i in range(5):
+        for x in (q, k, v, qw):
+            x.copy_(dev(r.standard_normal(tuple(x.shape)), "bf16"))
+        one.replay()
+        if i % 2:
+            two.replay()
+        eager, eb, em = torch.empty_like(o), [torch.empty_like(x) for x in wide], torch.empty_like(ow)
+        token(caches[1], eager, eb)
+        many(caches[1], em)
+        if not i % 2:
+            two.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, eager) and torch.equal(ow, em) and all(torch.equal(a, b) for a, b in zip(wide, eb))
+        assert torch.isfinite(o).all() and torch.isfinite(ow).all()
+        first += 1
+        lens += 1
+
+
+def test_calls_on_streams_of_their_own():
+    """Calls on two streams at once, each with a cache, a workspace and outputs of its own, give what they give one after the other."""
+    r = rng(33)
+    jobs = []
+    for i, (dtype, tq) in enumerate((("bf16", 1), ("f16", 100))):
+        k, v, q = (dev(r.standard_normal((2, t, h, 64)), dtype) for t, h in ((3000, 2), (3000, 2), (tq, 8)))
+        cache, _ = new_cache(2 * 47, 64, 2, 64)
+        table = ints(r.permutation(94).reshape(2, 47))
+        o = [torch.empty_like(q) for _ in range(6)]
+        ws = torch.empty(max(16, wmdec.cache_attention_workspace_bytes(q, cache, 3000)), dtype=torch.uint8, device="cuda")
+        back = [torch.empty_like(k) for _ in range(2)]
+        jobs.append((k, v, q, cache, table, o, ws, back))
+    lens = ints([3000, 1700])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for i in range(5):
+        for s, (k, v, q, cache, table, o, ws, back) in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                wmdec.cache_write(k, v, cache, table)
+                wmdec.cache_attention(q, cache, table, lens, o[i], 0.125, 3000, workspace=ws)
+                wmdec.cache_read(cache, table, *back)
+    torch.cuda.synchronize()
+    for k, v, q, cache, table, o, ws, back in jobs:
+        wmdec.cache_attention(q, cache, table, lens, o[5], 0.125, 3000, workspace=ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, o[5]) for x in o[:5])
+        same_values(host(back[0]), ref.cache_held(host(k), {torch.bfloat16: "bf16", torch.float16: "f16"}[k.dtype]))
+
+
+def test_attend_samples_that_share_pages():
+    """A prefix that all samples have in common is held once: rows of the table with the same pages, and one row for all."""
+    r = rng(34)
+    k, v = (dev(r.standard_normal((1, 200, 2, 64)), "bf16") for _ in range(2))
+    cache, check = new_cache(7, 32, 2, 64)
+    row = ints([[4, 0, 6, 1, 2, 3, 5]])
+    wmdec.cache_write(k, v, cache, row)
+    for tq in (1, 80):
+        q = dev(r.standard_normal((3, tq, 4, 64)), "bf16")
+        o, again = torch.empty_like(q), torch.empty_like(q)
+        lens = ints([200, 33, 150])
+        wmdec.cache_attention(q, cache, row.expand(3, 7), lens, o, 0.125, 200)
+        wmdec.cache_attention(q, cache, row.repeat(3, 1), lens, again, 0.125, 200)
+        assert torch.equal(o, again)
+        kh, vh = (ref.cache_held(host(x), "bf16").repeat(3, 0) for x in (k, v))
+        want, weighted = ref.cross_attention(host(q), kh, vh, 0.125, [200, 33, 150])
+        assert (np.abs(host(o) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.125, 200, vh)).all()
+    check()
