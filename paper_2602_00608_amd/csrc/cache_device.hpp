@@ -18,6 +18,7 @@ constexpr int kFewRows = 16, kManyRows = 128, kCacheMaxSplits = 64;
 struct CachePlan {
   int nb = 1;                                        // blocks of 32 channels
   bool few = true;                                   // blocks of kFewRows rows, else of kManyRows
+  bool halves = false;                               // many: the wavefronts of a workgroup are eight and take halves of a tile's keys
   int rows = 0, row_blocks = 0, range = 0, splits = 1;
   __host__ __device__ int bq() const { return few ? kFewRows : kManyRows; }
   __host__ __device__ int block_rows() const { return rows < bq() ? rows : bq(); }   // of partial outputs
@@ -400,31 +401,35 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
 // before; the codes of the tile after that are on their way meanwhile.  Per 32 keys a wavefront forms S^T = K Q^T of 32x32x16 products (keys along the accumulator's
 // registers, one row a lane), the softmax, and O^T += V^T P^T with the probabilities as they are in their registers: an accumulator's keys of lane half lk
 // are 8 (r / 4) + 4 lk + r % 4, so V^T is read from LDS in that order of keys, transposed on the way.
-template <int NB>
+__host__ __device__ constexpr bool has_halves(int nb) { return nb != 4; }   // (measured beside the rule in kernels_cache.hip)
+
+// KW: 1, or 2 where there are few blocks: eight wavefronts, of which the first and the last four take half of a tile's keys each, joined at the end.
+template <int NB, int KW>
 struct ManyForm {
-  static constexpr int D = 32 * NB, KT = NB <= 4 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = NB <= 1 ? 4 : NB == 2 ? 3 : 2;   // (TILE: chunks of a tile)
-  static constexpr bool TIGHT = NB >= 7;   // queries and outputs leave few registers
-  static constexpr bool PAIR = NB >= 3;              // a thread widens a block of 32 channels of a key and of its value, else of one of them
+  static constexpr int D = 32 * NB, KT = NB <= 4 || KW == 2 ? 64 : 32, CH = 4 * NB, TILE = KT * CH, WAVES = KW == 2 ? 2 : NB <= 1 ? 4 : NB == 2 ? 3 : 2;   // (TILE: chunks of a tile)
+  static constexpr bool TIGHT = NB >= 7;             // queries and outputs leave few registers
+  static constexpr bool PAIR = NB >= (KW == 2 ? 5 : 3);   // a thread widens a block of 32 channels of a key and of its value, else of one of them
 };
 
 // every LDS access of this wavefront is done, and so for the others: codes on their way are not waited for
 __device__ __forceinline__ void sync_tiles_of_cache() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 // SMALL: for pages of any size; else they hold a tile or more.
-template <typename T, int NB, bool SMALL>
-__global__ __launch_bounds__(256, (ManyForm<NB>::WAVES)) void cache_many_kernel(CacheLaunch launch) {
-  typedef ManyForm<NB> F;
-  constexpr int CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32, QS = CH / 2, TILE = F::TILE, ROW = 16 * NB, EXP = exponent_bytes(NB);
+template <typename T, int NB, int KW, bool SMALL>
+__global__ __launch_bounds__(256 * KW, (ManyForm<NB, KW>::WAVES)) void cache_many_kernel(CacheLaunch launch) {
+  typedef ManyForm<NB, KW> F;
+  constexpr int CH = F::CH, D = F::D, KT = F::KT, NS = KT / 32 / KW, QS = CH / 2, TILE = F::TILE, ROW = 16 * NB, EXP = exponent_bytes(NB);
   constexpr int GP = CH % 8 == 0 ? 8 : 4;            // chunks that are exchanged among each other
   constexpr bool TIGHT = F::TIGHT;
-  __shared__ __align__(16) u32x4 s_k[2 * TILE], s_v[2 * TILE];
+  __shared__ __align__(16) u32x4 s_k[4 * TILE];      // two tiles of keys, and two of values
+  u32x4* const s_v = s_k + 2 * TILE;
   // what is out of the ordinary in a tile: bits of the keys whose values are not a number, by block; whether there are any (1), or keys without a page (2); those
   constexpr int FLAGS = 2 * NB, GONE = FLAGS + 1, BAD = FLAGS + 3;
   __shared__ unsigned s_bad[3][BAD];
   const CacheAttentionArgs& a = launch.a;
   const CachePages& cp = a.pages;
   const CachePlan& p = launch.plan;
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lk = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lk = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6) % 4, kw = __builtin_amdgcn_readfirstlane(tid >> 6) / 4;
 
   // workgroup id -> (sample, key head, range, row block), as for few rows
   const int per_sample = cp.heads * p.splits * p.row_blocks, n = blockIdx.x / per_sample;
@@ -581,13 +586,13 @@ __global__ __launch_bounds__(256, (ManyForm<NB>::WAVES)) void cache_many_kernel(
       for (int r = 0; r < 16; ++r) s[ns][r] = 0.f;
 #pragma unroll
       for (int st = 0; st < QS; ++st) {
-        s[ns] = Mma<T>::m32(tk[k_at[st % (GP / 2)] + st / (GP / 2) * GP + ns * 32 * CH], q[st], s[ns]);
+        s[ns] = Mma<T>::m32(tk[k_at[st % (GP / 2)] + st / (GP / 2) * GP + (kw * NS + ns) * 32 * CH], q[st], s[ns]);
       }
     }
 #pragma unroll
     for (int ns = 0; ns < NS; ++ns) {
-      const int at = k0 + 32 * ns;
-      const unsigned is_there = (unsigned)(there >> (32 * ns));
+      const int at = k0 + 32 * (kw * NS + ns);
+      const unsigned is_there = (unsigned)(there >> (32 * (kw * NS + ns)));
       if (is_there != ~0u || at + 31 > all_see) {
         const int seen = see - at + 1;
         const unsigned b = (is_there & (seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1)) >> (4 * lk);
@@ -659,7 +664,7 @@ __global__ __launch_bounds__(256, (ManyForm<NB>::WAVES)) void cache_many_kernel(
       for (int e = 0; e < 4; ++e) pr[e] = pack2<T>(s[i / 2][8 * (i % 2) + 2 * e], s[i / 2][8 * (i % 2) + 2 * e + 1]);
 #pragma unroll
       for (int dt = 0; dt < NB; ++dt) {
-        const unsigned char* at = tv + v_at[dt % (GP / 4)] + dt / (GP / 4) * GP * 16 + i * 16 * CH * 16;
+        const unsigned char* at = tv + v_at[dt % (GP / 4)] + dt / (GP / 4) * GP * 16 + (kw * 2 * NS + i) * 16 * CH * 16;
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)at));
         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(at + 8 * CH * 16)));
         o[dt] = Mma<T>::m32(u32x4{lo.x, lo.y, hi.x, hi.y}, pr, o[dt]);
@@ -685,7 +690,7 @@ __global__ __launch_bounds__(256, (ManyForm<NB>::WAVES)) void cache_many_kernel(
     }
     if (tid < BAD) s_bad[(j + 2) % 3][tid] = 0;
     const int k0 = begin + j * KT, left = end - k0;
-    if (idle || k0 > last_see) continue;
+    if (idle || k0 + 32 * kw * NS > last_see) continue;
     there = left >= 64 ? ~0ul : (1ul << left) - 1;
     const unsigned* bad = s_bad[j % 3];
     const unsigned flags = __builtin_amdgcn_readfirstlane((int)bad[FLAGS]);
@@ -707,6 +712,32 @@ __global__ __launch_bounds__(256, (ManyForm<NB>::WAVES)) void cache_many_kernel(
 
   // ---- output.  A lane holds channels 32 dt + 8 g + 4 lk .. + 3 of its row
   l += __shfl_xor(l, 32);
+  if constexpr (KW == 2) {                           // the last four wavefronts' sums to the first four, through the tiles' memory
+    __shared__ float2 s_ml[kManyRows];
+    f32x4* s_o = reinterpret_cast<f32x4*>(s_k) + (wave * 32 + l32) * (D / 4);
+    sync_tiles_of_cache();
+    if (kw == 1) {
+      if (lk == 0) s_ml[wave * 32 + l32] = make_float2(m, l);
+#pragma unroll
+      for (int dt = 0; dt < NB; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) s_o[(8 * dt + 2 * g + lk) ^ (l32 & 7)] = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+    }
+    sync_tiles_of_cache();
+    if (kw == 1) return;
+    const float2 e = s_ml[wave * 32 + l32];
+    const float top = fmaxf(m, e.x), own = cache_weight(m, top), other = cache_weight(e.x, top);
+    m = top;
+    l = l * own + e.y * other;
+#pragma unroll
+    for (int dt = 0; dt < NB; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 x = s_o[(8 * dt + 2 * g + lk) ^ (l32 & 7)];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[dt][4 * g + r] = o[dt][4 * g + r] * own + x[r] * other;
+      }
+  }
   if (row >= view.rows) return;
   if (whole) {
     T* dst = output_row<T>(a, n, h, row);
@@ -780,6 +811,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheLaunch launch, int
   }
 }
 
+template <typename T, int NB, int KW>
+void cache_launch_many(const CacheLaunch& l, dim3 grid, hipStream_t s) {
+  if (l.a.pages.page_tokens < ManyForm<NB, KW>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, KW, true>), grid, dim3(256 * KW), 0, s, l);
+  else hipLaunchKernelGGL((cache_many_kernel<T, NB, KW, false>), grid, dim3(256 * KW), 0, s, l);
+}
+
 template <typename T, int NB>
 int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const CachePlan& p = l.plan;
@@ -788,8 +825,8 @@ int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const bool even = l.a.pages.page_tokens % 32 == 0;
   if (!p.few) {
     if constexpr (sizeof(T) == 2) {
-      if (l.a.pages.page_tokens < ManyForm<NB>::KT) hipLaunchKernelGGL((cache_many_kernel<T, NB, true>), grid, dim3(256), 0, s, l);
-      else hipLaunchKernelGGL((cache_many_kernel<T, NB, false>), grid, dim3(256), 0, s, l);
+      if (!p.halves) cache_launch_many<T, NB, 1>(l, grid, s);
+      else if constexpr (has_halves(NB)) cache_launch_many<T, NB, 2>(l, grid, s);
     }
   } else if (even) {
     hipLaunchKernelGGL((cache_few_kernel<T, NB, true>), grid, dim3(256), 0, s, l);

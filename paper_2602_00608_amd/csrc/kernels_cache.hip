@@ -234,6 +234,10 @@ CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   ranges = std::max(ranges, 1L);
   p.range = std::max(128, (int)(((long)tk + ranges - 1) / ranges + 127) / 128 * 128);
   p.splits = std::max(1, (int)(((long)tk + p.range - 1) / p.range));
+  // us, four wavefronts / eight that halve the keys: one workgroup a compute unit or less, bf16, 2048x2048 of 16 of 256 137 / 98, 2000x2000 of 16 of 160 91 / 68, 1000x2000 of 30 of
+  // 64 45 / 38, 1000x1000 of 12 of 96 29 / 27, but 5 to 64 x 2048 of 32 / 8 of 128 14.1 .. 22.1 / 15.0 .. 23.3; more workgroups, 2 x 4096x4096 of 16 of 256 677 / 733, 2 x 5400x5400
+  // of 30 of 64 599 / 634.
+  p.halves = !p.few && has_halves(p.nb) && blocks * p.splits <= 256;
   return p;
 }
 
