@@ -1,8 +1,8 @@
 """Per-operator timing of the C-ABI entry points at the decoder's layer shapes and around a transformer block (one MI355X).
 
-    python -m paper_2602_00608_amd.bench_ops [--dtype f16|bf16] [--reps 20] [--block]      (or run the file directly)
+    python -m paper_2602_00608_amd.bench_ops [--dtype f16|bf16] [--reps 20] [--block] [--cache]      (or run the file directly)
 
---block: only the operators of a transformer block.  Prints one line per operator: microseconds per call, algorithmic TFLOP/s or GB/s, and the fraction of the
+--block, --cache: only the operators of a transformer block, or of a cache of keys and values in four bits.  Prints one line per operator: microseconds per call, algorithmic TFLOP/s or GB/s, and the fraction of the
 published MI355X peak (2516.6 TFLOP/s dense f16/bf16 MFMA, 8000 GB/s HBM).  Two timings per operator, both with HIP
 events on the current stream and inputs resident in HBM:
   warm  `reps` back-to-back calls on the same tensors (tensors up to a few hundred MB partly stay in the last-level
@@ -88,6 +88,7 @@ def main():
     ap.add_argument("--dtype", default="f16", choices=["f16", "bf16"])
     ap.add_argument("--reps", type=int, default=20)
     ap.add_argument("--block", action="store_true")
+    ap.add_argument("--cache", action="store_true")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         sys.exit("bench_ops: no GPU visible; the HIP path has no CPU fallback")
@@ -104,8 +105,11 @@ def main():
         wmdec.gn_stats(x, groups, eps, mean, rstd, ws)
         return mean, rstd, ws
 
-    if args.block:
-        return block_operators(dt, line, args.reps)
+    if args.block or args.cache:
+        for wanted, operators in ((args.block, block_operators), (args.cache, cache_operators)):
+            if wanted:
+                operators(dt, line, args.reps)
+        return
 
     # cin, cout, h_out, w_out, kernel, upsample, normalise + SiLU on load, residual
     convs = [(128, 128, 480, 720, 3, 0, 1, 1), (256, 128, 480, 720, 3, 0, 1, 0), (256, 256, 240, 360, 3, 0, 1, 1),
@@ -213,6 +217,7 @@ def main():
         line("adaln 3 launches", "batch %d %d->3x%d" % (batch, d, d), sep, nbytes, "GB/s", PEAK_GBPS)
 
     block_operators(dt, line, args.reps)
+    cache_operators(dt, line, args.reps)
 
 
 def block_operators(dt, line, reps):
@@ -246,6 +251,35 @@ def block_operators(dt, line, reps):
         flops, nbytes = 4.0 * n * hq * tq * tk * d, 2 * (2 * q.numel() + 2 * k.numel())
         unit = "TFLOP/s" if flops / nbytes >= 315 else "GB/s"
         line("cross_attention", "%dx%dx%d, %d/%d of %d" % (n, tq, tk, hq, hk, d), us, flops if unit == "TFLOP/s" else nbytes, unit, PEAK_TFLOPS if unit == "TFLOP/s" else PEAK_GBPS)
+
+
+def cache_operators(dt, line, reps):
+    """Keys and values in four bits: written, read back, attended to.  (A token's head of d channels is 2 * 17 / 32 * d bytes in the cache.)"""
+    def filled(n, t, hk, d, page):
+        per = -(-t // page)
+        cache = wmdec.Cache(torch.empty((n * per, wmdec.cache_page_bytes(page, hk, d)), dtype=torch.uint8, device="cuda"), page, hk, d)
+        table = torch.randperm(n * per, device="cuda").to(torch.int32).view(n, per)
+        k, v = (torch.randn((n, t, hk, d), device="cuda").to(dt) for _ in range(2))
+        wmdec.cache_write(k, v, cache, table)
+        return cache, table, k, v
+
+    for n, t, hk, d, page in ((1, 1, 30, 64, 256), (2, 5400, 30, 64, 5400), (1, 32768, 8, 128, 256)):
+        cache, table, k, v = filled(n, t, hk, d, page)
+        nbytes = 2 * (2 * k.numel() + k.numel() * 17 // 32)
+        shape = "%dx%d of %dx%d" % (n, t, hk, d)
+        line("cache_write", shape, timeit(lambda: wmdec.cache_write(k, v, cache, table), reps), nbytes, "GB/s", PEAK_GBPS)
+        line("cache_read", shape, timeit(lambda: wmdec.cache_read(cache, table, k, v), reps), nbytes, "GB/s", PEAK_GBPS)
+
+    for n, tq, tk, hq, hk, d, page in ((2, 1, 77, 30, 30, 64, 64), (16, 1, 4096, 32, 8, 128, 64), (4, 1, 65536, 32, 8, 128, 256), (1, 700, 3500, 16, 4, 128, 100),
+                                       (1, 5400, 10800, 30, 30, 64, 5400), (1, 8192, 8192, 32, 8, 128, 256)):
+        cache, table, _, _ = filled(n, tk, hk, d, page)
+        q = torch.randn((n, tq, hq, d), device="cuda").to(dt)
+        o, lens = torch.empty_like(q), torch.full((n,), tk, dtype=torch.int32, device="cuda")
+        ws = torch.empty(max(16, wmdec.cache_attention_workspace_bytes(q, cache, tk)), dtype=torch.uint8, device="cuda")
+        us = timeit(lambda: wmdec.cache_attention(q, cache, table, lens, o, d ** -0.5, tk, workspace=ws), reps)
+        flops, nbytes = 4.0 * n * hq * tq * tk * d, 4 * q.numel() + 2 * n * tk * hk * d * 17 // 32
+        unit = "TFLOP/s" if flops / nbytes >= 315 else "GB/s"
+        line("cache_attention", "%dx%dx%d, %d/%d of %d" % (n, tq, tk, hq, hk, d), us, flops if unit == "TFLOP/s" else nbytes, unit, PEAK_TFLOPS if unit == "TFLOP/s" else PEAK_GBPS)
 
 
 if __name__ == "__main__":

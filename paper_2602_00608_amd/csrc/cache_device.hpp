@@ -4,6 +4,18 @@
 // and l = sum_j 2^(a q.k_j - m) are formed in one pass over the keys; o / l is what comes out.  Keys and values are widened to 16 bits on their way into the matrix
 // cores, which rounds nothing (cache_pages.hpp); fp32 queries and probabilities go in as the three bf16 numbers that they are the sum of (24 bits: exact, and
 // three products of 16 bits where products of 32 would take eight times as long).
+//
+// What bounds it.  Few rows: the one read of the cache, and behind short ones the trips (length, page number, codes), what a wavefront alone on its SIMD waits for from
+// step to step, and the second launch.  Many rows: the power that the matrix cores may draw, beside it the exponentials and what widening costs; of those 207
+// vector instructions a wavefront and tile of 64 keys at 64 channels, 32 are exponentials of four times the cycles.
+// us on inputs that are not the call's before, host included: one token of 32 / 8 heads of 128 against 4 x 65536 tokens (ragged) in bf16 39.0, of which the first kernel 30.2 =
+// 4.7 TB/s and the second 4.7, against 65536 20.6, 16 x 4096 in f16 20.1, 2048 10.6; 30 heads of 64 against 4 x 32768 62 = 4.3 TB/s; 5400x10800 of 30 of 64 in f16 620 = 720 TFLOP/s,
+// 8192x8192 of 32 / 8 of 128 in bf16 1100 = 1000, 2 x 4096x4096 of 16 of 256 677 = 812, 3000x3000 of 8 of 128 in fp32 108 = 341 (products of 32 bits reach 155 at most).
+// Steps, us for 4 x 65536, 16 x 4096, 5400x10800: sixteen rows a wavefront for all sizes, two sets of codes under way 46.7, 24.8, 1157; 128 rows a workgroup 669 of the last; one
+// set, asked for again as soon as it has been used, four wavefronts a SIMD 39.5, 20.8; pages by the wavefront where they are multiples of 32; places from tile to tile 618.
+// Measured and not kept: 32 rows a wavefront for few rows (half the wavefronts: 16 x 64 tokens against 4096 294 against 181), 16 wavefronts a workgroup in place of ranges of
+// keys (2000 tokens 14.1 against 10.7, eight samples of 1000 11.8 against 15.7: no better but there), the sum of the probabilities as a product with ones (5400x10800 672), four wavefronts a
+// SIMD at 64 channels and many rows, with what a thread widens worked out anew (645).
 #pragma once
 #include <algorithm>
 
@@ -84,7 +96,7 @@ template <int N> struct Words { unsigned w[N]; };
 // A wavefront takes 16 rows and every fourth 32 keys of its workgroup's range by itself: S^T = K Q^T of 16x16x32 products, whose keys come straight from memory (a lane
 // has 1 / 4 of a key's channels; the queries are in the same order), the softmax, and O^T += V^T P^T with the values turned in LDS.  The next 32 keys are on
 // their way meanwhile.
-template <typename T, int NB> constexpr int kFewWaves = sizeof(T) == 4 ? (NB <= 2 ? 3 : NB <= 5 ? 2 : 1) : NB <= 4 ? 4 : 2;   // a SIMD
+template <typename T, int NB> constexpr int kFewWaves = sizeof(T) == 4 ? (NB <= 2 ? 3 : 2) : NB <= 4 ? 4 : 2;   // a SIMD
 
 // EVEN: pages hold a multiple of 32 tokens, so that 32 keys lie together in one of them: its number and address are the wavefront's, not a lane's.
 template <typename T, int NB, bool EVEN>

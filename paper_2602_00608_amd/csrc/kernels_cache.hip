@@ -1,8 +1,12 @@
 // A cache of keys and values in four bits: states are rounded to it as they are written, and read back.  (Attention to it: cache_device.hpp.)
 //
 // Bound by HBM: 16-bit states are 3.8 times what is held of them, so the dense side counts.  A wavefront takes tokens of one head: its reads of the
-// states are whole rows of a head, what it writes of a page lies together, and neighbouring wavefronts have the next heads of the same tokens.  A lane has eight
-// channels (16 bytes of 16-bit states, four of codes); the four lanes of a block find its largest magnitude among themselves.
+// states are whole rows of a head, what it writes of a page lies together, and neighbouring wavefronts have the next heads of the same tokens.  A lane has 16 bytes of a
+// state; the four lanes of a block (eight in fp32) find its largest magnitude among themselves.
+// us on inputs that are not the call's before: 32768 tokens of 8 heads of 128 read back in bf16 26.8 = 6.3 TB/s (a copy reaches 5.1 to 5.4), written and read back 63; a frame of
+// 5400 tokens of 30 heads of 64 and its twin written and read back 43 = 4.8 TB/s; rows that are no whole pieces of 64 bytes run at half of that (27962 of 30 of 40 read back 64).
+// Steps, reading 32768 / writing and reading two frames: 40.9, 54.6; states that are whole pieces pass by the caches 27.4, 45 (else a kernel ends with waiting for what lies in
+// the L2s; codes that pass by them too make the pair 55); two tokens of a lane under way, not four or eight 26.8, 43.  Neighbouring heads on one XCD: no difference.
 #include <algorithm>
 #include <cmath>
 
@@ -154,7 +158,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(TokenParams p) {
 int blocks_of(int d) { return (d + 31) / 32; }
 int chunks_of(int t, int d, int channels) { const int per = kSteps * tokens_abreast(blocks_of(d), channels); return (int)(((long)t + per - 1) / per); }
 
-// States that are whole 64-byte pieces of memory pass by the caches.
+// States that are whole 64-byte pieces of memory pass by the caches (us, by them or not: read back in bf16, 30 heads of 32 35 / 44, of 64 27 / 41, 8 of 128 27 / 41, but 30 of 40 79 / 65, of
+// 72 59 / 57, of 8 50 / 20); those to be written only from 128 bytes on (30 of 32 77 / 70, of 64 64 / 76).
 bool pieces(const void* p, const wmdec_strides& s, int d, size_t es) {
   return !p || ((uintptr_t)p % 64 == 0 && d * es % 64 == 0 && s.sample * es % 64 == 0 && s.token * es % 64 == 0 && s.head * es % 64 == 0);
 }

@@ -549,7 +549,7 @@ def test_graphs_are_replayed():
     """A token's step captured: what it reads and writes is on the device, positions and lengths among it.  Two graphs share a workspace; every replay is compared with
     an eager step on a cache of its own, with eager work and synchronisation in between."""
     r = rng(32)
-    n, hq, hk, d, page, most = 2, 8, 2, 128, 64, 3000
+    n, hq, hk, d, page, most = 2, 8, 2, 128, 64, 20000
     per = -(-most // page)
     table = ints(r.permutation(n * per).reshape(n, per))
     start = [dev(r.standard_normal((n, 2500, hk, d)), "bf16") for _ in range(2)]
