@@ -328,3 +328,19 @@ def cache_held(x, dtype):
         held = np.copysign(np.ldexp(CACHE_VALUES[place], e), clean)
         out[..., at:at + 32] = np.where(finite, held, np.nan)
     return out
+
+
+def seen_attention(q, k, v, scale, seen):
+    """cross_attention of queries that see keys of their own: seen [n,tq,tk]."""
+    q, k, v = _f64(q), _f64(k), _f64(v)
+    seen = np.asarray(seen, dtype=bool)
+    o, a = np.zeros(q.shape), np.zeros(q.shape)
+    some = seen.any(-1)
+    for i in range(q.shape[0]):
+        for h in range(q.shape[2]):
+            kk, vv = (x[i, :, h // (q.shape[2] // k.shape[2])] for x in (k, v))
+            s = np.where(seen[i], q[i, :, h] @ kk.T * scale, -np.inf)[some[i]]
+            p = np.exp(s - s.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            o[i, some[i], h], a[i, some[i], h] = p @ vv, p @ np.abs(vv)
+    return o, a

@@ -51,6 +51,20 @@ def test_held_oracle_at_the_ends_of_the_types():
     assert np.isnan(held[0, :32]).all() and np.isfinite(held[0, 32:]).all() and np.isnan(held[1, 64:]).all() and np.isfinite(held[1, :64]).all()
 
 
+def test_seen_attention_oracle():
+    r = np.random.default_rng(5)
+    q, k, v = r.standard_normal((2, 6, 4, 8)), r.standard_normal((2, 9, 2, 8)), r.standard_normal((2, 9, 2, 8))
+    mask = r.random((2, 9)) < 0.6
+    mask[1] = False
+    for got, want in zip(ref.seen_attention(q, k, v, 0.4, np.repeat(mask[:, None], 6, 1)), ref.cross_attention(q, k, v, 0.4, None, mask)):
+        assert np.allclose(got, want, atol=1e-14) and not got[1].any()
+    seen = np.broadcast_to(np.arange(9)[None] <= np.arange(-2, 4)[:, None], (2, 6, 9))
+    o, a = ref.seen_attention(q, k, v, 0.4, seen)
+    assert not o[:, :2].any() and np.allclose(o[:, 2], np.repeat(v[:, 0], 2, 1))
+    for j in range(3, 6):
+        assert np.allclose(o[:, j:j + 1], ref.cross_attention(q[:, j:j + 1], k, v, 0.4, [j - 1, j - 1])[0])
+
+
 # ------------------------------------------------------------------ sizes
 def test_page_bytes():
     size = wmdec.cache_page_bytes

@@ -295,16 +295,17 @@ def run_attend(dtype, n, tq, tk, hq, hk, d, page, lens=None, counts=None, causal
     for b in range(n):
         length = int(np.clip(lens[b], 0, tk))
         assert (got[b, c[b]:] == MARK).all()
-        groups = [(slice(0, c[b]), there[b:b + 1])]
+        if c[b] == 0 or tk == 0:
+            assert not got[b, :c[b]].any()
+            continue
+        seen = np.broadcast_to(there[b], (c[b], tk))
         if causal:
-            groups = [(slice(j, j + 1), there[b:b + 1] & (np.arange(tk) <= length - c[b] + j)[None]) for j in range(c[b])]
-        for rows, keep in groups:
-            if rows.stop == rows.start:
-                continue
-            want, weighted = ref.cross_attention(q[b:b + 1, rows], np.where(keep[..., None, None], kh[b:b + 1], 0), np.where(keep[..., None, None], vh[b:b + 1], 0), scale, None, keep)
-            tol = tolerance(dtype, q[b:b + 1], kh[b:b + 1], want, weighted, scale, tk, vh[b:b + 1])
-            bad = ~(np.abs(got[b:b + 1, rows] - want) <= tol)
-            assert not bad.any(), (b, rows, int(bad.sum()), np.argwhere(bad)[:4].tolist(), float(np.abs(got[b:b + 1, rows] - want)[bad].max()), float(np.broadcast_to(tol, want.shape)[bad].max()))
+            seen = seen & (np.arange(tk)[None] <= length - c[b] + np.arange(c[b])[:, None])
+        rows = slice(0, c[b])
+        want, weighted = ref.seen_attention(q[b:b + 1, rows], kh[b:b + 1], vh[b:b + 1], scale, seen[None])
+        tol = tolerance(dtype, q[b:b + 1], kh[b:b + 1], want, weighted, scale, tk, vh[b:b + 1])
+        bad = ~(np.abs(got[b:b + 1, rows] - want) <= tol)
+        assert not bad.any(), (b, int(bad.sum()), np.argwhere(bad)[:4].tolist(), float(np.abs(got[b:b + 1, rows] - want)[bad].max()), float(np.broadcast_to(tol, want.shape)[bad].max()))
     return o
 
 
@@ -345,6 +346,15 @@ def test_attend_causal(dtype):
     run_attend(dtype, 3, 40, 100, 3, 3, 40, 8, lens=[10, 39, 100], causal=True, seed=2)               # more queries than tokens: the first see none
     run_attend(dtype, 3, 140, 100, 3, 1, 64, 8, lens=[10, 0, 100], causal=True, seed=3)
     run_attend(dtype, 3, 3, 5000, 4, 1, 128, 64, lens=[5000, 700, 2], counts=[3, 1, 2], causal=True, seed=4)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [24, 64, 72, 128, 160, 192, 224, 256])
+def test_attend_blocks_for_all_compute_units(dtype, d):
+    """More than 256 blocks of 128 rows: pages that hold less than a tile and more, keys that end inside a tile, pages that are none, causal."""
+    run_attend(dtype, 1, 1000, 150, 33, 33, d, 16, seed=d)
+    run_attend(dtype, 1, 300, 333, 88, 88, d, 100, spoil=1, lens=[331], seed=d + 1)
+    run_attend(dtype, 1, 150, 200, 130, 130, d, 64, causal=True, spoil=1, seed=d + 2)
 
 
 def test_attend_nothing_to_see():
@@ -414,20 +424,21 @@ def test_attend_largest_probability_is_one():
 
 def test_attend_not_finite_stays_where_it_is_seen():
     """A block that is not a number reaches the rows that see it, and no others; what lies past a sample's tokens does not matter."""
-    for tq in (4, 150):
-        k, v = (torch.randn((2, 200, 2, 64), device="cuda") for _ in range(2))
+    for tq, heads, d in ((4, 2, 64), (150, 2, 64), (150, 200, 64), (150, 2, 128), (150, 2, 256), (150, 200, 256)):
+        k, v = (torch.randn((2, 200, heads, d), device="cuda") for _ in range(2))
         v[0, 190, 1, 40] = float("inf")
         k[1, 199, 0, 3] = float("nan")
-        cache, check = new_cache(26, 16, 2, 64)
+        cache, check = new_cache(26, 16, heads, d)
         table = ints(np.arange(26).reshape(2, 13))
         wmdec.cache_write(k.bfloat16(), v.bfloat16(), cache, table)
-        q = torch.randn((2, tq, 4, 64), device="cuda").bfloat16()
-        o = torch.empty_like(q)
-        wmdec.cache_attention(q, cache, table, ints([191, 199]), o, 0.125, 200, causal=True)
-        bad = torch.isnan(o)
-        want = torch.zeros_like(bad)
-        want[0, -1, 2:, 32:] = True                      # the last query alone sees token 190
-        assert torch.equal(bad, want)
+        q = torch.randn((2, tq, 2 * heads, d), device="cuda").bfloat16()
+        for rows in (2 * heads, heads):                  # two query heads a key head, and one
+            o = torch.empty_like(q[:, :, :rows])
+            wmdec.cache_attention(q[:, :, :rows], cache, table, ints([191, 199]), o, 0.125, 200, causal=True)
+            bad = torch.isnan(o)
+            want = torch.zeros_like(bad)
+            want[0, -1, rows // heads:2 * rows // heads, 32:64] = True   # the last query alone sees token 190
+            assert torch.equal(bad, want)
 
 
 def test_attend_bits_do_not_depend_on_the_batch():
