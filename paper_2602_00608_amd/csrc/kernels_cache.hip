@@ -227,9 +227,10 @@ CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   const long blocks = (long)heads * p.row_blocks;
   long ranges;
   if (p.few) {
-    // Up to eight ranges of 256 keys or more, then of 512 or more, at most 64 (us, 256 or 512 keys a range: one token of 32 / 8 heads of 128 against 2048 10.6 / 12.1, 16384
-    // 17.0 / 15.8, 16 x 4096 23.1 / 20.3; 512 or 1024: against 65536 22.8 / 20.5), as long as there are no more than four workgroups a compute unit.
-    ranges = std::min({1024 / blocks, std::max(std::min(8L, tk / 256L), tk / 512L), (long)kCacheMaxSplits});
+    // One range below 640 keys, then of 256 up to eight of them, then of 512 or more and at most 64, as long as there are no more than four workgroups a compute unit (us, one
+    // token of 32 / 8 heads of 128 against 500 keys in one range / two 8.3 / 9.7, 1000 in three / four 10.5 / 9.9, 4000 in eight / sixteen 11.7 / 9.9 but 16 x 4096 20.3 / 22.7, 16384 in 32
+    // / 64 15.8 / 17.0, 65536 in 64 / 128 20.5 / 22.8).
+    ranges = tk < 640 ? 1 : std::min({1024 / blocks, std::max(std::min(8L, (tk + 255L) / 256L), tk / 512L), (long)kCacheMaxSplits});
   } else {
     // Partial outputs of 128 rows weigh: s ranges take a / s for their keys, b * s for writing and reading what they leave, and the second launch.
     const double a = 1.8e-4 * tk * 32 * p.nb, b = 1.2e-6 * 512 * 32 * p.nb * blocks;   // us
