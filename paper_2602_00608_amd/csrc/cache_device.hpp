@@ -12,7 +12,7 @@
 // 4.7 TB/s and the second 4.7, against 65536 20.8, 16 x 4096 in f16 20.3, 2000 10.0, 300 7.3; 30 heads of 64 against 4 x 32768 62 = 4.3 TB/s; 5400x10800 of 30 of 64 in f16 620 = 720 TFLOP/s,
 // 8192x8192 of 32 / 8 of 128 in bf16 1100 = 1000, 2 x 4096x4096 of 16 of 256 677 = 812, 3000x3000 of 8 of 128 in fp32 108 = 341 (products of 32 bits reach 155 at most).
 // Steps, us for 4 x 65536, 16 x 4096, 5400x10800: sixteen rows a wavefront for all sizes, two sets of codes under way 46.7, 24.8, 1157; 128 rows a workgroup 669 of the last; one
-// set, asked for again as soon as it has been used, four wavefronts a SIMD 39.5, 20.8; pages by the wavefront where they are multiples of 32; places from tile to tile 618.
+// set, asked for again as soon as it has been used, four wavefronts a SIMD 39.5, 20.8; pages by the wavefront where they are multiples of 16; places from tile to tile 618.
 // Measured and not kept: two sets of codes under way with few rows (300 to 500 keys 3 % faster, 16 x 4096 26.0 against 22.7), 32 rows a wavefront for few rows (half the wavefronts: 16 x 64 tokens against 4096 294 against 181), 16 wavefronts a workgroup in place of ranges of
 // keys (2000 tokens 14.1 against 10.7, eight samples of 1000 11.8 against 15.7: no better but there), the sum of the probabilities as a product with ones (5400x10800 672), four wavefronts a
 // SIMD at 64 channels and many rows, with what a thread widens worked out anew (645).
@@ -98,7 +98,7 @@ template <int N> struct Words { unsigned w[N]; };
 // their way meanwhile.
 template <typename T, int NB> constexpr int kFewWaves = sizeof(T) == 4 ? (NB <= 2 ? 3 : 2) : NB <= 4 ? 4 : 2;   // a SIMD
 
-// EVEN: pages hold a multiple of 32 tokens, so that 32 keys lie together in one of them: its number and address are the wavefront's, not a lane's.
+// EVEN: pages hold a multiple of 16 tokens, so that 16 keys lie together in one of them: its number and address are the wavefront's, not a lane's.
 template <typename T, int NB, bool EVEN>
 __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(CacheLaunch launch) {
   typedef typename CacheOperand<T>::type O;
@@ -119,13 +119,16 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
   }
   const int rb = L % p.row_blocks, split = L / p.row_blocks % p.splits, h = L / (p.row_blocks * p.splits);
   // pages of 32 keys; where they are the wavefront's, the first are asked for before the sample's length is known
-  struct Place { int number[EVEN ? 1 : 2], slot[EVEN ? 1 : 2]; };   // of keys k0, or k0 + l16 and k0 + 16 + l16; no page past the range
+  struct Place { int number[2], slot[2]; };          // of keys k0 and k0 + 16, or k0 + l16 and k0 + 16 + l16; no page past the range
   const int* table = cp.table + n * cp.table_stride;
   auto find_even = [&](int k0) {
     typedef const __attribute__((address_space(4))) int* uniform_t;
     Place w;
-    const int page = div_rem((unsigned)k0, cp.page_tokens, cp.inv_page_tokens, w.slot[0]);
-    w.number[0] = ((uniform_t)(uintptr_t)table)[min(page, cp.table_pages - 1)];   // (past the range: not used)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int page = div_rem((unsigned)(k0 + 16 * t), cp.page_tokens, cp.inv_page_tokens, w.slot[t]);
+      w.number[t] = ((uniform_t)(uintptr_t)table)[min(page, cp.table_pages - 1)];   // (past the range: not used)
+    }
     return w;
   };
   Place next;
@@ -186,13 +189,12 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
   auto ask = [&](Half& x, bool values, const Place& w) {
     const unsigned codes_at = values ? values_at : 0, to_exps = exps_at + (values ? EXP * cp.page_tokens : 0);
     if constexpr (EVEN) {
-      // (no page: none of them is a key, and what page 0 has instead is taken for zeros)
-      const unsigned char* page = head_of_page(cp, (unsigned)w.number[0] < (unsigned)cp.pages ? w.number[0] : 0, h);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const unsigned row = 16 * t + l16;
-        x.w[t] = *reinterpret_cast<const Words<NB>*>(page + (codes_at + (unsigned)w.slot[0] * ROW + (row * ROW + 4 * NB * g)));
-        x.e[t] = *reinterpret_cast<const E*>(page + (to_exps + (unsigned)w.slot[0] * EXP + row * EXP));
+        // (no page: none of them is a key, and what page 0 has instead is taken for zeros)
+        const unsigned char* page = head_of_page(cp, (unsigned)w.number[t] < (unsigned)cp.pages ? w.number[t] : 0, h);
+        x.w[t] = *reinterpret_cast<const Words<NB>*>(page + (codes_at + (unsigned)w.slot[t] * ROW + (l16 * ROW + 4 * NB * g)));
+        x.e[t] = *reinterpret_cast<const E*>(page + (to_exps + (unsigned)w.slot[t] * EXP + l16 * EXP));
       }
     } else {
 #pragma unroll
@@ -208,7 +210,10 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
     }
   };
   auto keys_of = [&](const Place& w, int k0) {
-    if constexpr (EVEN) return (unsigned)w.number[0] >= (unsigned)cp.pages ? 0u : end - k0 >= 32 ? ~0u : (1u << (end - k0)) - 1;
+    if constexpr (EVEN) {
+      const unsigned here = end - k0 >= 32 ? ~0u : (1u << (end - k0)) - 1;
+      return here & (((unsigned)w.number[0] < (unsigned)cp.pages ? 0xffffu : 0u) | ((unsigned)w.number[1] < (unsigned)cp.pages ? 0xffff0000u : 0u));
+    }
     else return ((unsigned)__ballot((unsigned)w.number[0] < (unsigned)cp.pages) & 0xffffu) | (unsigned)__ballot((unsigned)w.number[1] < (unsigned)cp.pages) << 16;
   };
   // what is no key: zeros (its exponents may be anything)
@@ -834,7 +839,7 @@ int cache_attention_width(const CacheLaunch& l, hipStream_t s) {
   const CachePlan& p = l.plan;
   const int heads = l.a.pages.heads;
   const dim3 grid((unsigned)((long)l.a.n * heads * p.row_blocks * p.splits));
-  const bool even = l.a.pages.page_tokens % 32 == 0;
+  const bool even = l.a.pages.page_tokens % 16 == 0;   // (us, the wavefront's places / a lane's: 4 x 32768 tokens of 30 heads of 64 in pages of 16 64 / 78, of 48 64 / 76, 8 of 128 38 / 40)
   if (!p.few) {
     if constexpr (sizeof(T) == 2) {
       if (!p.halves) cache_launch_many<T, NB, 1>(l, grid, s);
