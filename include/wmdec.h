@@ -416,7 +416,9 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
  * head i / (heads_q / heads).  A query that sees no key, or whose scores are all -inf, gets zeros.
  * q, o: [n,tq,heads_q,d] of dtype as above; 0 < scale <= 2e38; o overlaps nothing.  Scores, softmax and sums are
  * fp32; BF16 and F16 round the probabilities to dtype for the second product, F32 is
- * fp32 throughout; F16 takes keys and values as wmdec_cache_read gives them in F16.  A sample's bits do not depend on
+ * fp32 throughout; F16 takes keys and values as wmdec_cache_read gives them in F16: a value past its range is infinite,
+ * and so is its channel of the queries that see its key (not a number where they see both signs, or where its
+ * weight is below 2^-126 of the largest).  A sample's bits do not depend on
  * what it is batched with.  workspace:
  * wmdec_cache_attention_workspace_bytes(...) bytes (may be 0, and is for sizes that the
  * call refuses), 16-byte aligned, no initialisation; one or two kernels.  A launch of 2^24 workgroups (16

@@ -88,6 +88,53 @@ template <int CHUNKS> __device__ __forceinline__ int tile_turn(int row) {
   else return (row & 2) | ((row >> 2) & 1);
 }
 
+// F16 does not hold every value: of what another type wrote with exponents past 13, what exceeds 65504 is infinite.  Infinities must not get into the products, where
+// nothing times them is not a number for the rows that do not see them (and for those whose probability is nothing in f16).  They are zeros there; where there were
+// any, they are looked for once more behind the last key, and added to the outputs of the rows that see theirs.  (Among the products there are no registers for that.)
+template <typename T> constexpr bool kHasInfinities = std::is_same<T, f16_t>::value;
+constexpr unsigned kLastFiniteExponent = 13 + 127;
+__device__ __forceinline__ bool may_be_infinite(unsigned exponent) { return exponent > kLastFiniteExponent && exponent < 255u; }
+// how many codes of a sign are finite where some may not be: up to 3 * 2^14, 1.5 * 2^15, 0.5 * 2^16, 0
+__device__ __forceinline__ unsigned finite_codes(unsigned exponent) { return exponent == 141 ? 6 : exponent == 142 ? 4 : exponent == 143 ? 2 : 1; }
+__device__ __forceinline__ unsigned infinite_codes(unsigned codes, unsigned finite) { return ((codes & 0x77777777u) + (8 - finite) * 0x11111111u) & 0x88888888u; }   // bit 3 of those
+__device__ __forceinline__ unsigned without_infinities(unsigned codes, unsigned finite) { return codes & ~((infinite_codes(codes, finite) >> 3) * 15u); }
+__device__ __forceinline__ unsigned without_infinities(unsigned word) {   // (of two f16 values)
+  return word & ((word & 0x7fffu) == 0x7c00u ? 0xffff0000u : ~0u) & ((word & 0x7fff0000u) == 0x7c000000u ? 0xffffu : ~0u);
+}
+// bit 7 of the bytes that are above kLastFiniteExponent, where `ones` has a 1 in them
+template <typename E> __device__ __forceinline__ E past_f16(E e, E ones) { return ((e & 127 * ones) + (128 - (kLastFiniteExponent - 127)) * ones) & e & 128 * ones; }
+// A lane's row sees keys up to `see`; element j of its fours of channels STEP i + first .. + 3 is o(i, j).  All lanes of the wavefront, with the same keys.
+template <int NB, int STEP, typename F>
+__device__ __forceinline__ void add_infinities(const CachePages& cp, const int* table, int h, int begin, int end, int see, int first, F o) {
+  const unsigned values_at = 16 * NB * cp.page_tokens, exps_at = 2 * values_at + exponent_bytes(NB) * cp.page_tokens;
+  auto page_of = [&](int key, int& slot) { return head_of_page(cp, table[div_rem((unsigned)key, cp.page_tokens, cp.inv_page_tokens, slot)], h); };
+#pragma unroll 1
+  for (int k0 = begin; k0 < end; k0 += 64) {
+    const int own = k0 + (threadIdx.x & 63);
+    bool any = false;
+    int slot;
+    if (own < end) {
+      if (const unsigned char* page = page_of(own, slot))
+        for (int b = 0; b < NB; ++b) any = any || may_be_infinite(page[exps_at + (unsigned)slot * exponent_bytes(NB) + b]);
+    }
+#pragma unroll 1
+    for (unsigned long keys = __ballot(any); keys; keys &= keys - 1) {
+      const int key = k0 + __builtin_ctzl(keys);
+      const unsigned char* page = page_of(key, slot);
+#pragma unroll
+      for (int i = 0; i < 32 / STEP * NB; ++i) {
+        const unsigned e = page[exps_at + (unsigned)slot * exponent_bytes(NB) + STEP * i / 32];
+        const unsigned codes = *reinterpret_cast<const unsigned short*>(page + (values_at + (unsigned)slot * 16 * NB + (STEP * i + first) / 2));
+        if (!may_be_infinite(e) || key > see) continue;
+        const unsigned infinite = infinite_codes(codes, finite_codes(e));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((infinite >> (4 * j + 3)) & 1u) o(i, j) += (codes >> (4 * j + 3)) & 1u ? -INFINITY : INFINITY;
+      }
+    }
+  }
+}
+
 constexpr float kCacheSlack = 8.0f;   // log2 of how far a maximum may exceed the reference before that moves
 
 template <int N> struct Words { unsigned w[N]; };
@@ -105,6 +152,7 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
   constexpr int PIECES = CacheOperand<T>::pieces, CH = 4 * NB, ROW = 16 * NB, EXP = exponent_bytes(NB), D = 32 * NB, TILES = 2 * NB, RED = D + 4;
   constexpr int TILE_BYTES = 32 * CH * 16, JOIN_BYTES = 2 * 16 * (RED + 2) * 4, SMEM = 4 * TILE_BYTES > JOIN_BYTES ? 4 * TILE_BYTES : JOIN_BYTES;
   __shared__ __align__(16) unsigned char smem[SMEM];
+  __shared__ bool s_infinite[4];
   const CacheAttentionArgs& a = launch.a;
   const CachePages& cp = a.pages;
   const CachePlan& p = launch.plan;
@@ -274,6 +322,16 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
     }
   };
 
+  bool infinite = false;                             // whether there were infinities
+  auto take_out_infinities = [&]() {                 // of the tile
+    infinite = true;
+    int at = lane;
+    asm volatile("" : "+v"(at));                     // (not worked out ahead: there are no registers for that)
+#pragma unroll 1
+    for (; at < 32 * CH * 4; at += 64) reinterpret_cast<unsigned*>(tile)[at] = without_infinities(reinterpret_cast<const unsigned*>(tile)[at]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+
   auto work = [&](int k0) {                          // and asks for the wavefront's next keys as soon as there is room for them
     const bool more = k0 + 128 < end;
     f32x4 s[2];
@@ -292,6 +350,11 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
       }
     }
     if (more) ask(xk, false, next);
+    bool past = false;
+    if constexpr (kHasInfinities<T>) {
+      constexpr EW ones = (EW)0x0101010101010101ul >> (8 * (sizeof(EW) - NB));
+      past = __ballot((past_f16<EW>(xv.e[0], ones) | past_f16<EW>(xv.e[1], ones)) != 0) != 0;
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (the tile has been read)
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -301,6 +364,7 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
     }
     if (more) ask(xv, true, next);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (past) take_out_infinities();
     if (there != ~0u || k0 + 31 > all_see) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -377,6 +441,7 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
   // ---- the wavefronts' sums are joined: 2 and 3 to 0 and 1, then 1 to 0.  A lane has channels 16 i + 4 g .. + 3 of its row
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
+  if (kHasInfinities<T> && lane == 0) s_infinite[wave] = infinite;
   float* s_o = reinterpret_cast<float*>(smem);                       // [2][16][RED]
   float2* s_ml = reinterpret_cast<float2*>(s_o + 2 * 16 * RED);      // [2][16]
 #pragma unroll
@@ -398,7 +463,11 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
       for (int i = 0; i < TILES; ++i) o[i] = o[i] * own + *reinterpret_cast<const f32x4*>(s_o + (wave * 16 + l16) * RED + 16 * i + 4 * g) * other;
     }
   }
-  if (wave > 0 || row >= view.rows) return;
+  if (wave > 0) return;
+  if constexpr (kHasInfinities<T>) {
+    if (s_infinite[0] | s_infinite[1] | s_infinite[2] | s_infinite[3]) add_infinities<NB, 16>(cp, table, h, begin, end, see, 4 * g, [&](int i, int j) -> float& { return ((float*)&o[i])[j]; });
+  }
+  if (row >= view.rows) return;
   if (whole) {
     T* dst = output_row<T>(a, n, h, row);
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -443,6 +512,7 @@ __global__ __launch_bounds__(256 * KW, (ManyForm<NB, KW>::WAVES)) void cache_man
   // what is out of the ordinary in a tile: bits of the keys whose values are not a number, by block; whether there are any (1), or keys without a page (2); those
   constexpr int FLAGS = 2 * NB, GONE = FLAGS + 1, BAD = FLAGS + 3;
   __shared__ unsigned s_bad[3][BAD];
+  __shared__ bool s_infinite;                        // whether there were infinities
   const CacheAttentionArgs& a = launch.a;
   const CachePages& cp = a.pages;
   const CachePlan& p = launch.plan;
@@ -556,13 +626,23 @@ __global__ __launch_bounds__(256 * KW, (ManyForm<NB, KW>::WAVES)) void cache_man
         codes[i] = u32x4{0, 0, 0, 0};
         held[i] = 0;
       }
-      if (held[i] >= 255u) {
-        const bool gone = held[i] == kGone, bad = !gone && a.causal && values;   // (as take_out does for few rows)
+      if (held[i] > (kHasInfinities<T> ? kLastFiniteExponent : 254u)) {
+        const bool gone = held[i] == kGone, bad = held[i] == 255u && a.causal && values;   // (as take_out does for few rows)
         if (gone ? !values && block == 0 : bad) {
           atomicOr(&s_bad[j % 3][(gone ? GONE : 2 * block) + (key >> 5)], 1u << (key & 31));
           atomicOr(&s_bad[j % 3][FLAGS], gone ? 2u : 1u);
         }
         if (gone || bad) held[i] = 0;
+        if (kHasInfinities<T> && values && may_be_infinite(held[i])) {
+          s_infinite = true;
+          unsigned most = finite_codes(held[i]);
+          if constexpr (TIGHT) asm volatile("" : "+v"(most));   // (2 x 4096x4096 of 16 heads of 256 680 us, else 710)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            __builtin_amdgcn_sched_barrier(0);
+            codes[i][c] = without_infinities(codes[i][c], most);
+          }
+        }
       }
       u32x4* to = (values ? s_v : s_k) + (j & 1) * TILE + key * CH;
       const float unit = unit_of(held[i]);
@@ -690,6 +770,7 @@ __global__ __launch_bounds__(256 * KW, (ManyForm<NB, KW>::WAVES)) void cache_man
   };
 
   if (tid < 3 * BAD) s_bad[0][tid] = 0;
+  if (kHasInfinities<T> && tid == 0) s_infinite = false;
   if (tiles > 0) {
     first_place();
     ask();
@@ -754,6 +835,9 @@ __global__ __launch_bounds__(256 * KW, (ManyForm<NB, KW>::WAVES)) void cache_man
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[dt][4 * g + r] = o[dt][4 * g + r] * own + x[r] * other;
       }
+  }
+  if constexpr (kHasInfinities<T>) {
+    if (tiles > 0 && !idle && s_infinite) add_infinities<NB, 8>(cp, table, h, begin, end, see, 4 * lk, [&](int i, int j) -> float& { return ((float*)&o[i / 4])[i % 4 * 4 + j]; });
   }
   if (row >= view.rows) return;
   if (whole) {

@@ -654,3 +654,76 @@ def test_attend_samples_that_share_pages():
         want, weighted = ref.cross_attention(host(q), kh, vh, 0.125, [200, 33, 150])
         assert (np.abs(host(o) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.125, 200, vh)).all()
     check()
+
+
+# ------------------------------------------------------------------ values that the type of the call does not hold
+def attend_what_is_held(dtype, q, kh, vh, scale, lens, causal, source, k, v, page):
+    """Writes k and v as `source`, attends in `dtype`, and compares with the oracle on kh, vh.  An infinite value makes its channel infinite for the queries that see its
+    key (not a number, where they see both signs), and is nothing to the others; what is finite is compared as ever."""
+    n, tq, hq, d = q.shape
+    tk, hk = k.shape[1:3]
+    per = -(-tk // page)
+    table, pages = tables(rng(600), n, per)
+    cache, check = new_cache(pages, page, hk, d)
+    wmdec.cache_write(dev(k, source), dev(v, source), cache, ints(table), None, ints(lens))
+    qd = dev(q, dtype)
+    o = torch.full_like(qd, MARK)
+    need = wmdec.cache_attention_workspace_bytes(qd, cache, tk)
+    wmdec.cache_attention(qd, cache, ints(table), ints(lens), o, scale, tk, causal=causal, workspace=torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"))
+    got = host(o)
+    check()
+    group = hq // hk
+    for b in range(n):
+        seen = np.broadcast_to(np.arange(tk)[None] < lens[b], (tq, tk))
+        if causal:
+            seen = seen & (np.arange(tk)[None] <= lens[b] - tq + np.arange(tq)[:, None])
+        finite = np.where(np.isfinite(vh[b:b + 1]), vh[b:b + 1], 0.0)
+        want, weighted = ref.seen_attention(q[b:b + 1], kh[b:b + 1], finite, scale, seen[None])
+        tol = tolerance(dtype, q[b:b + 1], kh[b:b + 1, :lens[b]], want, weighted, scale, tk, finite)
+        at = np.flatnonzero(~np.isfinite(vh[b]).all((1, 2)))
+        up, down, none = ((seen[:, at, None, None] & x[None, at]).any(1).repeat(group, 1) for x in (vh[b] == np.inf, vh[b] == -np.inf, np.isnan(vh[b])))
+        special = np.where(none | (up & down), np.nan, np.where(up, np.inf, np.where(down, -np.inf, 0.0)))
+        ordinary = special == 0.0
+        assert ordinary.any() and not ordinary.all()
+        g = got[b]
+        bad = np.where(ordinary, ~(np.abs(np.where(ordinary, g, 0.0) - want[0]) <= tol[0]), ~((g == special) | (np.isnan(g) & np.isnan(special))))
+        assert not bad.any(), (b, int(bad.sum()), np.argwhere(bad)[:4].tolist(), g[bad][:4].tolist(), want[0][bad][:4].tolist(), special[bad][:4].tolist())
+
+
+@pytest.mark.parametrize("source", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("tq, tk, hq, hk, d, page", [
+    (4, 90, 2, 2, 40, 16), (5, 100, 8, 2, 64, 33), (3, 2000, 4, 2, 128, 64), (6, 500, 2, 2, 160, 33), (3, 1300, 2, 2, 256, 100), (16, 70, 4, 2, 96, 16), (9, 40, 2, 2, 32, 7),
+    (150, 200, 2, 2, 40, 16), (150, 330, 4, 2, 64, 100), (100, 4000, 2, 2, 128, 100), (140, 150, 2, 2, 160, 16), (130, 260, 2, 2, 224, 64), (70, 300, 2, 2, 256, 31),
+    (300, 200, 88, 88, 64, 64), (300, 150, 90, 90, 96, 16), (150, 180, 130, 130, 192, 32), (260, 330, 90, 90, 256, 100)])
+def test_attend_values_past_f16(source, causal, tq, tk, hq, hk, d, page):
+    """f16 over what another type wrote: values past 65504 are infinite, as cache_read gives them, and reach the queries that see them alone."""
+    r = rng(700 + d + tk)
+    q = G.stored(r.standard_normal((2, tq, hq, d)) * 1.5, "f16")
+    k, v = (r.standard_normal((2, tk, hk, d)) for _ in range(2))
+    last, blocks = min(tq, tk), (d + 31) // 32
+    # blocks whose largest is infinite in f16, and all or some of whose others are not: of a token that all queries see in the first head, of some that the last ones see in the second
+    for b in range(2):
+        v[b, 1, 0, 32 * (blocks - 1):] *= 2.0 ** 15
+        for i, power in enumerate((14, 15, 16, 17, 40)):
+            v[b, tk - 1 - (i * (last - 1)) // 5 - 3 * b, 1, 32 * (i % blocks):32 * (i % blocks) + 32] *= 2.0 ** power
+    k, v = G.stored(k, source), G.stored(v, source)
+    kh, vh = ref.cache_held(k, source), ref.cache_held(v, source)
+    with np.errstate(over="ignore"):
+        vh = vh.astype(np.float16).astype(np.float64)
+    attend_what_is_held("f16", q, kh, vh, float(np.float32(1 / math.sqrt(d))), [tk, tk - 3], causal, source, k, v, page)
+
+
+def test_attend_values_past_f16_whatever_their_weight():
+    """An infinite value counts where its probability is nothing in f16, before and behind larger ones, and where no query of a tile has a score before it."""
+    for tq, tk, slope in ((1, 300, 40), (4, 3000, 40), (120, 300, 40), (1, 300, -40), (4, 3000, -40), (120, 300, -40)):
+        q, k, v = np.zeros((1, tq, 2, 64)), np.zeros((1, tk, 2, 64)), np.ones((1, tk, 2, 64))
+        q[..., 0] = 1.0
+        k[0, :, :, 0] = np.linspace(-slope, slope, tk)[:, None]
+        v[0, 3, 0, 5], v[0, tk - tq, 1, 40], v[0, tk // 2, 1, 41] = 1e6, -1e30, 3e5
+        v[0, :, 0, 7] = np.arange(tk) % 5
+        k, v = G.stored(k, "bf16"), G.stored(v, "bf16")
+        with np.errstate(over="ignore"):
+            kh, vh = ref.cache_held(k, "bf16"), ref.cache_held(v, "bf16").astype(np.float16).astype(np.float64)
+        for causal in (False, True):
+            attend_what_is_held("f16", q, kh, vh, 1.0, [tk], causal, "bf16", k, v, 32)
