@@ -136,6 +136,11 @@ __device__ __forceinline__ void add_infinities(const CachePages& cp, const int* 
 }
 
 constexpr float kCacheSlack = 8.0f;   // log2 of how far a maximum may exceed the reference before that moves
+// (The difference, not the sum: from 2^27 on the reference and eight more may round to the next score, whose probability of 2^16 is infinite in f16.)
+__device__ __forceinline__ bool is_past(float mx, float m) {
+#pragma clang fp contract(off)
+  return mx - m > kCacheSlack;
+}
 
 template <int N> struct Words { unsigned w[N]; };
 
@@ -385,10 +390,10 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
           s[t][r] = s[t][r] * c;
           mx = __builtin_elementwise_maximum(mx, s[t][r]);
         }
-      if (__ballot(mx > m + kCacheSlack)) {          // all lanes of a row move together
+      if (__ballot(is_past(mx, m))) {               // all lanes of a row move together
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const bool moves = mx > m + kCacheSlack;
+        const bool moves = is_past(mx, m);
         const float factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
         m = moves ? mx : m;
         l = l * factor;
@@ -721,7 +726,7 @@ __global__ __launch_bounds__(256 * KW, (ManyForm<NB, KW>::WAVES)) void cache_man
     for (int i = 3; i + 1 < 16 * NS; i += 2) mx = maximum(maximum(mx, s[i / 16][i % 16]), s[(i + 1) / 16][(i + 1) % 16]);
     mx = maximum(mx, s[NS - 1][15]);
     mx = half_max(mx) * c;
-    const bool moves = mx > m + kCacheSlack;
+    const bool moves = is_past(mx, m);
     if (__ballot(moves)) {
       const float to = moves ? mx : m, factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
       m = to;

@@ -727,3 +727,24 @@ def test_attend_values_past_f16_whatever_their_weight():
             kh, vh = ref.cache_held(k, "bf16"), ref.cache_held(v, "bf16").astype(np.float16).astype(np.float64)
         for causal in (False, True):
             attend_what_is_held("f16", q, kh, vh, 1.0, [tk], causal, "bf16", k, v, 32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attend_scores_half_a_step_beside_the_reference(dtype):
+    """From 2^27 on fp32 holds scores in steps of 16, and a reference and eight more may be the next score: that one's probability is 2^16 unless the reference moves,
+    which f16 does not hold.  Two keys alone have weight, with values of 1 and 2: an output lies between them."""
+    for tq in (1, 5, 140):
+        for low, high in ((8, 24), (16, 24), (32, 48)):
+            k, v = np.zeros((1, 200, 2, 64)), np.ones((1, 200, 2, 64))
+            k[0, (5, 133), :, 0] = 4096.0
+            k[0, 5, :, 32], k[0, 133, :, 32] = low, high
+            v[0, 133] = 2.0
+            cache, check = new_cache(13, 16, 2, 64)
+            table = ints([list(range(13))])
+            wmdec.cache_write(dev(k, dtype), dev(v, dtype), cache, table)
+            q = torch.zeros((1, tq, 2, 64), dtype=G.TORCH[dtype], device="cuda")
+            q[..., 0], q[..., 32] = 22720.0, 1.0
+            o = torch.empty_like(q)
+            wmdec.cache_attention(q, cache, table, ints([200]), o, 1.0, 200)
+            assert bool(((o >= 1.0) & (o <= 2.0)).all()), (tq, low, high, o.flatten()[:4].tolist())
+            check()
