@@ -93,6 +93,11 @@ template <typename T> __device__ __forceinline__ void store_quad(T* row, int at,
 }
 
 constexpr float kCrossSlack = 8.0f;   // log2 of how far a tile's maximum may exceed the reference before that moves
+// (The difference, not the sum: from 2^27 on the reference and eight more may round to the next score, whose probability of 2^16 is infinite in f16.)
+__device__ __forceinline__ bool is_past(float mx, float m) {
+#pragma clang fp contract(off)
+  return mx - m > kCrossSlack;
+}
 
 // MASKED: tiles are made of the valid keys alone, whose places are worked out for up to kMaskKeys keys at a time
 template <typename T, int D, int QW, int KW, int KT, int WAVES, bool MASKED>
@@ -326,7 +331,7 @@ __global__ __launch_bounds__(64 * QW * KW, WAVES) void cross_attention_kernel(Cr
     for (int i = 3; i + 1 < 16 * NS; i += 2) mx = maximum(maximum(mx, s[i / 16][i % 16]), s[(i + 1) / 16][(i + 1) % 16]);
     mx = maximum(mx, s[NS - 1][15]);
     mx = half_max(mx) * c;
-    const bool moves = mx > m + kCrossSlack;
+    const bool moves = is_past(mx, m);
     if (__ballot(moves)) {
       const float to = moves ? mx : m, factor = moves ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
       m = to;

@@ -811,3 +811,20 @@ def test_calls_follow_the_current_stream():
                 b.run()
         torch.cuda.synchronize()
         assert all(torch.equal(b.x2, w) for b, w in zip(blocks, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_cross_scores_half_a_step_beside_the_reference(dtype):
+    """From 2^27 on fp32 holds scores in steps of 16, and a reference and eight more may be the next score: that one's probability is 2^16 unless the reference moves,
+    which f16 does not hold.  Two keys alone have weight, with values of 1 and 2: an output lies between them."""
+    for tq in (1, 40, 140):
+        for low, high in ((8, 24), (16, 24), (32, 48)):
+            q, k, v = (torch.zeros((1, t, 2, 64), dtype=G.TORCH[dtype], device="cuda") for t in (tq, 600, 600))
+            q[..., 0], q[..., 32] = 22720.0, 1.0
+            k[0, 5, :, 0] = k[0, 517, :, 0] = 4096.0
+            k[0, 5, :, 32], k[0, 517, :, 32] = low, high
+            v[:], v[0, 517] = 1.0, 2.0
+            o = torch.empty_like(q)
+            ws = torch.empty(max(16, wmdec.cross_attention_workspace_bytes(q, k)), dtype=torch.uint8, device="cuda")
+            wmdec.cross_attention(q, k, v, o, 1.0, workspace=ws)
+            assert bool(((o >= 1.0) & (o <= 2.0)).all()), (tq, low, high, o.flatten()[:4].tolist())
