@@ -46,12 +46,38 @@ template <typename T> struct CacheOperand { typedef T type; static constexpr int
 template <> struct CacheOperand<float> { typedef bf16_t type; static constexpr int pieces = 3; };
 
 // the sum of the pieces is x (to 24 bits)
-__device__ __forceinline__ void split3(float a, float b, unsigned (&w)[3]) {
-  w[0] = pack2<bf16_t>(a, b);
-  a -= unpack_lo<bf16_t>(w[0]); b -= unpack_hi<bf16_t>(w[0]);
+__device__ __forceinline__ void split_rest(float a, float b, unsigned (&w)[3]) {
   w[1] = pack2<bf16_t>(a, b);
   a -= unpack_lo<bf16_t>(w[1]); b -= unpack_hi<bf16_t>(w[1]);
   w[2] = pack2<bf16_t>(a, b);
+}
+__device__ __forceinline__ void split3(float a, float b, unsigned (&w)[3]) {
+  w[0] = pack2<bf16_t>(a, b);
+  split_rest(a - unpack_lo<bf16_t>(w[0]), b - unpack_hi<bf16_t>(w[0]), w);
+}
+// eight of any numbers: those that bf16 would round to infinity have its largest as their first piece, and infinities have no rest
+__device__ __forceinline__ void split3_any(f32x4 x, f32x4 y, unsigned (&w)[4][3]) {
+  float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}, top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
+  if (!__ballot(top > 0x1.fep127f)) {                // bf16's largest
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split3(v[2 * i], v[2 * i + 1], w[i]);
+    return;
+  }
+  float first[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool past = fabsf(v[i]) > 0x1.fep127f, infinite = fabsf(v[i]) == INFINITY;
+    first[i] = past && !infinite ? copysignf(0x1.fep127f, v[i]) : v[i];
+    if (infinite) v[i] = 0.f;
+    else v[i] -= past ? first[i] : unpack_lo<bf16_t>(pack2<bf16_t>(first[i], 0.f));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i][0] = pack2<bf16_t>(first[2 * i], first[2 * i + 1]);
+    split_rest(v[2 * i], v[2 * i + 1], w[i]);
+  }
 }
 
 // what is in the cache for a sample, and how far a block of rows sees of it
@@ -208,7 +234,7 @@ __global__ __launch_bounds__(256, (kFewWaves<T, NB>)) void cache_few_kernel(Cach
         if constexpr (sizeof(T) == 4) {
           const f32x4 x = *reinterpret_cast<const f32x4*>(src + at), y = *reinterpret_cast<const f32x4*>(src + at + 4);
           unsigned w[4][3];
-          split3(x[0], x[1], w[0]); split3(x[2], x[3], w[1]); split3(y[0], y[1], w[2]); split3(y[2], y[3], w[3]);
+          split3_any(x, y, w);
 #pragma unroll
           for (int i = 0; i < 3; ++i) q[s][i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
         } else {

@@ -748,3 +748,49 @@ def test_attend_scores_half_a_step_beside_the_reference(dtype):
             wmdec.cache_attention(q, cache, table, ints([200]), o, 1.0, 200)
             assert bool(((o >= 1.0) & (o <= 2.0)).all()), (tq, low, high, o.flatten()[:4].tolist())
             check()
+
+
+def test_attend_queries_at_the_end_of_fp32():
+    """fp32 queries go into the products in pieces; those next to the largest number, and infinite ones, are in order too."""
+    top = 3.4028234e38
+    for tq in (1, 40):
+        q = np.zeros((1, tq, 1, 64))
+        q[..., 0] = np.array([top, -top, 3.39e38, 3.3961776e38, 3.3961775e38])[np.arange(tq) % 5][None, :, None]
+        q = G.stored(q, "f32")
+        k = np.zeros((1, 50, 1, 64))
+        k[0, :, 0, 0] = 2.0 ** -125 * np.array([0.5, 1, 1.5, 2, 3, 4, -2, 0])[np.arange(50) % 8]
+        v = rng(41).standard_normal((1, 50, 1, 64))
+        cache, check = new_cache(4, 16, 1, 64)
+        table = ints([[1, 3, 0, 2]])
+        wmdec.cache_write(dev(k, "f32"), dev(v, "f32"), cache, table)
+        qd = dev(q, "f32")
+        o = torch.full_like(qd, MARK)
+        wmdec.cache_attention(qd, cache, table, ints([50]), o, 1.0, 50)
+        kh, vh = ref.cache_held(k, "f32"), ref.cache_held(G.stored(v, "f32"), "f32")
+        want, weighted = ref.cross_attention(q, kh, vh, 1.0)
+        # (the tolerance of test_attend_*, whose bound on the scores, sums of 64 |q| |k|, is of their magnitude here)
+        with np.errstate(over="ignore"):
+            size = float(np.abs(q[0, :, 0, :1] * kh[0, :, 0, 0][None]).max())
+        fp32 = 2 * (3 * 64 + 8) * U * size + (math.sqrt(50) + 64) * 2 * U
+        assert (np.abs(host(o) - want) <= U * np.abs(want) + fp32 * weighted + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attend_scores_of_minus_infinity(dtype):
+    """A query whose scores are all -inf gets zeros; the others are not touched by it."""
+    for tq in (2, 80):
+        q = rng(42).standard_normal((1, tq, 1, 64))
+        k, v = rng(43).standard_normal((1, 60, 1, 64)), rng(44).standard_normal((1, 60, 1, 64))
+        k[..., 0] = 1.0 + np.abs(k).max()
+        q[0, 0, 0, 0] = -np.inf
+        cache, check = new_cache(4, 16, 1, 64)
+        table = ints([[1, 3, 0, 2]])
+        wmdec.cache_write(dev(k, dtype), dev(v, dtype), cache, table)
+        qd = dev(q, dtype)
+        o = torch.full_like(qd, MARK)
+        wmdec.cache_attention(qd, cache, table, ints([60]), o, 0.125, 60)
+        assert not o[0, 0].any()
+        kh, vh = (ref.cache_held(G.stored(x, dtype), dtype) for x in (k, v))
+        rest = G.stored(q[:, 1:], dtype)
+        want, weighted = ref.cross_attention(rest, kh, vh, 0.125)
+        assert (np.abs(host(o[:, 1:]) - want) <= tolerance(dtype, rest, kh, want, weighted, 0.125, 60, vh)).all()
