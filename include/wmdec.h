@@ -422,7 +422,8 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
  * what it is batched with.  workspace:
  * wmdec_cache_attention_workspace_bytes(...) bytes (may be 0, and is for sizes that the
  * call refuses), 16-byte aligned, no initialisation; one or two kernels.  A launch of 2^24 workgroups (16
- * rows of a key head or more, and a range of its keys each) or more is refused, and
+ * rows of a key head or more, and a range of its keys each) or more is refused, one of 2^23 where a sample has
+ * 256 or less of 128 rows each (they have 512 threads then, but for 97 to 128 channels), and
  * one of 2^26 rows or more where keys are divided into ranges. */
 typedef struct {
   void* data;

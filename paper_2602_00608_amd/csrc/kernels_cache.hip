@@ -254,7 +254,7 @@ size_t part_rows(const CachePlan& p, int n, int heads) { return p.splits == 1 ? 
 bool cache_attention_fits(int dtype, int n, int tq, int tk, int heads, int group, int d) {
   const CachePlan p = plan_of(dtype, tq, tk, heads, group, d);
   const double blocks = (double)n * heads * p.row_blocks;
-  return blocks * p.splits < 0x1p24 && (p.splits == 1 || (double)n * heads * p.rows < 0x1p26);
+  return blocks * p.splits * (p.halves ? 512 : 256) < 0x1p32 && (p.splits == 1 || (double)n * heads * p.rows < 0x1p26);   // threads of a launch; rows that are joined
 }
 
 size_t cache_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d) {

@@ -225,3 +225,13 @@ def test_library_refusals_come_through_the_binding():
     with pytest.raises(wmdec.WmdecError) as e:
         wmdec._check(_attend(cache=_cache(d=60)))
     assert e.value.status == wmdec.ERR_UNSUPPORTED and "multiple of 8" in str(e.value)
+
+
+def test_launches_of_2_to_the_32_threads_are_refused():
+    """Workgroups of eight wavefronts count twice."""
+    wide = dict(cache=_cache(heads=1, d=8), table=_table(stride=0), qs=S(520, 8, 8), os=S(520, 8, 8), hq=1, tq=65)
+    assert _attend(**dict(wide, n=1 << 23)) == wmdec.ERR_UNSUPPORTED and "too many" in wmdec.last_error()
+    assert _attend(**dict(wide, cache=_cache(heads=1, d=128), qs=S(65 * 128, 128, 128), os=S(65 * 128, 128, 128), n=1 << 24)) == wmdec.ERR_UNSUPPORTED   # (four at this width)
+    assert _attend(**dict(wide, dtype=0, n=1 << 22)) == wmdec.ERR_UNSUPPORTED                                                                    # (blocks of 16 rows)
+    for heads, n in ((128, 1 << 16), (256, 1 << 15)):
+        assert _attend(**dict(wide, cache=_cache(heads=heads, d=8), qs=S(65 * 8 * heads, 8 * heads, 8), os=S(65 * 8 * heads, 8 * heads, 8), hq=heads, n=n)) == wmdec.ERR_UNSUPPORTED

@@ -794,3 +794,19 @@ def test_attend_scores_of_minus_infinity(dtype):
         rest = G.stored(q[:, 1:], dtype)
         want, weighted = ref.cross_attention(rest, kh, vh, 0.125)
         assert (np.abs(host(o[:, 1:]) - want) <= tolerance(dtype, rest, kh, want, weighted, 0.125, 60, vh)).all()
+
+
+def test_attend_as_many_samples_as_a_launch_takes():
+    n = (1 << 23) - 1
+    k, v = (torch.randn((1, 3, 1, 8), device="cuda").bfloat16() for _ in range(2))
+    cache, check = new_cache(1, 16, 1, 8)
+    wmdec.cache_write(k, v, cache, ints([[0]]))
+    q = torch.randn((1, 65, 1, 8), device="cuda").bfloat16()
+    o = torch.full((n, 65, 1, 8), MARK, dtype=torch.bfloat16, device="cuda")
+    wmdec.cache_attention(q.expand(n, 65, 1, 8), cache, ints([[0]]).expand(n, 1), torch.full((n,), 3, dtype=torch.int32, device="cuda"), o, 0.3, 3)
+    kh, vh = (ref.cache_held(host(x), "bf16") for x in (k, v))
+    want, weighted = ref.cross_attention(host(q), kh, vh, 0.3)
+    assert (np.abs(host(o[:1]) - want) <= tolerance("bf16", host(q), kh, want, weighted, 0.3, 3, vh)).all()
+    for at in range(0, n, 1 << 20):
+        assert bool((o[at:at + (1 << 20)] == o[:1]).all())
+    check()
