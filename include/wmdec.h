@@ -404,7 +404,7 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
  * wmdec_cache_read is the way back, rounded once to dtype; rows of k and v from counts[i] on are
  * left as they were.  k or v may be NULL.  Strides in elements, channels
  * contiguous, pointers and strides multiples of 16 bytes; outputs overlap nothing.
- * A call of 2^26 wavefronts or more, with a head and 2 to 16 tokens of a sample each, is refused.
+ * A call of more than 2^26 - 4 wavefronts, with a head and 2 to 16 tokens of a sample each, is refused.
  *
  * wmdec_cache_attention: o = softmax over the keys (scale * q k^T) v of tq queries per
  * sample to its first lens[i] tokens in the cache (int32 [n]; clamped to 0 .. tk and to

@@ -206,7 +206,7 @@ size_t cache_head_bytes(int page_tokens, int d) {
   return ((size_t)page_tokens * 2 * (16 * nb + exponent_bytes(nb)) + 15) / 16 * 16;
 }
 
-bool cache_tokens_fit(int n, int t, int heads, int d) { return (double)n * chunks_of(t, d, 4) * heads < 0x1p26; }   // (64 threads each)
+bool cache_tokens_fit(int n, int t, int heads, int d) { return (double)n * chunks_of(t, d, 4) * heads <= 0x1p26 - 4; }   // (64 threads each, in whole workgroups of 256)
 
 int launch_cache_write(const CacheTokens& a, int dtype, hipStream_t s) { return launch_type<true>(a, dtype, s); }
 int launch_cache_read(const CacheTokens& a, int dtype, hipStream_t s) { return launch_type<false>(a, dtype, s); }

@@ -235,3 +235,12 @@ def test_launches_of_2_to_the_32_threads_are_refused():
     assert _attend(**dict(wide, dtype=0, n=1 << 22)) == wmdec.ERR_UNSUPPORTED                                                                    # (blocks of 16 rows)
     for heads, n in ((128, 1 << 16), (256, 1 << 15)):
         assert _attend(**dict(wide, cache=_cache(heads=heads, d=8), qs=S(65 * 8 * heads, 8 * heads, 8), os=S(65 * 8 * heads, 8 * heads, 8), hq=heads, n=n)) == wmdec.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("name", ["cache_write", "cache_read"])
+def test_tokens_of_2_to_the_32_threads_are_refused(name):
+    """Workgroups are whole: one to three wavefronts less than 2^26 fill as many."""
+    for heads, n, t in ((2731, 8191, 48), (62, 1082401, 1)):   # a head and sixteen tokens of fp32 each: 2^26 - 1, 2^26 - 2
+        states = S(t * heads * 8, heads * 8, 8)
+        assert _tokens("wmdec_" + name, cache=_cache(page_tokens=1, heads=heads, d=8), table=_table(stride=0), dtype=0, ks=states, vs=states, n=n, t=t) == wmdec.ERR_UNSUPPORTED
+        assert "too many" in wmdec.last_error()

@@ -810,3 +810,19 @@ def test_attend_as_many_samples_as_a_launch_takes():
     for at in range(0, n, 1 << 20):
         assert bool((o[at:at + (1 << 20)] == o[:1]).all())
     check()
+
+
+def test_store_as_many_tokens_as_a_launch_takes():
+    """2^26 - 4 wavefronts."""
+    n, heads = 4097, 16380
+    assert n * heads == (1 << 26) - 4
+    k = torch.randn((n, 1, heads, 8), device="cuda")
+    cache, check = new_cache(n, 1, heads, 8)
+    table = torch.arange(n, dtype=torch.int32, device="cuda").flip(0).contiguous()[:, None]
+    wmdec.cache_write(k, None, cache, table)
+    out = torch.full_like(k, MARK)
+    wmdec.cache_read(cache, table, out, None)
+    for at in (0, 1, 2047, n - 1):
+        same_values(host(out[at]), ref.cache_held(host(k[at]), "f32"))
+    assert bool((out.abs() <= 8).all()) and not bool((out == MARK).any())
+    check()
