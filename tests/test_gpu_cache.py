@@ -826,3 +826,41 @@ def test_store_as_many_tokens_as_a_launch_takes():
         same_values(host(out[at]), ref.cache_held(host(k[at]), "f32"))
     assert bool((out.abs() <= 8).all()) and not bool((out == MARK).any())
     check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [40, 72, 160, 256])
+@pytest.mark.parametrize("page", [16, 33])
+@pytest.mark.parametrize("tq, tk, hq, hk", [(4, 90, 2, 2), (3, 1400, 4, 2), (150, 200, 2, 2), (100, 4000, 2, 2), (300, 150, 88, 88)])
+def test_attend_not_a_number_by_block(dtype, d, page, tq, tk, hq, hk):
+    """Blocks of values that are not a number, the last of a head among them, in tiles that some of a block's rows see, whose sums are joined from ranges or not."""
+    r = rng(800 + d)
+    q = G.stored(r.standard_normal((2, tq, hq, d)) * 1.5, dtype)
+    k, v = (G.stored(r.standard_normal((2, tk, hk, d)), dtype) for _ in range(2))
+    blocks, last = (d + 31) // 32, min(tq, tk)
+    for b in range(2):
+        v[b, tk - 1 - 3 * b, 0, 32 * (blocks - 1) + 7] = np.nan
+        v[b, tk - 1 - last // 2, 1, 32 * (blocks // 2) + 1] = np.inf
+        v[b, tk - last, 1, 32 * (blocks // 3)] = -np.inf
+    kh, vh = ref.cache_held(k, dtype), ref.cache_held(v, dtype)
+    for causal in (True, False):
+        attend_what_is_held(dtype, q, kh, vh, float(np.float32(1 / math.sqrt(d))), [tk, tk - 3], causal, dtype, k, v, page)
+
+
+def test_attend_keys_that_are_not_a_number():
+    """A key that is not a number makes every channel of the queries that see it so, and is nothing to the others."""
+    for dtype, tq, tk, d, page in (("bf16", 4, 90, 160, 16), ("f16", 5, 1400, 72, 33), ("f32", 4, 700, 256, 16), ("bf16", 150, 200, 160, 33), ("f16", 100, 4000, 64, 100)):
+        q, k, v = (torch.randn((1, t, 2, d), device="cuda").to(G.TORCH[dtype]) for t in (tq, tk, tk))
+        bad = tk - 1 - tq // 2
+        k[0, bad, 1, d - 1] = float("nan")
+        per = -(-tk // page)
+        cache, check = new_cache(per, page, 2, d)
+        table = ints(rng(45).permutation(per)[None])
+        wmdec.cache_write(k, v, cache, table)
+        o = torch.empty_like(q)
+        ws = torch.empty(max(16, wmdec.cache_attention_workspace_bytes(q, cache, tk)), dtype=torch.uint8, device="cuda")
+        wmdec.cache_attention(q, cache, table, ints([tk]), o, 0.1, tk, causal=True, workspace=ws)
+        want = torch.zeros_like(o, dtype=torch.bool)
+        want[0, tq - 1 - tq // 2:, 1] = True
+        assert torch.equal(torch.isnan(o), want)
+        check()
