@@ -392,8 +392,9 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
  * sample; stride 0: the same pages for all samples), at place p % page_tokens.  A page number
  * outside 0 .. pages - 1 is no page: what would be written there is dropped, what
  * would be read is zeros, and its keys do not count; so for tokens past the row's end.  Samples may
- * share pages that are read; of two tokens that one call writes to the same place, either may be what is held of each block
- * there, and calls that write and read the same pages have to be ordered on one stream.
+ * share pages that are read; two tokens that one call writes to the same place leave what both are held as where that is
+ * the same, else a mixture of them, values of the one with powers of two of the other among it; and calls that write and read
+ * the same pages have to be ordered on one stream.
  * d: a multiple of 8, at most 256; page_tokens 1 to 65536; heads at most 16384; a page
  * less than 2 GiB (wmdec_cache_page_bytes is 0 for sizes that are refused); count *
  * page_tokens at most 2^31 - 2048.
@@ -418,8 +419,9 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
  * fp32; BF16 and F16 round the probabilities to dtype for the second product, F32 is
  * fp32 throughout; F16 takes keys and values as wmdec_cache_read gives them in F16: a value past its range is infinite,
  * and so is its channel of the queries that see its key (not a number where they see both signs, or where its
- * weight is below 2^-126 of the largest).  A sample's bits do not depend on
- * what it is batched with.  workspace:
+ * weight is below 2^-126 of the largest).  Probabilities reach 2^8 before
+ * they are divided by their sum, so sums of values past 2^120 may overflow.  A sample's bits depend on tq and tk (which decide
+ * how the work is divided), not on what else it is batched with.  workspace:
  * wmdec_cache_attention_workspace_bytes(...) bytes (may be 0, and is for sizes that the
  * call refuses), 16-byte aligned, no initialisation; one or two kernels.  A launch of 2^24 workgroups (16
  * rows of a key head or more, and a range of its keys each) or more is refused, one of 2^23 where a sample has
