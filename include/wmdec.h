@@ -417,7 +417,7 @@ int wmdec_cross_attention(const void* q, const wmdec_strides* q_strides, const v
  * head i / (heads_q / heads).  A query that sees no key, or whose scores are all -inf, gets zeros.
  * q, o: [n,tq,heads_q,d] of dtype as above; 0 < scale <= 2e38; o overlaps nothing.  Scores, softmax and sums are
  * fp32; BF16 and F16 round the probabilities to dtype for the second product, F32 is
- * fp32 throughout; F16 takes keys and values as wmdec_cache_read gives them in F16: a value past its range is infinite,
+ * fp32 throughout (of queries and probabilities what is below 2^-133 is lost); F16 takes keys and values as wmdec_cache_read gives them in F16: a value past its range is infinite,
  * and so is its channel of the queries that see its key (not a number where they see both signs, or where its
  * weight is below 2^-126 of the largest).  Probabilities reach 2^8 before
  * they are divided by their sum, so sums of values past 2^120 may overflow.  A sample's bits depend on tq and tk (which decide

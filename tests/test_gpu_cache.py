@@ -864,3 +864,28 @@ def test_attend_keys_that_are_not_a_number():
         want[0, tq - 1 - tq // 2:, 1] = True
         assert torch.equal(torch.isnan(o), want)
         check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attend_scales_of_any_size(dtype):
+    """Scales at both ends of what is taken, with queries that bring the scores back to their size, or not."""
+    for tq in (2, 90):
+        for scale, size in ((1e-45, 1.0), (1e-39, 1.0), (2.0 ** -10, 2.0 ** 10)) + (((2e38, 2.0 ** -126), (1e38, 2.0 ** -121)) if dtype != "f16" else ((2.0 ** 24, 2.0 ** -24), (2.0 ** 20, 2.0 ** -18))):
+            r = rng(900 + tq)
+            q = G.stored(r.standard_normal((1, tq, 2, 64)) * size, dtype)
+            k, v = (G.stored(r.standard_normal((1, 150, 2, 64)), dtype) for _ in range(2))
+            cache, check = new_cache(10, 16, 2, 64)
+            table = ints([list(range(10))])
+            wmdec.cache_write(dev(k, dtype), dev(v, dtype), cache, table)
+            qd = dev(q, dtype)
+            o = torch.full_like(qd, MARK)
+            scale = float(np.float32(scale))
+            wmdec.cache_attention(qd, cache, table, ints([150]), o, scale, 150, causal=True)
+            kh, vh = (ref.cache_held(x, dtype) for x in (k, v))
+            seen = (np.arange(150)[None] <= 150 - tq + np.arange(tq)[:, None])[None]
+            want, weighted = ref.seen_attention(q, kh, vh, scale, seen)
+            tol = tolerance(dtype, q, kh, want, weighted, scale, 150, vh)
+            if dtype == "f32":   # the last of a query's three pieces is a bf16 number, in steps of 2^-133: an element is off by half of one, a score by that times |k|, and a weight by a factor of twice that score's exponential
+                tol = tol + math.expm1(2 * 2.0 ** -134 * float(np.abs(kh).sum(-1).max()) * scale) * weighted
+            bad = ~(np.abs(host(o) - want) <= tol)
+            assert not bad.any(), (tq, scale, size, int(bad.sum()), np.abs(host(o) - want)[bad].max())
