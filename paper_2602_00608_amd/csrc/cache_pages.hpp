@@ -14,7 +14,7 @@ namespace wmdec {
 
 __host__ __device__ constexpr int exponent_bytes(int blocks) { return blocks <= 1 ? 1 : blocks <= 2 ? 2 : blocks <= 4 ? 4 : 8; }
 
-// the head's part of the page that holds token `at` of sample n; null where there is none
+// head h's part of page `number`; null where that is no page
 __device__ __forceinline__ unsigned char* head_of_page(const CachePages& p, int number, int h) {
   return (unsigned)number < (unsigned)p.pages ? p.data + (unsigned long)number * p.page_bytes + (unsigned long)((unsigned)h * p.head_bytes) : nullptr;
 }

@@ -236,7 +236,7 @@ bool cross_attention_fits(int dtype, int n, int tq, int tk, int heads, int group
 size_t cross_attention_scratch_bytes(int dtype, int n, int tq, int tk, int heads, int group, int d);
 int launch_cross_attention(const CrossArgs& a, int dtype, hipStream_t s);
 
-// kernels_cache.hip: keys and values in four bits, in pages (the layout is described in cache_device.hpp)
+// kernels_cache.hip: keys and values in four bits, in pages (the layout is described in cache_pages.hpp)
 struct CachePages {
   unsigned char* data = nullptr;
   const int* table = nullptr; long table_stride = 0;   // page numbers, a row a sample

@@ -221,7 +221,7 @@ CachePlan plan_of(int dtype, int tq, int tk, int heads, int group, int d) {
   p.rows = tq * group;
   // us, blocks of 16 rows / of 128: bf16, causal, 32 / 8 heads of 128, 64 rows a key head against 2048 keys 11.2 / 16.0, 16384 21.4 / 31.1, 16 x 4096 80 / 72; 128 rows against
   // 2048 13.3 / 18.1, 16 x 4096 137 / 90; 100 of 30 heads of 64 against 2000 15.0 / 18.7, 16 x 1000 62 / 31.  In fp32, where products weigh more than what is widened for
-  // them, all: 1000x1000 of 12 of 64 19 / 30, four of 1000x3000 of 8 of 128 161 / 221, 2000x2000 of 16 of 160 138 / 205, of 192 247 / 226.
+  // them, all: 1000x1000 of 12 of 64 19 / 30, four of 1000x3000 of 8 of 128 161 / 221, 2000x2000 of 16 of 160 138 / 205, of 192 161 / 226.
   p.few = p.rows <= 64 || dtype == WMDEC_F32;
   p.row_blocks = (p.rows + p.bq() - 1) / p.bq();
   const long blocks = (long)heads * p.row_blocks;
