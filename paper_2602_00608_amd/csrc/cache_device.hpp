@@ -10,8 +10,8 @@
 // vector instructions a wavefront and tile of 64 keys at 64 channels, 32 are exponentials of four times the cycles.
 // us on inputs that are not the call's before, host included, over several boxes: one token of 32 / 8 heads of 128 against 4 x 65536 tokens (ragged) in bf16 39 to 41 (under the tracer the
 // first kernel 35 = 4.0 TB/s and the second 4.8), in fp32 51 to 54, against 65536 21 to 22, 16 x 4096 in f16 20.3 to 23 (18.1 and 4.6), in fp32 28 to 32, 2000 10 to 11, 300 7.3 to 7.9; 30 heads of 64
-// against 4 x 32768 62 to 66 = 4.1 to 4.3 TB/s; 5400x10800 of 30 of 64 in f16 618 to 670 = 725 to 669 TFLOP/s (to 695 under the tracer), 8192x8192 of 32 / 8 of 128 in bf16 1100 to 1120 = 1000 to 982, in f16
-// 1130 to 1195 (to 1210), 2 x 4096x4096 of 16 of 256 680 = 806, 3000x3000 of 8 of 128 in fp32 108 to 113 = 341 to 326 (products of 32 bits reach 155 at most).
+// against 4 x 32768 62 to 66 = 4.1 to 4.3 TB/s; 5400x10800 of 30 of 64 in f16 618 to 700 = 725 to 640 TFLOP/s, 8192x8192 of 32 / 8 of 128 in bf16 1100 to 1120 = 1000 to 982, in f16 1130 to 1215
+// (the longer the call is repeated, the slower), 2 x 4096x4096 of 16 of 256 680 = 806, 3000x3000 of 8 of 128 in fp32 108 to 113 = 341 to 326 (products of 32 bits reach 155 at most).
 // Steps, us for 4 x 65536, 16 x 4096, 5400x10800: sixteen rows a wavefront for all sizes, two sets of codes under way 46.7, 24.8, 1157; 128 rows a workgroup 669 of the last; one
 // set, asked for again as soon as it has been used, four wavefronts a SIMD 39.5, 20.8; pages by the wavefront where they are multiples of 16; places from tile to tile 653 to 624 of the last;
 // infinities of f16 taken out, no more than 1 %.
